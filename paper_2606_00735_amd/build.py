@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmoe.so")
 
 SOURCES = ["route_kernels.hip", "ffn_kernels.hip", "mx_kernels.hip", "placement_kernels.hip", "moe_abi.cpp"]
-HEADERS = ["common.hpp", "launch.hpp", "mx.hpp"]
+HEADERS = ["common.hpp", "grouped_gemm.hpp", "launch.hpp", "mx.hpp"]
 
 
 def hipcc() -> str:

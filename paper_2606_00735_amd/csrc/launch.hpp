@@ -61,6 +61,10 @@ hipError_t launch_ffn_mx(const uint8_t* xq, const uint32_t* xs, const uint8_t* w
                          const int32_t* offsets, int E_local, int H, int I, int ld_gu, int ld_dn, int M_cap,
                          void* y_perm, void* ws, hipStream_t s, int rows = 0);
 
+// The result of the check that block b of a launch runs on XCD b % 8, for a
+// launch on stream s, or nullptr (ffn_kernels.hip).
+const int32_t* xcd_state(hipStream_t s);
+
 // compute units of the current device (256 if it cannot be asked)
 int device_cu_count();
 
