@@ -396,6 +396,118 @@ moe_status moe_grouped_swiglu_ffn_mx(const uint8_t* xq, const uint32_t* xs, cons
                                      size_t* ws_bytes, hipStream_t stream);
 
 /*
+ * MXFP4 expert FFN (4-bit experts).
+ *
+ * OCP Microscaling FP4 (MXFP4): elements are E2M1 (+-0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6), 32 consecutive elements along the reduction dimension share one E8M0 scale
+ * code c, the power of two 2^(c - 127). A weight takes 17/32 of a byte, a quarter
+ * of bf16's traffic at decode, and the MFMA runs at four times the bf16 rate.
+ *
+ * Quantisation of a 32-element block v: shared exponent s = floor(log2(max
+ * |v_i|)) - 2 clamped to at least -127 (an all-zero block takes -127), code
+ * c = s + 127, element q_i = E2M1 of v_i / 2^s clamped to +-6 and rounded to
+ * nearest, ties to even (a value that rounds to zero keeps its sign). A block
+ * with a NaN or an infinity takes code 255 (NaN) and zero elements: whatever is
+ * computed from it is NaN.
+ *
+ * Layout of an MXFP4 matrix with R rows and reduction length K (K % 32 == 0):
+ * rows are padded with zero elements to C = ceil(K / 256) chunks of 256.
+ *   codes  [R, 128 C]   uint8, row-major (16-byte aligned): byte j of a row holds
+ *                       elements 2 j (low half) and 2 j + 1 (high half)
+ *   scales [C, R, 2]    uint32, chunk-major: byte s of dword (k, r, h) is the code
+ *                       of block 2 s + h of row r's chunk k, elements
+ *                       [256 k + 64 s + 32 h, +32)
+ * A batch of B such matrices is codes [B, R, 128 C] and scales [B, C, R, 2].
+ * Weight codes may have padded rows, ld bytes apart (0: 128 C; otherwise at least
+ * that, a multiple of 16 and <= 2^20); activation codes are dense. Operands of
+ * the products need zero codes and scale codes below 255 in the chunk padding of
+ * the weights (as moe_mx4_quantize writes them); in that of activations any
+ * codes, with scale codes below 255.
+ */
+
+/*
+ * moe_mx4_quantize - MXFP4 quantisation of `batch` matrices of `rows` x K.
+ *
+ * x         [batch, rows, K] dt (bf16 or fp32)
+ * row_count DEVICE int32 or NULL (batch 1 only): quantise rows
+ *           [0, min(rows, *row_count)) only; the others are left untouched
+ * codes     [batch, rows, 128 C] uint8, rows ld_codes bytes apart (0: dense)
+ * scales    [batch, C, rows, 2] uint32
+ * Limits: K % 32 == 0, K <= 2^20; batch * rows * K <= 2^40.
+ */
+moe_status moe_mx4_quantize(const void* x, moe_dtype dt, int batch, int rows, int K,
+                            int ld_codes, const int32_t* row_count, uint8_t* codes,
+                            uint32_t* scales, hipStream_t stream);
+
+/*
+ * moe_mx4_dequantize - the values x [batch, rows, K] bf16 that MXFP4 codes stand
+ * for (exact: every value of a code below 253 is a bf16; NaN for scale code 255).
+ * Arguments and limits as moe_mx4_quantize.
+ */
+moe_status moe_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, int batch, int rows,
+                              int K, int ld_codes, void* x, hipStream_t stream);
+
+/*
+ * moe_grouped_swiglu_mx4 - the gate/up half of the MXFP4 expert FFN.
+ *
+ * For local slot l and rows R = [offsets[l], offsets[l+1]) (clamped to [0, M_cap]):
+ *   G = X[R] Wg[l]^T, U = X[R] Wu[l]^T  from the MXFP4 operands (scaled MFMA,
+ *                                        fp32 accumulation)
+ *   h = silu(G) * U                      (fp32)
+ *   (hq, hs)[R] = MXFP4 quantisation of h along I (rules above)
+ * perm_src NULL: X has M_cap rows and T and k are not read. Otherwise (DEVICE
+ * int32 [M_cap], from moe_permute) X has T rows and row r of the expert input is
+ * row perm_src[r] / k of it, clamped to [0, T): tokens are quantised once each
+ * and no permuted copy is made. Entries of rows outside the local experts' are
+ * not read.
+ * xq [M_cap or T, 128 C(H)], xs; wgq, wuq [E_local, I, 128 C(H)] (rows ldw bytes
+ * apart, 0: dense), wgs, wus; hq [M_cap, 128 C(I)], hs: rows R written, the rest
+ * untouched (and, for I % 256 != 0, the codes in the padding).
+ * Limits: 0 <= E_local <= 256; H % 128 == 0, I % 128 == 0; H, I <= 2^20; with
+ * perm_src T >= 1, 1 <= k <= 16 and T * 128 C(H) < 2^32.
+ */
+moe_status moe_grouped_swiglu_mx4(const uint8_t* xq, const uint32_t* xs, const int32_t* perm_src,
+                                  int T, int k, const uint8_t* wgq, const uint32_t* wgs,
+                                  const uint8_t* wuq, const uint32_t* wus, const int32_t* offsets,
+                                  int E_local, int H, int I, int ldw, int M_cap, uint8_t* hq,
+                                  uint32_t* hs, hipStream_t stream);
+
+/*
+ * moe_grouped_gemm_mx4 - grouped MXFP4 GEMM with bf16 output: for local slot l,
+ * c[R] = bf16( A[R] B[l]^T ) (fp32 accumulation), R as above.
+ * aq [M_cap, 128 C(K)], as; bq [E_local, N, 128 C(K)] (rows ldb bytes apart, 0:
+ * dense), bs; c [M_cap, N] bf16, rows R written.
+ * Limits: 0 <= E_local <= 256; N % 128 == 0, K % 128 == 0; N, K <= 2^20.
+ */
+moe_status moe_grouped_gemm_mx4(const uint8_t* aq, const uint32_t* as, const uint8_t* bq,
+                                const uint32_t* bs, const int32_t* offsets, int E_local, int N,
+                                int K, int ldb, int M_cap, void* c, hipStream_t stream);
+
+/*
+ * moe_grouped_swiglu_ffn_mx4 - the MXFP4 expert FFN: moe_grouped_swiglu_mx4 into
+ * the workspace, then moe_grouped_gemm_mx4 with W_down (wdq [E_local, H,
+ * 128 C(I)], wds) into y_perm [M_cap, H] bf16. Code rows are ldw_gu (W_gate,
+ * W_up) and ldw_dn (W_down) bytes apart (0: dense). E: the experts of the whole
+ * layer or 0 (as moe_grouped_swiglu_ffn_gather_of: with perm_src the library then
+ * expects T * k / E rows an expert; the results do not depend on it).
+ * ws starts with 16 KiB of counters that must be zero before the first call on
+ * the workspace (every call leaves them zero), then h codes [M_cap, 128 C(I)]
+ * and, 256-byte aligned after them, their scales, then the split plan and the
+ * fp32 partial sums of tiles split along K (summed in a fixed order, so results
+ * are deterministic). Calls that share a workspace must not overlap. The
+ * schedules and launches are those of moe_grouped_swiglu_ffn; without a
+ * reduction launch where no expert can have more than 128 rows (M_cap <= 128;
+ * with perm_src min(T, M_cap) <= 128).
+ */
+moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs,
+                                      const int32_t* perm_src, int T, int k, const uint8_t* wgq,
+                                      const uint32_t* wgs, const uint8_t* wuq, const uint32_t* wus,
+                                      const uint8_t* wdq, const uint32_t* wds,
+                                      const int32_t* offsets, int E, int E_local, int H, int I,
+                                      int ldw_gu, int ldw_dn, int M_cap, void* y_perm, void* ws,
+                                      size_t* ws_bytes, hipStream_t stream);
+
+/*
  * moe_load_sweep - per-expert latency versus token load.
  *
  * Algorithm 1 Phase 1 / Section 4.2.1: profile the expert computation over a

@@ -15,8 +15,10 @@ from ._lib import (  # noqa: F401
     FFN_COUNTER_BYTES,
     LIB_PATH,
     MoeError,
+    Mx4Tensor,
     MxTensor,
     ffn_hidden,
+    ffn_mx4_ws_bytes,
     ffn_mx_ws_bytes,
     ffn_ws_bytes,
     gate_ws_bytes,
@@ -27,14 +29,19 @@ from ._lib import (  # noqa: F401
     moe_fit_latency_model,
     moe_gate_topk,
     moe_grouped_gemm_mx,
+    moe_grouped_gemm_mx4,
     moe_grouped_swiglu_ffn,
     moe_grouped_swiglu_ffn_gather,
     moe_grouped_swiglu_ffn_mx,
+    moe_grouped_swiglu_ffn_mx4,
     moe_grouped_swiglu_ffn_noalloc,
     moe_grouped_swiglu_mx,
+    moe_grouped_swiglu_mx4,
     moe_layer,
     moe_load_sweep,
     moe_load_sweep_mx,
+    moe_mx4_dequantize,
+    moe_mx4_quantize,
     moe_mx_quantize,
     moe_permute,
     moe_place_greedy,
@@ -42,6 +49,7 @@ from ._lib import (  # noqa: F401
     moe_placement_cost,
     moe_unpermute_combine,
     moe_window_push,
+    mx4_chunks,
     pad_weight_rows,
     weight_row_stride,
 )

@@ -27,7 +27,8 @@ EXPORTED = ("moe_status_string", "moe_abi_version", "moe_gate_topk", "moe_expert
             "moe_window_push", "moe_drift_distance", "moe_mx_quantize", "moe_grouped_swiglu_mx",
             "moe_grouped_gemm_mx", "moe_grouped_swiglu_ffn_mx", "moe_load_sweep_mx",
             "moe_grouped_swiglu_ffn_gather", "moe_grouped_swiglu_ffn_gather_of",
-            "moe_grouped_swiglu_ffn_noalloc", "moe_ffn_scratch_bytes")
+            "moe_grouped_swiglu_ffn_noalloc", "moe_ffn_scratch_bytes", "moe_mx4_quantize", "moe_mx4_dequantize",
+            "moe_grouped_swiglu_mx4", "moe_grouped_gemm_mx4", "moe_grouped_swiglu_ffn_mx4")
 
 
 class MoeError(RuntimeError):
@@ -103,6 +104,17 @@ def load_library(path: str = LIB_PATH):
     L.moe_grouped_swiglu_ffn_noalloc.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _P]
     L.moe_ffn_scratch_bytes.restype = _SZ
     L.moe_ffn_scratch_bytes.argtypes = []
+    L.moe_mx4_quantize.restype = _I
+    L.moe_mx4_quantize.argtypes = [_P, _I, _I, _I, _I, _I, _P, _P, _P, _P]
+    L.moe_mx4_dequantize.restype = _I
+    L.moe_mx4_dequantize.argtypes = [_P, _P, _I, _I, _I, _I, _P, _P]
+    L.moe_grouped_swiglu_mx4.restype = _I
+    L.moe_grouped_swiglu_mx4.argtypes = [_P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P]
+    L.moe_grouped_gemm_mx4.restype = _I
+    L.moe_grouped_gemm_mx4.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P]
+    L.moe_grouped_swiglu_ffn_mx4.restype = _I
+    L.moe_grouped_swiglu_ffn_mx4.argtypes = [_P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I,
+                                             _I, _P, _P, _PSZ, _P]
     if L.moe_abi_version() != 3:
         raise RuntimeError("libmoe ABI version mismatch")
     _lib = L
@@ -720,6 +732,193 @@ def moe_grouped_swiglu_ffn_mx(x, w_gate, w_up, w_down, offsets, ws=None, y_perm=
                                      _dev(y_perm, "y_perm", torch.bfloat16), _dev(ws, "ws", torch.uint8),
                                      ctypes.byref(n), _stream())
     _check("moe_grouped_swiglu_ffn_mx", st)
+    return y_perm, ws
+
+
+# ---------------------------------------------------------------------------
+# MXFP4 (4-bit experts)
+# ---------------------------------------------------------------------------
+def mx4_chunks(K):
+    """Chunks of 256 elements (128 bytes of codes) that a row of K elements takes."""
+    return (K + 255) // 256
+
+
+class Mx4Tensor:
+    """An MXFP4 operand of shape [.., R, K]: E2M1 codes [.., R, 128 C] uint8 (two a
+    byte, the even element in the low half; C = ceil(K / 256), the rows padded with
+    zero codes) and scale dwords [.., C, R, 2] int32 (byte s of dword (k, r, h): the
+    E8M0 code of elements [256 k + 64 s + 32 h, +32) of row r). The codes may be a
+    view with padded rows (row stride ld bytes, matrices R * ld apart), which weight
+    operands accept."""
+
+    def __init__(self, codes, scales, K):
+        if codes.dtype != torch.uint8 or scales.dtype != torch.int32:
+            raise ValueError("MXFP4 codes are uint8 and scales int32")
+        C = mx4_chunks(K)
+        if K < 1 or K % 32 or codes.dim() not in (2, 3) or codes.shape[-1] != 128 * C:
+            raise ValueError("codes must be [R, 128 C] or [B, R, 128 C], C = ceil(K / 256), K a multiple of 32")
+        R = codes.shape[-2]
+        if tuple(scales.shape) != tuple(codes.shape[:-2]) + (C, R, 2):
+            raise ValueError("scales must be [.., C, R, 2] for codes [.., R, 128 C]")
+        if scales.device != codes.device:
+            raise ValueError("codes and scales must be on one device")
+        ld = codes.stride(-2) if R > 1 and codes.numel() > 0 else 128 * C
+        if codes.numel() > 0 and (codes.stride(-1) != 1 or ld < 128 * C or
+                                  (codes.dim() == 3 and codes.shape[0] > 1 and codes.stride(0) != R * ld)):
+            raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
+        self.codes, self.scales, self.K, self.ld = codes, scales, K, ld
+
+    @property
+    def shape(self):
+        return tuple(self.codes.shape[:-1]) + (self.K,)
+
+
+def moe_mx4_quantize(x, out=None, row_count=None, ld=None):
+    """MXFP4 quantisation of x [R, K] or [B, R, K] (bf16 or fp32) along K, a multiple
+    of 32. row_count: optional device int32 tensor of one element (R-row x only):
+    rows from it on are left as they are in `out`. ld: row stride in bytes of newly
+    allocated codes."""
+    L = load_library()
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [R, K] or [B, R, K]")
+    B, (R, K) = (1 if x.dim() == 2 else x.shape[0]), x.shape[-2:]
+    if out is None:
+        row = 128 * mx4_chunks(K)
+        codes = torch.empty(tuple(x.shape[:-1]) + (row if ld is None else ld,), dtype=torch.uint8,
+                            device=x.device)[..., :row]
+        out = Mx4Tensor(codes, torch.empty(tuple(x.shape[:-2]) + (mx4_chunks(K), R, 2), dtype=torch.int32,
+                                           device=x.device), K)
+    elif out.shape != tuple(x.shape):
+        raise ValueError(f"out must have shape {tuple(x.shape)}, got {out.shape}")
+    rc = None
+    if row_count is not None:
+        if row_count.numel() != 1 or row_count.dtype != torch.int32 or not row_count.is_cuda or x.dim() != 2:
+            raise ValueError("row_count must be one device int32 (for x [R, K])")
+        rc = row_count.data_ptr()
+    st = L.moe_mx4_quantize(_dev(x, "x"), _dtype_code(x), B, R, K, out.ld, rc, _mx_codes(out.codes, "codes"),
+                            _dev(out.scales, "scales", torch.int32), _stream())
+    _check("moe_mx4_quantize", st)
+    return out
+
+
+def moe_mx4_dequantize(t, out=None):
+    """The values (bf16) that an Mx4Tensor stands for."""
+    L = load_library()
+    if not isinstance(t, Mx4Tensor):
+        raise TypeError("t must be an Mx4Tensor")
+    if out is None:
+        out = torch.empty(t.shape, dtype=torch.bfloat16, device=t.codes.device)
+    elif tuple(out.shape) != t.shape:
+        raise ValueError(f"out must have shape {t.shape}")
+    B, (R, K) = (1 if len(t.shape) == 2 else t.shape[0]), t.shape[-2:]
+    st = L.moe_mx4_dequantize(_mx_codes(t.codes, "codes"), _dev(t.scales, "scales", torch.int32), B, R, K, t.ld,
+                              _dev(out, "out", torch.bfloat16), _stream())
+    _check("moe_mx4_dequantize", st)
+    return out
+
+
+def _mx4_dev(t, name, shape, padded=False):
+    """Pointers of an MXFP4 operand; only weight operands (padded=True) may have
+    padded code rows."""
+    if not isinstance(t, Mx4Tensor):
+        raise TypeError(f"{name} must be an Mx4Tensor")
+    if t.shape != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {t.shape}")
+    if not padded and t.ld != t.codes.shape[-1]:
+        raise ValueError(f"{name} must have dense code rows")
+    return _mx_codes(t.codes, name + ".codes"), _dev(t.scales, name + ".scales", torch.int32)
+
+
+def _mx4_rows(x, perm_src, k):
+    """(M_cap, T, perm_src pointer) of an expert input that is x itself or gathered from it."""
+    if not isinstance(x, Mx4Tensor) or len(x.shape) != 2:
+        raise TypeError("x must be a two-dimensional Mx4Tensor")
+    if perm_src is None:
+        return x.shape[0], x.shape[0], None
+    return perm_src.numel(), x.shape[0], _dev(perm_src, "perm_src", torch.int32)
+
+
+def moe_grouped_swiglu_mx4(x, w_gate, w_up, offsets, h=None, perm_src=None, k=1):
+    """Gate/up half of the MXFP4 FFN: h = MXFP4(silu(x Wg^T) * (x Wu^T)) per local
+    expert. With perm_src (moe_permute) row r of the input is x[perm_src[r] // k]."""
+    L = load_library()
+    M_cap, T, src = _mx4_rows(x, perm_src, k)
+    H = x.shape[1]
+    E_local, I, _ = w_gate.shape
+    if offsets.numel() != E_local + 1:
+        raise ValueError("offsets must have E_local + 1 entries")
+    dev = x.codes.device
+    if h is None:
+        C = mx4_chunks(I)
+        h = Mx4Tensor(torch.empty((M_cap, 128 * C), dtype=torch.uint8, device=dev),
+                      torch.empty((C, M_cap, 2), dtype=torch.int32, device=dev), I)
+    if w_up.ld != w_gate.ld:
+        raise ValueError("w_gate and w_up must have the same row stride")
+    st = L.moe_grouped_swiglu_mx4(*_mx4_dev(x, "x", (T, H)), src, T, k,
+                                  *_mx4_dev(w_gate, "w_gate", (E_local, I, H), True),
+                                  *_mx4_dev(w_up, "w_up", (E_local, I, H), True),
+                                  _dev(offsets, "offsets", torch.int32), E_local, H, I, w_gate.ld, M_cap,
+                                  *_mx4_dev(h, "h", (M_cap, I)), _stream())
+    _check("moe_grouped_swiglu_mx4", st)
+    return h
+
+
+def moe_grouped_gemm_mx4(a, b, offsets, c=None):
+    """Grouped MXFP4 GEMM: c[R] = bf16(a[R] b[l]^T) per local expert l."""
+    L = load_library()
+    M_cap, K = a.shape
+    E_local, N, _ = b.shape
+    if offsets.numel() != E_local + 1:
+        raise ValueError("offsets must have E_local + 1 entries")
+    if c is None:
+        c = torch.empty((M_cap, N), dtype=torch.bfloat16, device=a.codes.device)
+    elif tuple(c.shape) != (M_cap, N):
+        raise ValueError(f"c must be [{M_cap}, {N}]")
+    st = L.moe_grouped_gemm_mx4(*_mx4_dev(a, "a", (M_cap, K)), *_mx4_dev(b, "b", (E_local, N, K), True),
+                                _dev(offsets, "offsets", torch.int32), E_local, N, K, b.ld, M_cap,
+                                _dev(c, "c", torch.bfloat16), _stream())
+    _check("moe_grouped_gemm_mx4", st)
+    return c
+
+
+def ffn_mx4_ws_bytes(E_local, H, I, M_cap):
+    L = load_library()
+    n = ctypes.c_size_t(0)
+    st = L.moe_grouped_swiglu_ffn_mx4(None, None, None, 0, 0, None, None, None, None, None, None, None, 0, E_local, H,
+                                      I, 0, 0, M_cap, None, None, ctypes.byref(n), None)
+    _check("moe_grouped_swiglu_ffn_mx4", st)
+    return n.value
+
+
+def moe_grouped_swiglu_ffn_mx4(x, w_gate, w_up, w_down, offsets, ws=None, y_perm=None, perm_src=None, k=1, experts=0):
+    """MXFP4 expert FFN. x: Mx4Tensor [M_cap, H], or with perm_src [M_cap] (moe_permute)
+    [T, H], of which row r of the input is x[perm_src[r] // k]. ``experts``: the experts
+    of the whole layer, if known (the results are the same). Returns (y_perm [M_cap, H]
+    bf16, ws)."""
+    L = load_library()
+    M_cap, T, src = _mx4_rows(x, perm_src, k)
+    H = x.shape[1]
+    E_local, I, _ = w_gate.shape
+    if offsets.numel() != E_local + 1:
+        raise ValueError("offsets must have E_local + 1 entries")
+    dev = x.codes.device
+    if ws is None:
+        ws = torch.zeros(ffn_mx4_ws_bytes(E_local, H, I, M_cap), dtype=torch.uint8, device=dev)  # counters start at zero
+    if y_perm is None:
+        y_perm = torch.empty((M_cap, H), dtype=torch.bfloat16, device=dev)
+    elif tuple(y_perm.shape) != (M_cap, H):
+        raise ValueError(f"y_perm must be [{M_cap}, {H}]")
+    n = ctypes.c_size_t(ws.numel())
+    if w_up.ld != w_gate.ld:
+        raise ValueError("w_gate and w_up must have the same row stride")
+    st = L.moe_grouped_swiglu_ffn_mx4(*_mx4_dev(x, "x", (T, H)), src, T, k,
+                                      *_mx4_dev(w_gate, "w_gate", (E_local, I, H), True),
+                                      *_mx4_dev(w_up, "w_up", (E_local, I, H), True),
+                                      *_mx4_dev(w_down, "w_down", (E_local, H, I), True),
+                                      _dev(offsets, "offsets", torch.int32), experts, E_local, H, I, w_gate.ld,
+                                      w_down.ld, M_cap, _dev(y_perm, "y_perm", torch.bfloat16),
+                                      _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
+    _check("moe_grouped_swiglu_ffn_mx4", st)
     return y_perm, ws
 
 

@@ -234,8 +234,8 @@ __device__ __forceinline__ void pipeline(int nK, bf16_t* smem, int stage_elems, 
 // The same pipeline for consumers that read their operands from LDS one
 // k-step ahead of the MFMAs that use them, across chunk boundaries too. A
 // chunk holds KS k-steps (KS even); read(stage, s, buf) loads the fragments of
-// k-step s into register buffer buf, mma(buf) issues one k-step's MFMAs from
-// buffer buf (k-step s always uses buffer s % 2), and mix() orders the LDS
+// k-step s into register buffer buf, mma(s) issues k-step s's MFMAs from buffer
+// s % 2 (k-step s always uses that buffer), and mix() orders the LDS
 // reads and MFMAs of one k-step (sched_group_barrier hints).
 //
 // The wait for chunk c+1 and the barrier come before the last k-step of
@@ -282,11 +282,11 @@ __device__ __forceinline__ void pipeline_xk(int nK, bf16_t* smem, int stage_elem
     for (int s = 0; s + 1 < KS; ++s) {
       issue(c + NS - 1, live, prev, s + 1);
       if (MMA_FIRST) {
-        mma(s & 1);
+        mma(s);
         read(st, s + 1, (s + 1) & 1);
       } else {
         read(st, s + 1, (s + 1) & 1);
-        mma(s & 1);
+        mma(s);
       }
       mix();
       __builtin_amdgcn_sched_barrier(0);
@@ -300,11 +300,11 @@ __device__ __forceinline__ void pipeline_xk(int nK, bf16_t* smem, int stage_elem
     // first fragments of chunk c+1 (after the last chunk: an unused read of a
     // stage that holds a placeholder load; LDS reads cannot fault)
     if (MMA_FIRST) {
-      mma((KS - 1) & 1);
+      mma(KS - 1);
       read(smem + nxt * stage_elems, 0, 0);
     } else {
       read(smem + nxt * stage_elems, 0, 0);
-      mma((KS - 1) & 1);
+      mma(KS - 1);
     }
     mix();
     __builtin_amdgcn_sched_barrier(0);

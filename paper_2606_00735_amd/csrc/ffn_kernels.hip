@@ -26,14 +26,14 @@ namespace moe {
 
 template <bool DUAL, int W>
 __global__ __launch_bounds__(W* kWave) void grouped_gemm_bf16_kernel(GemmArgs a) {
-  grouped_gemm_body<W, DUAL, false>(a);
+  grouped_gemm_body<W, DUAL, kBf16>(a);
 }
 
 // MXFP8 grouped GEMM: the same tile schedule; the dual GEMM writes MXFP8 h,
 // the single one bf16.
 template <bool DUAL, int W>
 __global__ __launch_bounds__(W* kWave) void grouped_gemm_mx_kernel(GemmArgs a) {
-  grouped_gemm_body<W, DUAL, true>(a);
+  grouped_gemm_body<W, DUAL, kMx8>(a);
 }
 
 // The MXFP8 gate/up reduction: sums the S partials of gate and up for 4

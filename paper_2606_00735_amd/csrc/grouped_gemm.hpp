@@ -13,6 +13,10 @@ namespace moe {
 
 constexpr int kBK = 64;  // K chunk per pipeline stage (128-byte tile rows)
 
+// Operand format of a grouped GEMM: a K chunk is 128 bytes of a row in each, 64
+// bf16, 128 E4M3 or 256 E2M1 elements.
+enum Fmt : int { kBf16, kMx8, kMx4 };
+
 // Tile classes (see row_tiles):
 //   small   64 x 128 tiles   (weight streaming at small M_e)
 //   mid    128 x 128 tiles
@@ -60,6 +64,9 @@ struct GemmArgs {
   // a row, moved as pairs of bf16 slots), As [K/128][M_cap] and
   // Bs0/Bs1 [E_local][K/128][N] their scale dwords (mx.hpp); the dual GEMM
   // writes E4M3 codes of h to C and their scale dwords to Cs [N/128][M_cap].
+  // MXFP4 GEMMs (grouped_gemm_mx4_kernel): the same with E2M1 codes, K the bytes
+  // of a padded row, two scale dwords a row and chunk ([K/128][rows][2]), and h
+  // codes in rows of mx4_row_bytes(N).
   const uint32_t* As;
   const uint32_t* Bs0;
   const uint32_t* Bs1;
@@ -67,9 +74,9 @@ struct GemmArgs {
   // Per-XCD work counters (8 ints, zero before the launch) or nullptr for
   // the static tile order.
   int32_t* queue;
-  // Row gather (bf16 GEMMs): when a_src != nullptr, row m of the A operand
+  // Row gather (bf16 and MXFP4 GEMMs): when a_src != nullptr, row m of the A operand
   // is row clamp(a_src[m] / a_div, 0, a_T - 1) of A (A holds a_T rows and
-  // a_T * K * 2 < 2^32), so the gate/up GEMM reads the routed tokens of x
+  // its bytes < 2^32), so the gate/up GEMM reads the routed tokens of x
   // directly instead of a permuted copy.
   const int32_t* a_src;
   int a_div, a_T;
@@ -381,7 +388,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, bf16_t* smem, int e
       for (int j = 0; j < NI; ++j)
         bfr[buf][b][j] = lds_frag<kBK>(st + (AR + b * BN) * kBK, wn * WN + j * 32 + (lane & 31), chunk);
   };
-  auto mma = [&](int buf) {
+  auto mma = [&](int s) {
+    const int buf = s & 1;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -427,15 +435,17 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, bf16_t* smem, int e
 
 // MXFP8 stages: the same 128-byte tile rows as the bf16 path (a K chunk is
 // 128 E4M3 codes), plus one scale dword per operand row. A
-// global_load_lds_dword of a wave brings 64 scale rows, so a stage has room for
-// SLOADS * W * 64 of them, a multiple of what all waves load at once.
-template <int BM, int BN, bool DUAL, int W>
+// global_load_lds_dword of a wave brings 64 scale dwords, so a stage has room for
+// SLOADS * W * 64 of them, a multiple of what all waves load at once. MXFP4: two
+// scale dwords a row.
+template <int BM, int BN, bool DUAL, int W, int F = kMx8>
 struct MxStages {
   static constexpr int NB = DUAL ? 2 : 1;
   static constexpr int DROWS = W * 1024 / (2 * kBK);
   static constexpr int AROWS = BM > DROWS ? BM : DROWS;
   static constexpr int ROWS = AROWS + NB * BN;
-  static constexpr int SLOADS = (ROWS + W * 64 - 1) / (W * 64);  // scale loads per wave per chunk
+  static constexpr int DW = F == kMx4 ? 2 : 1;                          // scale dwords per row
+  static constexpr int SLOADS = (DW * ROWS + W * 64 - 1) / (W * 64);  // scale loads per wave per chunk
   static constexpr int SCALE_OFF = ROWS * 2 * kBK;                   // bytes
   static constexpr int STAGE = SCALE_OFF + SLOADS * W * 64 * 4;  // bytes
   static constexpr int FIT = (152 * 1024) / STAGE;
@@ -448,12 +458,85 @@ __device__ __forceinline__ uint4 lds16(const bf16_t* lds, int row, int chunk) {
   return *reinterpret_cast<const uint4*>(lds + row * kBK + swz_chunk<kBK>(row, chunk) * 8);
 }
 
+// One k-step (64 elements) of the MXFP4 MFMA: q is the k-step within the chunk
+// and the byte of the scale dwords.
+__device__ __forceinline__ f32x16_t mfma_mx4(int q, uint4 b, uint4 a, f32x16_t acc, uint32_t sb, uint32_t sa) {
+  // the upper half of an operand register of eight is not read for 4-bit formats
+  auto f4 = [](uint4 v) { return int32x8_t{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0}; };
+  constexpr int kE2M1 = 4;  // format code of the instruction
+  switch (q) {
+    case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f4(b), f4(a), acc, kE2M1, kE2M1, 0, (int)sb, 0, (int)sa);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f4(b), f4(a), acc, kE2M1, kE2M1, 1, (int)sb, 1, (int)sa);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f4(b), f4(a), acc, kE2M1, kE2M1, 2, (int)sb, 2, (int)sa);
+    default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f4(b), f4(a), acc, kE2M1, kE2M1, 3, (int)sb, 3, (int)sa);
+  }
+}
+
+// The scale code of block `col / 32` of h row `row`. The last chunk of a row of
+// an odd number of 128 columns is half empty: its other four blocks get code 0
+// (any finite code: the other operand of the product that reads them holds
+// zeros there).
+__device__ __forceinline__ void mx4_store_scale(const GemmArgs& a, int row, int col, uint32_t code) {
+  const int b = (col / kMxBlock) & 7;
+  uint8_t* p = reinterpret_cast<uint8_t*>(a.Cs) + ((size_t)(col / kMx4Chunk) * a.M_cap + row) * 8;
+  p[mx4_scale_byte(b)] = static_cast<uint8_t>(code);
+  if (a.N % kMx4Chunk != 0 && col / kMx4Chunk == a.N / kMx4Chunk) p[mx4_scale_byte(b + 4)] = 0;
+}
+
+// A wave's block of h = val(i, j, v) as MXFP4. The 32 values of a row and block
+// sit in lanes l and l ^ 32, four columns of each eight in either; the two swap
+// halves so that a lane stores whole blocks, 16 bytes of one row.
+template <int MI, int NI, class Val>
+__device__ __forceinline__ void mx4_store_h(const GemmArgs& a, int row0, int m_end, int col0, int lane, Val&& val) {
+  const int hi = lane >> 5;
+  const size_t ldc = mx4_row_bytes(a.N);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int row = row0 + i * 32 + (lane & 31);
+    if (row0 + i * 32 >= m_end) break;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int col = col0 + j * 32;
+      float r[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        r[v] = val(i, j, v);
+        top = max(top, abs_bits(r[v]));
+      }
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
+      const uint32_t code = mx4_scale_code(top);
+      const float sc = mx4_scale(code);
+      uint32_t w[2];  // groups g = 0, 1 and 2, 3: columns 8 g + 4 hi + (0..3)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        w[q] = e2m1x4(r[8 * q], r[8 * q + 1], r[8 * q + 2], r[8 * q + 3], sc) |
+               e2m1x4(r[8 * q + 4], r[8 * q + 5], r[8 * q + 6], r[8 * q + 7], sc) << 16;
+        if (code == kMxNan) w[q] = 0;
+      }
+      // lane half 0 keeps columns 0-15 and gets the partner's, half 1 columns 16-31
+      const uint32_t keep = hi ? w[1] : w[0];
+      const uint32_t other = (uint32_t)__shfl_xor((int)(hi ? w[0] : w[1]), 32, kWave);
+      const uint32_t lo = hi ? other : keep, up = hi ? keep : other;  // of lane halves 0 and 1
+      const uint2 out = make_uint2((lo & 0xFFFFu) | up << 16, lo >> 16 | (up & 0xFFFF0000u));
+      if (row < m_end) {
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(a.C) + (size_t)row * ldc + col / 2 + hi * 8) = out;
+        if (hi == 0) mx4_store_scale(a, row, col, code);
+      }
+    }
+  }
+}
+
 // A wave's WM x WN block of h = val(i, j, v) as MXFP8: the 32 values of a row
 // and block sit in lanes l and l ^ 32; codes through store_block, one scale
 // code byte per row and block.
-template <int MI, int NI, int WM, int WN, class Val>
+template <int F, int MI, int NI, int WM, int WN, class Val>
 __device__ __forceinline__ void mx_store_h(const GemmArgs& a, bf16_t* smem, int row0, int m_end, int col0, int wave,
                                            int lane, Val&& val) {
+  if constexpr (F == kMx4) {
+    mx4_store_h<MI, NI>(a, row0, m_end, col0, lane, val);
+    return;
+  }
   uint32_t codes[MI][NI][4];
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
@@ -631,7 +714,8 @@ __device__ __forceinline__ void gemm_tile_mx(const GemmArgs& a, bf16_t* smem, in
         sb[b][j] = sc[AR + b * BN + row] >> sh;
       }
   };
-  auto mma = [&](int buf) {
+  auto mma = [&](int s) {
+    const int buf = s & 1;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -663,9 +747,174 @@ __device__ __forceinline__ void gemm_tile_mx(const GemmArgs& a, bf16_t* smem, in
   // Epilogue: output layout as in gemm_tile (lane l: row l % 32, columns
   // 8 g + 4 h + (0..3) of each 32-column block).
   if constexpr (DUAL) {
-    mx_store_h<MI, NI, WM, WN>(
+    mx_store_h<kMx8, MI, NI, WM, WN>(
         a, smem, m0 + wm * WM, m_end, n0 + wn * WN, wave, lane,
         [&](int i, int j, int v) { return silu_mul_fast(acc[0][i][j][v], acc[NB - 1][i][j][v]); });
+  } else {
+    store_block<WM, WN, 2>(smem, a.C, N, m0 + wm * WM, m_end, n0 + wn * WN, wave, lane, [&](int i, int j, int g) {
+      return make_uint2(pack_bf16x2(acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1]),
+                        pack_bf16x2(acc[0][i][j][4 * g + 2], acc[0][i][j][4 * g + 3]));
+    });
+  }
+}
+
+// One BM x BN MXFP4 tile (two when DUAL), as gemm_tile: a chunk is four k-steps
+// of 64 elements, and lane (r, h) supplies piece 2 s + h of its row for k-step s
+// as it does for bf16. The scale dwords of a chunk are read with the fragments
+// of its first k-step and serve all four: pipeline_xk with MMA_FIRST, so that
+// they are read after the last MFMAs of the chunk before are issued.
+template <int W, int BM, int BN, int WAVES_M, bool DUAL, bool SPLIT = false, bool COH = false>
+__device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, int e, int m0, int m_end, int n0,
+                                              int kc0 = 0, int kc1 = -1, float* pbase = nullptr,
+                                              size_t pstride = 0, int pld = 0, int pcol0 = 0, bool coh = true) {
+  using St = MxStages<BM, BN, DUAL, W, kMx4>;
+  constexpr int NB = DUAL ? 2 : 1;
+  constexpr int WAVES_N = W / WAVES_M;
+  constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N;
+  constexpr int MI = WM / 32, NI = WN / 32;
+  constexpr int AR = St::AROWS;
+  static_assert(MI >= 1 && NI >= 1, "wave tile");
+  e = uniform_int(e), m0 = uniform_int(m0), m_end = uniform_int(m_end), n0 = uniform_int(n0);
+  kc0 = uniform_int(kc0), kc1 = uniform_int(kc1);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+  const int h = lane >> 5, r32 = lane & 31;
+  const int K = a.K, N = a.N, nK = K / kMxChunk;  // K: bytes of an operand row
+  const int a_rows = m_end - m0;
+  const bool gather = a.a_src != nullptr;
+  const char* A = reinterpret_cast<const char*>(a.A) + (gather ? 0 : (size_t)m0 * K);
+  const int LDB = a.ldb;  // bytes
+  const char* B0 = reinterpret_cast<const char*>(a.B0) + ((size_t)e * N + n0) * LDB;
+  const char* B1 = DUAL ? reinterpret_cast<const char*>(a.B1) + ((size_t)e * N + n0) * LDB : nullptr;
+  auto a_row = [&](int r) {  // row of A (and of its scales) behind tile row r
+    const int rr = r < a_rows ? r : a_rows - 1;
+    return gather ? min(max(a.a_src[m0 + rr] / a.a_div, 0), a.a_T - 1) : rr;
+  };
+
+  constexpr int RPI = 8, LA = AR / (RPI * W), LB = BN / (RPI * W);
+  uint32_t offA[LA], offB[LB];
+#pragma unroll
+  for (int t = 0; t < LA; ++t) {
+    const int r = (t * W + wave) * RPI + lane / 8;
+    offA[t] = (uint32_t)a_row(r) * (uint32_t)K + (uint32_t)(swz_chunk<kBK>(r, lane % 8) * 16);
+  }
+#pragma unroll
+  for (int t = 0; t < LB; ++t) {
+    const int r = (t * W + wave) * RPI + lane / 8;
+    offB[t] = (uint32_t)(r * LDB + swz_chunk<kBK>(r, lane % 8) * 16);
+  }
+  // Scale dwords: load u of wave w takes those of stage rows [32 (u W + w), +32),
+  // all in one operand (AR and BN are multiples of 32), as in gemm_tile_mx.
+  const char* sb_base[St::SLOADS];
+  size_t s_stride[St::SLOADS];  // bytes per K chunk
+  uint32_t soff[St::SLOADS];
+  const size_t sa_rows = gather ? (size_t)a.a_T : (size_t)a.M_cap;
+#pragma unroll
+  for (int u = 0; u < St::SLOADS; ++u) {
+    const int q0 = (u * W + wave) * 32;
+    sb_base[u] = reinterpret_cast<const char*>(a.As + (gather ? 0 : (size_t)m0 * 2));
+    s_stride[u] = sa_rows * 8;
+    soff[u] = 0;  // past the stage's rows: a placeholder
+    if (q0 < AR) {
+      soff[u] = (uint32_t)a_row(q0 + (lane >> 1)) * 8u + (lane & 1) * 4u;
+    } else if (q0 < AR + NB * BN) {
+      const bool up = DUAL && q0 >= AR + BN;
+      const uint32_t* s = up ? a.Bs1 : a.Bs0;
+      sb_base[u] = reinterpret_cast<const char*>(s + ((size_t)e * nK * N + n0 + (q0 - AR - (up ? BN : 0))) * 2);
+      s_stride[u] = (size_t)N * 8;
+      soff[u] = (uint32_t)(lane * 4);
+    }
+  }
+
+  f32x16_t acc[NB][MI][NI];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[b][i][j] = f32x16_t{};
+
+  // A placeholder load (live == false) re-reads the last chunk, which is in
+  // the cache by then, so loads never leave the operands.
+  if (kc1 < 0) kc1 = nK;
+  constexpr int KS = 4;
+  auto issue = [&](int kc, bool live, bf16_t* st, int part) {
+    const int kcl = live ? kc0 + kc : kc1 - 1;
+    char* sl = reinterpret_cast<char*>(st);
+    const uint32_t l0 = lds_addr(st) + wave * (RPI * 128);
+    constexpr int LS = W * RPI * 128;  // LDS bytes between a wave's loads
+    auto mine = [&](int t) { return part < 0 || (St::NS > 2 ? t * KS / St::LOADS : 0) == part; };
+#pragma unroll
+    for (int t = 0; t < LA; ++t)
+      if (mine(t)) dma16a(uniform_ptr(A + (size_t)kcl * 128), offA[t], l0 + t * LS);
+#pragma unroll
+    for (int t = 0; t < LB; ++t)
+      if (mine(LA + t)) dma16a(uniform_ptr(B0 + (size_t)kcl * 128), offB[t], l0 + AR * 128 + t * LS);
+    if (DUAL) {
+#pragma unroll
+      for (int t = 0; t < LB; ++t)
+        if (mine(LA + LB + t))
+          dma16a(uniform_ptr(B1 + (size_t)kcl * 128), offB[t], l0 + (AR + BN) * 128 + t * LS);
+    }
+#pragma unroll
+    for (int u = 0; u < St::SLOADS; ++u)
+      if (mine(LA + NB * LB + u))
+        dma4s(uniform_ptr(sb_base[u] + (size_t)kcl * s_stride[u]), soff[u],
+              sl + St::SCALE_OFF + (u * W + wave) * 256);
+  };
+  uint4 af[2][MI], bfr[2][NB][NI];
+  uint32_t sa[MI], sb[NB][NI];
+  auto read = [&](const bf16_t* st, int s, int buf) {
+    const uint32_t* sc = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(st) + St::SCALE_OFF);
+    const int chunk = 2 * s + h;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int row = wm * WM + i * 32 + r32;
+      af[buf][i] = lds16(st, row, chunk);
+      if (s == 0) sa[i] = sc[row * 2 + h];
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int row = wn * WN + j * 32 + r32;
+        bfr[buf][b][j] = lds16(st + (AR + b * BN) * kBK, row, chunk);
+        if (s == 0) sb[b][j] = sc[(AR + b * BN + row) * 2 + h];
+      }
+  };
+  auto mma = [&](int s) {
+    const int buf = s & 1;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+          acc[b][i][j] = mfma_mx4(s, bfr[buf][b][j], af[buf][i], acc[b][i][j], sb[b][j], sa[i]);
+  };
+  auto mix = [&]() {
+    constexpr int NREAD = MI + NB * NI, NMFMA = NB * MI * NI;
+    constexpr int PAIRS = NREAD < NMFMA ? NREAD : NMFMA;
+#pragma unroll
+    for (int p = 0; p < PAIRS; ++p) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // DS read
+    }
+    if (NMFMA > PAIRS) __builtin_amdgcn_sched_group_barrier(0x008, NMFMA - PAIRS, 0);
+    if (NREAD > PAIRS) __builtin_amdgcn_sched_group_barrier(0x100, NREAD - PAIRS, 0);
+  };
+  pipeline_xk<St::NS, St::LOADS, KS, true>(kc1 - kc0, smem, St::STAGE / 2, issue, read, mma, mix);
+
+  if (SPLIT) {
+    split_epilogue<MI, NI, NB, WM, WN, COH>(acc, smem, m0, m_end, pcol0, pld, wm, wn, wave, lane, pbase, pstride,
+                                            coh);
+    return;
+  }
+  if constexpr (DUAL) {
+    mx4_store_h<MI, NI>(a, m0 + wm * WM, m_end, n0 + wn * WN, lane, [&](int i, int j, int v) {
+      return silu_mul_fast(acc[0][i][j][v], acc[NB - 1][i][j][v]);
+    });
   } else {
     store_block<WM, WN, 2>(smem, a.C, N, m0 + wm * WM, m_end, n0 + wn * WN, wave, lane, [&](int i, int j, int g) {
       return make_uint2(pack_bf16x2(acc[0][i][j][4 * g], acc[0][i][j][4 * g + 1]),
@@ -708,14 +957,18 @@ __device__ __forceinline__ void gemm_tile_mx(const GemmArgs& a, bf16_t* smem, in
 // ---------------------------------------------------------------------------
 constexpr int kSlotRows = 128;
 constexpr int kSlotElems = kSlotRows * kBK;  // bf16 elements: 16 KB
-template <bool MX>
+template <int F>
 struct BigStages {
   static constexpr int SCALE_OFF = 8 * kSlotElems;                     // elements: after the 8 slots
-  static constexpr int BYTES = 8 * kSlotElems * 2 + (MX ? 8 * kSlotRows * 4 : 0);
-  static constexpr int LOADS = MX ? 5 : 4;  // loads per wave per slot
+  static constexpr int SB = F == kMx4 ? 8 : 4;                         // scale bytes of a row and chunk
+  static constexpr int BYTES = 8 * kSlotElems * 2 + (F != kBf16 ? 8 * kSlotRows * SB : 0);
+  static constexpr int LOADS = F != kBf16 ? 5 : 4;  // loads per wave per slot
 };
 
-template <bool DUAL, bool MX>
+// MXFP4 takes the bf16 tile's steps (a chunk is four k-steps of 16-byte pieces in
+// both) with the scaled MFMA; the scale dword of a lane's row and half serves all
+// four k-steps of a chunk.
+template <bool DUAL, int F>
 __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e, int m0, int m_end, int n0,
                                          int kc0 = 0, int kc1 = -1, float* pbase = nullptr, size_t pstride = 0,
                                          int pld = 0, int pcol0 = 0) {
@@ -723,8 +976,9 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // them stay in SGPRs
   e = uniform_int(e), m0 = uniform_int(m0), m_end = uniform_int(m_end), n0 = uniform_int(n0);
   kc0 = uniform_int(kc0), kc1 = uniform_int(kc1);
-  using St = BigStages<MX>;
-  constexpr int EB = MX ? 1 : 2;           // bytes per element
+  using St = BigStages<F>;
+  constexpr bool MX = F != kBf16;
+  constexpr int EB = MX ? 1 : 2;           // bytes per unit of K and ldb
   constexpr int CB = 128;                  // bytes of a row per chunk
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
@@ -734,16 +988,18 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   if (kc1 < 0) kc1 = nKt;
   const int nK = kc1 - kc0;
   const int a_rows = m_end - m0;
-  const bool gather = !MX && a.a_src != nullptr;
+  const bool gather = F != kMx8 && a.a_src != nullptr;
   const size_t ldbB = (size_t)a.ldb * EB;  // bytes between weight rows
   const char* A = reinterpret_cast<const char*>(a.A) + (gather ? 0 : (size_t)m0 * K * EB);
   const char* B0 = reinterpret_cast<const char*>(a.B0) + ((size_t)e * N + n0) * ldbB;
   const char* B1 = DUAL ? reinterpret_cast<const char*>(a.B1) + ((size_t)e * N + n0) * ldbB : B0 + 64 * ldbB;
   const char *SA = nullptr, *SB0 = nullptr, *SB1 = nullptr;
+  const size_t sa_rows = gather ? (size_t)a.a_T : (size_t)a.M_cap;  // rows of the A scales
   if (MX) {
-    SA = reinterpret_cast<const char*>(a.As + m0);
-    SB0 = reinterpret_cast<const char*>(a.Bs0 + (size_t)e * nKt * N + n0);
-    SB1 = DUAL ? reinterpret_cast<const char*>(a.Bs1 + (size_t)e * nKt * N + n0) : SB0 + 64 * 4;
+    constexpr int DW = St::SB / 4;  // scale dwords of a row and chunk
+    SA = reinterpret_cast<const char*>(a.As + (gather ? 0 : (size_t)m0 * DW));
+    SB0 = reinterpret_cast<const char*>(a.Bs0 + ((size_t)e * nKt * N + n0) * DW);
+    SB1 = DUAL ? reinterpret_cast<const char*>(a.Bs1 + ((size_t)e * nKt * N + n0) * DW) : SB0 + 64 * St::SB;
   }
 
   // Slot row q of A half h is tile row 128 (q / 64) + 64 h + q % 64; of B
@@ -767,14 +1023,24 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // scale dwords: waves 0 and 2 load slot rows [0, 64), waves 1 and 3 rows
   // [64, 128) (the same values to the same place twice)
   uint32_t soffA[2], soffB = 0;
-  if (MX) {
+  if constexpr (F == kMx4) {
+    // two dwords a row: wave w loads slot rows [32 w, +32)
+    const int q = wave * 32 + (lane >> 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      int rr = min((q >> 6) * 128 + h * 64 + (q & 63), a_rows - 1);
+      if (gather) rr = min(max(a.a_src[m0 + rr] / a.a_div, 0), a.a_T - 1);
+      soffA[h] = (uint32_t)rr * 8u + (lane & 1) * 4u;
+    }
+    soffB = (uint32_t)(DUAL ? q : (q >> 6) * 128 + (q & 63)) * 8u + (lane & 1) * 4u;
+  } else if (MX) {
     soffA[0] = (uint32_t)min((wave & 1) * 128 + lane, a_rows - 1) * 4u;
     soffA[1] = (uint32_t)min((wave & 1) * 128 + 64 + lane, a_rows - 1) * 4u;
     soffB = (uint32_t)((wave & 1) * (DUAL ? 64 : 128) + lane) * 4u;
   }
 
   const uint32_t lds0 = lds_addr(smem) + wave * 8 * CB;
-  const uint32_t ldss = lds_addr(smem) + St::SCALE_OFF * 2 + (wave & 1) * 256;
+  const uint32_t ldss = lds_addr(smem) + St::SCALE_OFF * 2 + (F == kMx4 ? wave : wave & 1) * 256;
   // load t of slot w (0, 1: A halves; 2, 3: B halves) of chunk kc
   auto issue = [&](int w, int kc, int t) {
     // past the last chunk: a placeholder load of one line
@@ -785,8 +1051,8 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
            ((kc & 1) * 4 + w) * (kSlotElems * 2) + t * 32 * CB);
     if (MX && t == 3) {
       const char* sbase = w < 2 ? SA : (w == 2 ? SB0 : SB1);
-      dma4a(sbase + (size_t)kcl * (w < 2 ? a.M_cap : N) * 4, w < 2 ? soffA[w & 1] : soffB,
-            ldss + ((kc & 1) * 4 + w) * (kSlotRows * 4));
+      dma4a(sbase + (size_t)kcl * (w < 2 ? sa_rows : (size_t)N) * St::SB, w < 2 ? soffA[w & 1] : soffB,
+            ldss + ((kc & 1) * 4 + w) * (kSlotRows * St::SB));
     }
   };
   auto issue_slot = [&](int w, int kc) {
@@ -796,7 +1062,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // fragments: 16-byte piece 2 q + hi of the lane's row, q = 0..3 (bf16: the
   // k-step q; MXFP8: pieces 2 s and 2 s + 1 are k-step s)
   uint4 fr[4][2][4];     // [slot][32-row block][piece]
-  uint32_t sc[4][2];     // MXFP8: scale dword of the row, shifted to this lane's block
+  uint32_t sc[4][2];     // MXFP8: scale dword of the row, shifted to this lane's block; MXFP4: of the row and lane half
   uint32_t fofA[4], fofB[4];  // byte offset of the lane's piece in slot 0
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -809,10 +1075,12 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     fr[w][i][q] = *reinterpret_cast<const uint4*>(lds + (w < 2 ? fofA[q] : fofB[q]) +
                                                   ((kc & 1) * 4 + w) * (kSlotElems * 2) + i * 32 * CB);
   };
-  const uint32_t sofA = (uint32_t)(wm * 64 + r32) * 4, sofB = (uint32_t)(wn * 64 + r32) * 4;
+  const uint32_t sofA = (uint32_t)(wm * 64 + r32) * St::SB + (F == kMx4 ? hi * 4 : 0);
+  const uint32_t sofB = (uint32_t)(wn * 64 + r32) * St::SB + (F == kMx4 ? hi * 4 : 0);
   auto reads = [&](int w, int kc, int i) {
-    sc[w][i] = *reinterpret_cast<const uint32_t*>(lds + (w < 2 ? sofA : sofB) + St::SCALE_OFF * 2 +
-                                                  ((kc & 1) * 4 + w) * (kSlotRows * 4) + i * 128) >> (8 * hi);
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(
+        lds + (w < 2 ? sofA : sofB) + St::SCALE_OFF * 2 + ((kc & 1) * 4 + w) * (kSlotRows * St::SB) + i * 32 * St::SB);
+    sc[w][i] = F == kMx4 ? v : v >> (8 * hi);
   };
 
   f32x16_t acc[2][2][2][2];  // [A half][B half][row block][column block]
@@ -826,7 +1094,9 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
         for (int j = 0; j < 2; ++j) acc[h][b][i][j] = f32x16_t{};
 
   auto mma = [&](int ha, int hb, int i, int j, int q) {
-    if constexpr (!MX) {
+    if constexpr (F == kMx4) {
+      acc[ha][hb][i][j] = mfma_mx4(q, fr[2 + hb][j][q], fr[ha][i][q], acc[ha][hb][i][j], sc[2 + hb][j], sc[ha][i]);
+    } else if constexpr (F == kBf16) {
       acc[ha][hb][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fr[2 + hb][j][q]), as_bf16x8(fr[ha][i][q]),
                                                                   acc[ha][hb][i][j], 0, 0, 0);
     } else {
@@ -854,13 +1124,14 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     for (int t = 0; t < 4; ++t) {
       // four bf16 (or two MXFP8) MFMAs, one load and, in the first half of
       // the phase, four LDS reads
-      if constexpr (!MX) {
+      if constexpr (F != kMx8) {
         mma(ha, hb, 0, 0, t);
         mma(ha, hb, 0, 1, t);
         issue(iw, ic, t);
         if (t < 2) {
           readf(rw, rc, 0, 2 * t);
           readf(rw, rc, 1, 2 * t);
+          if constexpr (F == kMx4) reads(rw, rc, t);
         }
         mma(ha, hb, 1, 0, t);
         mma(ha, hb, 1, 1, t);
@@ -868,7 +1139,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
           readf(rw, rc, 0, 2 * t + 1);
           readf(rw, rc, 1, 2 * t + 1);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, F == kMx4 ? 2 : 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -958,7 +1229,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     return;
   }
   if constexpr (DUAL && MX) {
-    mx_store_h<4, 2, 128, 64>(a, smem, m0 + wm * 128, m_end, n0 + wn * 64, wave, lane, [&](int i, int j, int v) {
+    mx_store_h<F, 4, 2, 128, 64>(a, smem, m0 + wm * 128, m_end, n0 + wn * 64, wave, lane, [&](int i, int j, int v) {
       return silu_mul_fast(acc[i >> 1][0][i & 1][j][v], acc[i >> 1][1][i & 1][j][v]);
     });
   } else if constexpr (DUAL) {
@@ -982,7 +1253,7 @@ struct GemmShapes {
   // dual: 128 columns per matrix; single: 128 or 256 columns (see the kernel)
   static constexpr int BNW = DUAL ? 128 : 256;
   static constexpr int b0 = Stages<64, BNW, DUAL, W>::BYTES, b1 = Stages<128, BNW, DUAL, W>::BYTES;
-  static constexpr int b2 = W == 4 ? BigStages<false>::BYTES : Stages<256, BNW, DUAL, 8>::BYTES;
+  static constexpr int b2 = W == 4 ? BigStages<kBf16>::BYTES : Stages<256, BNW, DUAL, 8>::BYTES;
   static constexpr int b3 = DUAL ? 0 : Stages<256, 128, false, W>::BYTES;
   static constexpr int m01 = b0 > b1 ? b0 : b1, m23 = b2 > b3 ? b2 : b3;
   static constexpr int kSmem = (m01 > m23 ? m01 : m23) / 2;  // bf16 elements
@@ -1068,13 +1339,13 @@ __device__ __forceinline__ ExpertScan scan_experts(int tiles, int rows, int sk_r
           t0 & 0xffff,     t0 >> 16,       t1 & 0xffff,     t1 >> 16};
 }
 
-template <bool DUAL, int W>
+template <bool DUAL, int W, int F>
 struct MxShapes {
   static constexpr int BNW = DUAL ? 128 : 256;
-  static constexpr int b0 = MxStages<64, BNW, DUAL, W>::BYTES, b1 = MxStages<128, BNW, DUAL, W>::BYTES;
-  static constexpr int b2 = W == 4 ? BigStages<true>::BYTES : MxStages<256, BNW, DUAL, 8>::BYTES;
-  static constexpr int b3 = DUAL ? 0 : MxStages<256, 128, false, W>::BYTES;
-  static constexpr int b4 = MxStages<64, 128, DUAL, W>::BYTES, b5 = MxStages<128, 128, DUAL, W>::BYTES;
+  static constexpr int b0 = MxStages<64, BNW, DUAL, W, F>::BYTES, b1 = MxStages<128, BNW, DUAL, W, F>::BYTES;
+  static constexpr int b2 = W == 4 ? BigStages<F>::BYTES : MxStages<256, BNW, DUAL, 8, F>::BYTES;
+  static constexpr int b3 = DUAL ? 0 : MxStages<256, 128, false, W, F>::BYTES;
+  static constexpr int b4 = MxStages<64, 128, DUAL, W, F>::BYTES, b5 = MxStages<128, 128, DUAL, W, F>::BYTES;
   static constexpr int m01 = b0 > b1 ? b0 : b1, m23 = b2 > b3 ? b2 : b3, m45 = b4 > b5 ? b4 : b5;
   static constexpr int m = m01 > m23 ? m01 : m23;
   static constexpr int kSmem = (m > m45 ? m : m45) / 2;  // bf16 slots
@@ -1082,11 +1353,16 @@ struct MxShapes {
 
 // One tile of at most 128 rows (cls 0 or 1) and BN columns. SPLIT: K chunks
 // [kc0, kc1) only, fp32 sums to pbase (row stride pld, column base pcol0).
-template <int W, bool DUAL, bool MX, int BN, bool SPLIT, bool COH = false>
+template <int W, bool DUAL, int F, int BN, bool SPLIT, bool COH = false>
 __device__ __forceinline__ void run_low_tile(const GemmArgs& a, bf16_t* smem, int cls, int e, int m0, int m_end,
                                              int n0, int kc0 = 0, int kc1 = -1, float* pbase = nullptr,
                                              size_t ps = 0, int pld = 0, int pcol0 = 0, bool coh = true) {
-  if constexpr (MX) {
+  if constexpr (F == kMx4) {
+    if (cls == 0)
+      gemm_tile_mx4<W, 64, BN, 2, DUAL, SPLIT, COH>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0, coh);
+    else
+      gemm_tile_mx4<W, 128, BN, 2, DUAL, SPLIT, COH>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0, coh);
+  } else if constexpr (F == kMx8) {
     if (cls == 0)
       gemm_tile_mx<W, 64, BN, 2, DUAL, SPLIT, COH>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0, coh);
     else
@@ -1101,13 +1377,18 @@ __device__ __forceinline__ void run_low_tile(const GemmArgs& a, bf16_t* smem, in
 
 // One tile of the round schedule: any class, 128 columns per matrix or (a
 // wide single GEMM) 256; split along K when pbase != nullptr.
-template <int W, bool DUAL, bool MX, bool WIDE>
+template <int W, bool DUAL, int F, bool WIDE>
 __device__ __forceinline__ void run_tile(const GemmArgs& a, bf16_t* smem, int cls, int e, int m0, int m_end, int n0,
                                          int kc0, int kc1, float* pbase, size_t ps, int pld, int pcol0) {
   constexpr int BN = WIDE ? 256 : 128;
   if (cls == 2) {
     if constexpr (W == 8) {
-      if constexpr (MX) {
+      if constexpr (F == kMx4) {
+        if (pbase != nullptr)
+          gemm_tile_mx4<W, 256, BN, 4, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
+        else
+          gemm_tile_mx4<W, 256, BN, 4, DUAL>(a, smem, e, m0, m_end, n0);
+      } else if constexpr (F == kMx8) {
         if (pbase != nullptr)
           gemm_tile_mx<W, 256, BN, 4, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
         else
@@ -1119,8 +1400,13 @@ __device__ __forceinline__ void run_tile(const GemmArgs& a, bf16_t* smem, int cl
           gemm_tile<W, 256, BN, 4, DUAL>(a, smem, e, m0, m_end, n0);
       }
     } else if constexpr (DUAL || WIDE) {
-      big_tile<DUAL, MX>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
-    } else if constexpr (MX) {
+      big_tile<DUAL, F>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
+    } else if constexpr (F == kMx4) {
+      if (pbase != nullptr)
+        gemm_tile_mx4<W, 256, BN, 2, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
+      else
+        gemm_tile_mx4<W, 256, BN, 2, DUAL>(a, smem, e, m0, m_end, n0);
+    } else if constexpr (F == kMx8) {
       if (pbase != nullptr)
         gemm_tile_mx<W, 256, BN, 2, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
       else
@@ -1132,9 +1418,9 @@ __device__ __forceinline__ void run_tile(const GemmArgs& a, bf16_t* smem, int cl
         gemm_tile<W, 256, BN, 2, DUAL>(a, smem, e, m0, m_end, n0);
     }
   } else if (pbase != nullptr) {
-    run_low_tile<W, DUAL, MX, BN, true>(a, smem, cls, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
+    run_low_tile<W, DUAL, F, BN, true>(a, smem, cls, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
   } else {
-    run_low_tile<W, DUAL, MX, BN, false>(a, smem, cls, e, m0, m_end, n0);
+    run_low_tile<W, DUAL, F, BN, false>(a, smem, cls, e, m0, m_end, n0);
   }
 }
 
@@ -1207,6 +1493,20 @@ __device__ __forceinline__ void mx_quant_store4(float h0, float h1, float h2, fl
         static_cast<uint8_t>(code);
 }
 
+// The same as MXFP4.
+__device__ __forceinline__ void mx4_quant_store4(const GemmArgs& a, float h0, float h1, float h2, float h3, int row,
+                                                 int c) {
+  uint32_t top = max(max(abs_bits(h0), abs_bits(h1)), max(abs_bits(h2), abs_bits(h3)));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1, kWave));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2, kWave));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 4, kWave));
+  const uint32_t code = mx4_scale_code(top);
+  const uint32_t w = code == kMxNan ? 0 : e2m1x4(h0, h1, h2, h3, mx4_scale(code));
+  *reinterpret_cast<uint16_t*>(reinterpret_cast<uint8_t*>(a.C) + (size_t)row * mx4_row_bytes(a.N) + c / 2) =
+      static_cast<uint16_t>(w);
+  if ((c & (kMxBlock - 1)) == 0) mx4_store_scale(a, row, c, code);
+}
+
 // ---------------------------------------------------------------------------
 // Decode schedule (launches in which no expert exceeds sk_rows rows:
 // decode-sized batches and lightly loaded experts; bf16 and MXFP8). The work
@@ -1269,7 +1569,7 @@ __device__ __forceinline__ long long sk_blocks(long long U, long long G) {
 // this block's XCD. A slot holds NB planes of sk_rows x cols floats
 // (2 x 128 or 1 x 256 columns: the same size).
 constexpr int kFixBatch = 8;
-template <int W, bool DUAL, bool MX>
+template <int W, bool DUAL, int F>
 __device__ __forceinline__ void sk_fixup(const GemmArgs& a, int m0, int m_end, int n0, int cols, int bf, int nc,
                                          int j0, bool coh) {
   constexpr int NB = DUAL ? 2 : 1;
@@ -1307,7 +1607,9 @@ __device__ __forceinline__ void sk_fixup(const GemmArgs& a, int m0, int m_end, i
     float o[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = DUAL ? silu_mul_fast(g[v], u[v]) : g[v];
-    if (MX && DUAL) {
+    if constexpr (F == kMx4 && DUAL) {
+      mx4_quant_store4(a, o[0], o[1], o[2], o[3], m0 + r, n0 + c);
+    } else if (F == kMx8 && DUAL) {
       // h as MXFP8: the aligned 8 lanes around this one hold one 32-column
       // block of the row (items come in whole rows of 32 lanes)
       mx_quant_store4(o[0], o[1], o[2], o[3], m0 + r, n0 + c, a.N, a.M_cap, reinterpret_cast<uint8_t*>(a.C), a.Cs);
@@ -1323,7 +1625,7 @@ __device__ __forceinline__ void sk_fixup(const GemmArgs& a, int m0, int m_end, i
 // xcd_ok: the XCD check's result (1: block b runs on XCD b % 8). wide: a
 // single GEMM in 256-column tiles (T0 and s_start count those tiles), which
 // halves the tiles, and so the pipeline fills, of short-K launches.
-template <int W, bool DUAL, bool MX>
+template <int W, bool DUAL, int F>
 __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem, int T0, const int* s_start,
                                                 const int* s_row0, const int* s_rows, bool xcd_ok, bool wide) {
   constexpr int NB = DUAL ? 2 : 1;
@@ -1333,7 +1635,7 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
   const bool g8 = (G & 7) == 0;
   const int gx = G >> 3;  // blocks per XCD
   const int bo = g8 ? (b & 7) * gx + (b >> 3) : b;
-  const int nK = a.K / (MX ? kMxChunk : kBK);
+  const int nK = a.K / (F != kBf16 ? kMxChunk : kBK);  // MX operands: K in bytes
   // T0 * 8 stays far inside int: T0 <= E_local * N / 128 here
   SkPart P;
   P.U = (long long)T0 * nK;
@@ -1374,11 +1676,11 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
     if (kc0 == 0 && kc1 == nK) {
       if constexpr (!DUAL) {
         if (wide)
-          run_low_tile<W, DUAL, MX, 256, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
+          run_low_tile<W, DUAL, F, 256, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
         else
-          run_low_tile<W, DUAL, MX, 128, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
+          run_low_tile<W, DUAL, F, 128, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
       } else {
-        run_low_tile<W, DUAL, MX, 128, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
+        run_low_tile<W, DUAL, F, 128, false>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0);
       }
     } else {
       const long long t0 = (long long)t * nK;
@@ -1388,20 +1690,20 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
       float* mine = a.skpart + ((size_t)bo * 2 + (u == u_beg ? 0 : 1)) * slot_f;
       if constexpr (!DUAL) {
         if (wide)
-          run_low_tile<W, DUAL, MX, 256, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine,
+          run_low_tile<W, DUAL, F, 256, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine,
                                                   plane, 256, 0, coh);
         else
-          run_low_tile<W, DUAL, MX, 128, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine,
+          run_low_tile<W, DUAL, F, 128, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine,
                                                   plane, 128, 0, coh);
       } else {
-        run_low_tile<W, DUAL, MX, 128, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine, plane,
+        run_low_tile<W, DUAL, F, 128, true, true>(a, smem, cls, tr.e, tr.m0, tr.m_end, tr.n0, kc0, kc1, mine, plane,
                                                 128, 0, coh);
       }
       __syncthreads();  // every wave's stores have completed
       if (threadIdx.x == 0) s_last = atomicAdd(a.tcnt + bf, 1) == nc - 1;
       __syncthreads();
       if (uniform_int(s_last)) {
-        sk_fixup<W, DUAL, MX>(a, tr.m0, tr.m_end, tr.n0, cols, bf, nc, j0, coh);
+        sk_fixup<W, DUAL, F>(a, tr.m0, tr.m_end, tr.n0, cols, bf, nc, j0, coh);
         if (threadIdx.x == 0) __hip_atomic_store(a.tcnt + bf, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
@@ -1411,9 +1713,10 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
 
 // Body of the grouped GEMM kernels (bf16 or MXFP8; a K chunk is 64 bf16 or
 // 128 E4M3 elements, 128 bytes of a row either way).
-template <int W, bool DUAL, bool MX>
+template <int W, bool DUAL, int F>
 __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
-  constexpr int kSmem = MX ? MxShapes<DUAL, W>::kSmem : GemmShapes<DUAL, W>::kSmem;
+  constexpr bool MX = F != kBf16;
+  constexpr int kSmem = MX ? MxShapes<DUAL, W, F>::kSmem : GemmShapes<DUAL, W>::kSmem;
   constexpr int NB = DUAL ? 2 : 1;
   __shared__ __align__(16) bf16_t smem[kSmem];
   __shared__ int s_start[kMaxExperts + 1];
@@ -1486,12 +1789,12 @@ __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
       a.plan[2] = 1;
     }
     __syncthreads();
-    decode_schedule<W, DUAL, MX>(a, smem, dwide ? T0 / 2 : T0, s_start, s_row0, s_rows, uniform_int(s_xcd) == 1, dwide);
+    decode_schedule<W, DUAL, F>(a, smem, dwide ? T0 / 2 : T0, s_start, s_row0, s_rows, uniform_int(s_xcd) == 1, dwide);
     return;
   }
 
-  constexpr int CK = MX ? kMxChunk : kBK;  // K elements per chunk
-  constexpr int EB = MX ? 1 : 2;           // weight bytes per element (MX scales aside)
+  constexpr int CK = MX ? kMxChunk : kBK;  // units of K per chunk
+  constexpr int EB = MX ? 1 : 2;           // weight bytes per unit of K (MX scales aside)
   const int nK = a.K / CK;
   // K ranges the tail split (below) cuts each tile of the last round of an
   // unsplit launch of `tot` tiles of `tcols` columns into (1: none)
@@ -1604,11 +1907,11 @@ __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
     const int cls = tile_class(t.left);
     if constexpr (!DUAL) {
       if (wide) {
-        run_tile<W, DUAL, MX, true>(a, smem, cls, t.e, t.m0, t.m_end, t.n0, kc0, kc1, pbase, ps, pld, pcol0);
+        run_tile<W, DUAL, F, true>(a, smem, cls, t.e, t.m0, t.m_end, t.n0, kc0, kc1, pbase, ps, pld, pcol0);
         return;
       }
     }
-    run_tile<W, DUAL, MX, false>(a, smem, cls, t.e, t.m0, t.m_end, t.n0, kc0, kc1, pbase, ps, pld, pcol0);
+    run_tile<W, DUAL, F, false>(a, smem, cls, t.e, t.m0, t.m_end, t.n0, kc0, kc1, pbase, ps, pld, pcol0);
   };
 
   // Per-XCD work queues: block b runs on XCD b % 8 and takes items of that

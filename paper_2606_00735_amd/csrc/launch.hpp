@@ -61,6 +61,32 @@ hipError_t launch_ffn_mx(const uint8_t* xq, const uint32_t* xs, const uint8_t* w
                          const int32_t* offsets, int E_local, int H, int I, int ld_gu, int ld_dn, int M_cap,
                          void* y_perm, void* ws, hipStream_t s, int rows = 0);
 
+// MXFP4 (mx4_kernels.hip). Rows of activations: with src, row m of the operand is
+// row clamp(src[m] / div, 0, T - 1) of T rows.
+struct Mx4Rows {
+  const uint8_t* codes;
+  const uint32_t* scales;
+  const int32_t* src;
+  int div, T;
+};
+struct Mx4Weights {
+  const uint8_t* codes;
+  const uint32_t* scales;
+  int ld;  // bytes between code rows
+};
+hipError_t launch_mx4_quantize(const void* x, bool f32, int batch, int rows, int K, int ldc,
+                               const int32_t* row_count, uint8_t* codes, uint32_t* scales, hipStream_t s);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, int batch, int rows, int K, int ldc,
+                                 void* x, hipStream_t s);
+hipError_t launch_gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const int32_t* offsets,
+                             int E_local, int H, int I, int M_cap, uint8_t* hq, uint32_t* hs, hipStream_t s);
+hipError_t launch_gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weights& w, const int32_t* offsets,
+                           int E_local, int N, int K, int M_cap, void* c, hipStream_t s);
+size_t ffn_mx4_ws_bytes(int M_cap, int E_local, int H, int I);
+hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const Mx4Weights& wd,
+                          const int32_t* offsets, int E_local, int H, int I, int M_cap, void* y_perm, void* ws,
+                          hipStream_t s, int rows);
+
 // The result of the check that block b of a launch runs on XCD b % 8, for a
 // launch on stream s, or nullptr (ffn_kernels.hip).
 const int32_t* xcd_state(hipStream_t s);

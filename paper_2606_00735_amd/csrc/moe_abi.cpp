@@ -13,6 +13,7 @@
 #include "../../include/moe.h"
 #include "common.hpp"
 #include "launch.hpp"
+#include "mx.hpp"
 
 namespace {
 
@@ -157,6 +158,25 @@ moe_status mx_gemm_shape_ok(int E_local, int N, int K, int M_cap) {
   // tile offsets (256 rows of K bytes) are 32-bit in the kernels
   if (N > (1 << 20) || K > (1 << 20)) return MOE_ERR_UNSUPPORTED;
   if ((long long)M_cap * std::max(N, K) > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+// MXFP4: limits of the grouped products, as mx_gemm_shape_ok (rows of K / 2 bytes,
+// padded to whole 256-element chunks).
+moe_status mx4_row_stride(int ld, int K, int* out) {
+  const int row = moe::mx4_row_bytes(K);
+  if (ld == 0) ld = row;
+  if (ld < row || ld % 16 != 0 || ld > (1 << 20)) return MOE_ERR_INVALID_ARG;
+  *out = ld;
+  return MOE_OK;
+}
+
+// The rows of an MXFP4 FFN's x: M_cap of them, or T rows read through perm_src.
+moe_status mx4_rows_ok(const int32_t* perm_src, int T, int k, int H) {
+  if (perm_src == nullptr) return MOE_OK;
+  if (T < 1 || k < 1 || k > MOE_MAX_TOPK || !aligned4(perm_src)) return MOE_ERR_INVALID_ARG;
+  // row offsets are 32-bit in the kernels
+  if ((long long)T * std::max(moe::mx4_row_bytes(H), 8) >= (1LL << 32)) return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
 }
 
@@ -503,6 +523,90 @@ moe_status moe_grouped_swiglu_ffn_mx(const uint8_t* xq, const uint32_t* xs, cons
     return MOE_ERR_INVALID_ARG;
   return hip_status(moe::launch_ffn_mx(xq, xs, wgq, wgs, wuq, wus, wdq, wds, offsets, E_local, H, I, ld_gu, ld_dn,
                                        M_cap, y_perm, ws, stream));
+}
+
+moe_status moe_mx4_quantize(const void* x, moe_dtype dt, int batch, int rows, int K, int ld_codes,
+                            const int32_t* row_count, uint8_t* codes, uint32_t* scales, hipStream_t stream) {
+  if (!valid_dtype(dt) || batch < 0 || rows < 0 || K < 1) return MOE_ERR_INVALID_ARG;
+  if (K % 32 != 0 || K > (1 << 20)) return MOE_ERR_UNSUPPORTED;
+  int ldc = 0;
+  if (mx4_row_stride(ld_codes, K, &ldc) != MOE_OK) return MOE_ERR_INVALID_ARG;
+  if ((long long)batch * rows > (1LL << 40) / K) return MOE_ERR_UNSUPPORTED;
+  if (row_count != nullptr && (batch > 1 || !aligned4(row_count))) return MOE_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0) return MOE_OK;
+  if (!x || !aligned16(x) || !mx_operand_ok(codes, scales)) return MOE_ERR_INVALID_ARG;
+  return hip_status(
+      moe::launch_mx4_quantize(x, dt == MOE_F32, batch, rows, K, ldc, row_count, codes, scales, stream));
+}
+
+moe_status moe_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, int batch, int rows, int K, int ld_codes,
+                              void* x, hipStream_t stream) {
+  if (batch < 0 || rows < 0 || K < 1) return MOE_ERR_INVALID_ARG;
+  if (K % 32 != 0 || K > (1 << 20)) return MOE_ERR_UNSUPPORTED;
+  int ldc = 0;
+  if (mx4_row_stride(ld_codes, K, &ldc) != MOE_OK) return MOE_ERR_INVALID_ARG;
+  if ((long long)batch * rows > (1LL << 40) / K) return MOE_ERR_UNSUPPORTED;
+  if (batch == 0 || rows == 0) return MOE_OK;
+  if (!x || !aligned16(x) || !mx_operand_ok(codes, scales)) return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_mx4_dequantize(codes, scales, batch, rows, K, ldc, x, stream));
+}
+
+moe_status moe_grouped_swiglu_mx4(const uint8_t* xq, const uint32_t* xs, const int32_t* perm_src, int T, int k,
+                                  const uint8_t* wgq, const uint32_t* wgs, const uint8_t* wuq, const uint32_t* wus,
+                                  const int32_t* offsets, int E_local, int H, int I, int ldw, int M_cap, uint8_t* hq,
+                                  uint32_t* hs, hipStream_t stream) {
+  moe_status st = mx_gemm_shape_ok(E_local, I, H, M_cap);
+  if (st != MOE_OK) return st;
+  int ld = 0;
+  if ((st = mx4_row_stride(ldw, H, &ld)) != MOE_OK || (st = mx4_rows_ok(perm_src, T, k, H)) != MOE_OK) return st;
+  if (E_local == 0 || M_cap == 0) return MOE_OK;
+  if (!mx_operand_ok(xq, xs) || !mx_operand_ok(wgq, wgs) || !mx_operand_ok(wuq, wus) || !mx_operand_ok(hq, hs) ||
+      !offsets || !aligned4(offsets))
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_gateup_mx4({xq, xs, perm_src, k, T}, {wgq, wgs, ld}, {wuq, wus, ld}, offsets, E_local,
+                                           H, I, M_cap, hq, hs, stream));
+}
+
+moe_status moe_grouped_gemm_mx4(const uint8_t* aq, const uint32_t* as, const uint8_t* bq, const uint32_t* bs,
+                                const int32_t* offsets, int E_local, int N, int K, int ldb, int M_cap, void* c,
+                                hipStream_t stream) {
+  moe_status st = mx_gemm_shape_ok(E_local, N, K, M_cap);
+  if (st != MOE_OK) return st;
+  int ld = 0;
+  if ((st = mx4_row_stride(ldb, K, &ld)) != MOE_OK) return st;
+  if (E_local == 0 || M_cap == 0) return MOE_OK;
+  if (!mx_operand_ok(aq, as) || !mx_operand_ok(bq, bs) || !c || !aligned16(c) || !offsets || !aligned4(offsets))
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_gemm_mx4(aq, as, {bq, bs, ld}, offsets, E_local, N, K, M_cap, c, stream));
+}
+
+moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs, const int32_t* perm_src, int T, int k,
+                                      const uint8_t* wgq, const uint32_t* wgs, const uint8_t* wuq,
+                                      const uint32_t* wus, const uint8_t* wdq, const uint32_t* wds,
+                                      const int32_t* offsets, int E, int E_local, int H, int I, int ldw_gu,
+                                      int ldw_dn, int M_cap, void* y_perm, void* ws, size_t* ws_bytes,
+                                      hipStream_t stream) {
+  moe_status st = mx_gemm_shape_ok(E_local, I, H, M_cap);
+  if (st != MOE_OK) return st;
+  if (E < 0 || E > MOE_MAX_EXPERTS || (E > 0 && E < E_local) || ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  int ld_gu = 0, ld_dn = 0;
+  if ((st = mx4_row_stride(ldw_gu, H, &ld_gu)) != MOE_OK || (st = mx4_row_stride(ldw_dn, I, &ld_dn)) != MOE_OK)
+    return st;
+  const size_t need = moe::ffn_mx4_ws_bytes(M_cap, E_local, H, I);
+  if (ws == nullptr) {
+    *ws_bytes = need;
+    return MOE_OK;
+  }
+  if ((st = mx4_rows_ok(perm_src, T, k, H)) != MOE_OK) return st;
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (E_local == 0 || M_cap == 0) return MOE_OK;
+  if (!mx_operand_ok(xq, xs) || !mx_operand_ok(wgq, wgs) || !mx_operand_ok(wuq, wus) || !mx_operand_ok(wdq, wds) ||
+      !y_perm || !aligned16(y_perm) || !aligned16(ws) || !offsets || !aligned4(offsets))
+    return MOE_ERR_INVALID_ARG;
+  // rows an expert is expected to have, as in moe_grouped_swiglu_ffn_gather_of
+  const int rows = E > 0 && perm_src != nullptr ? (int)std::max(1LL, (long long)T * k / E) : 0;
+  return hip_status(moe::launch_ffn_mx4({xq, xs, perm_src, k, T}, {wgq, wgs, ld_gu}, {wuq, wus, ld_gu},
+                                        {wdq, wds, ld_dn}, offsets, E_local, H, I, M_cap, y_perm, ws, stream, rows));
 }
 
 }  // extern "C"

@@ -46,4 +46,57 @@ __device__ __forceinline__ uint32_t e4m3x4(float v0, float v1, float v2, float v
   return static_cast<uint32_t>(w);
 }
 
+// ---------------------------------------------------------------------------
+// OCP Microscaling FP4 (MXFP4): E2M1 elements (+-0, 0.5, 1, 1.5, 2, 3, 4, 6)
+// under the same 32-element E8M0 scales. A row is padded with zero codes to
+// whole chunks of 256 elements = 128 bytes (two codes a byte, the even element
+// in the low half), so a chunk is the same 128-byte tile row as 64 bf16 or 128
+// E4M3 elements.
+//
+// The scaled MFMA reads 32 consecutive elements of a row from lane (row, h), h
+// = 0, 1, for its 64 elements of K, i.e. one block, and that block's code from
+// byte s of a scale register of the same lane. The 8 codes of a chunk are kept
+// as two dwords, that of h holding block 2 s + h in byte s: a lane's dword then
+// serves all four k-steps of a chunk as it is. Dwords are stored chunk-major,
+// scales[chunk][row][2], so one chunk of a tile's rows is contiguous.
+//
+// A block that holds a NaN or an infinity takes scale code 255, E8M0's NaN (and
+// zero element codes): the MFMA makes every product with it a NaN, so a bad
+// value shows instead of being clamped to a number.
+// ---------------------------------------------------------------------------
+constexpr int kMx4Chunk = 256;
+constexpr uint32_t kMxNan = 255;
+
+// Bytes of a row of K elements: whole chunks.
+__host__ __device__ __forceinline__ int mx4_row_bytes(int K) {
+  return (K + kMx4Chunk - 1) / kMx4Chunk * (kMx4Chunk / 2);
+}
+
+// Scale code of a block from the largest of its elements' fp32 bits without the
+// sign (an integer maximum: NaNs and infinities, which have the largest bits,
+// are not lost). E2M1's largest power of two is 2^2: floor(log2 amax) - 2, as in
+// mx_scale_code.
+__device__ __forceinline__ uint32_t mx4_scale_code(uint32_t amax_bits) {
+  const int be = static_cast<int>(amax_bits >> 23);
+  return be == 255 ? kMxNan : (be > 2 ? static_cast<uint32_t>(be - 2) : 0u);
+}
+
+// 2^(c - 127) as fp32 (a NaN for code 255), the scale operand of the conversions.
+__device__ __forceinline__ float mx4_scale(uint32_t c) {
+  return __uint_as_float(c == 0 ? 0x00400000u : (c == kMxNan ? 0x7fc00000u : c << 23));
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Byte of a chunk's two scale dwords that holds block b (0..7).
+__device__ __forceinline__ int mx4_scale_byte(int b) { return (b & 1) * 4 + (b >> 1); }
+
+// Four values over a block's scale as E2M1 codes in the low 16 bits (v0 in bits
+// 0-3): v_cvt_scalef32_pk_fp4_f32 divides, rounds to nearest even and clamps to
+// +-6.
+__device__ __forceinline__ uint32_t e2m1x4(float v0, float v1, float v2, float v3, float scale) {
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v0, v1, scale, 0);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v2, v3, scale, 1);
+}
+
 }  // namespace moe

@@ -1,0 +1,334 @@
+// MXFP4 (OCP MX block scaling with E2M1 elements, mx.hpp): quantisation of
+// activations and expert weights, the values of codes, and the expert FFN on
+// 4-bit operands.
+#include <algorithm>
+
+#include "common.hpp"
+#include "grouped_gemm.hpp"
+#include "launch.hpp"
+#include "mx.hpp"
+
+namespace moe {
+
+// ---------------------------------------------------------------------------
+// Quantisation: x [batch][rows][K] (bf16 or fp32) -> codes (rows ldc bytes
+// apart) and scale dwords [batch][chunks][rows][2].
+//
+// Bound by the copy: a row's chunk of 256 elements is 512 bytes of bf16 (1 KB
+// of fp32) in, one 128-byte line of codes and 8 bytes of scales out. A block
+// takes kQRows rows x kQChunks chunks, so that the scales of a chunk leave as
+// whole lines (16 rows x 8 bytes) and every thread has kQChunks * 2 loads in
+// flight. 32 lanes work on a row's chunk, 8 elements each: the 4 lanes of a
+// block find its largest magnitude with two shuffles.
+// row_count (device, optional, batch 1 only): only rows [0, min(rows,
+// *row_count)) are quantised; the others are left as they are.
+// ---------------------------------------------------------------------------
+constexpr int kQRows = 16, kQChunks = 2;
+
+// A block's share: kQRows rows from row0 on of matrix b, kQChunks chunks from
+// chunk0 on. At most 2^31 of them (batch * rows * K <= 2^40, K >= 32).
+struct QTile {
+  size_t b;
+  int row0, chunk0;
+};
+__host__ __device__ __forceinline__ uint32_t q_cgroups(int K) {
+  return (uint32_t)((K + kMx4Chunk * kQChunks - 1) / (kMx4Chunk * kQChunks));
+}
+__host__ __device__ __forceinline__ uint32_t q_rgroups(int rows) {
+  return ((uint32_t)rows + kQRows - 1) / kQRows;
+}
+__device__ __forceinline__ QTile q_tile(uint32_t u, int rows, int K) {
+  const uint32_t ncg = q_cgroups(K), nrg = q_rgroups(rows);
+  const uint32_t r = u / ncg, b = r / nrg;
+  return {b, (int)((r - b * nrg) * kQRows), (int)((u - r * ncg) * kQChunks)};
+}
+constexpr uint32_t kQMaxGrid = 1u << 20;  // blocks of a launch; each loops over the rest
+
+template <bool F32IN>
+__global__ __launch_bounds__(256) void mx4_quantize_kernel(const void* __restrict__ x, uint32_t tiles, int rows,
+                                                           int K, int ldc, const int32_t* __restrict__ row_count,
+                                                           uint8_t* __restrict__ codes,
+                                                           uint32_t* __restrict__ scales) {
+  const int live = row_count != nullptr ? min(max(*row_count, 0), rows) : rows;
+  const int chunks = (K + kMx4Chunk - 1) / kMx4Chunk;
+  const int lane32 = threadIdx.x & 31, group = threadIdx.x >> 5;  // 8 groups of 32 lanes
+  constexpr int NT = kQRows * kQChunks / 8;                       // (row, chunk) pairs of a group
+  for (uint32_t u0 = blockIdx.x; u0 < tiles; u0 += gridDim.x) {
+    const QTile tile = q_tile(u0, rows, K);
+    const size_t b = tile.b;
+    uint32_t v[NT][8];  // fp32 bits
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int p = i * 8 + group, row = tile.row0 + p / kQChunks;
+      const int col = (tile.chunk0 + p % kQChunks) * kMx4Chunk + lane32 * 8;
+      const bool in = row < live && col < K;
+      const size_t off = in ? (b * rows + row) * (size_t)K + col : 0;
+      if (F32IN) {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const float*>(x) + off);
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        if (in) lo = s[0], hi = s[1];
+        v[i][0] = lo.x, v[i][1] = lo.y, v[i][2] = lo.z, v[i][3] = lo.w;
+        v[i][4] = hi.x, v[i][5] = hi.y, v[i][6] = hi.z, v[i][7] = hi.w;
+      } else {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (in) u = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(x) + off);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[i][2 * q] = w[q] << 16, v[i][2 * q + 1] = w[q] & 0xFFFF0000u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int p = i * 8 + group, row = tile.row0 + p / kQChunks, chunk = tile.chunk0 + p % kQChunks;
+      uint32_t top = 0;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) top = max(top, v[i][q] & 0x7fffffffu);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1, kWave));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2, kWave));
+      const uint32_t code = mx4_scale_code(top);
+      const float sc = mx4_scale(code);
+      auto f = [&](int q) { return __uint_as_float(v[i][q]); };
+      uint32_t out = e2m1x4(f(0), f(1), f(2), f(3), sc) | e2m1x4(f(4), f(5), f(6), f(7), sc) << 16;
+      if (code == kMxNan) out = 0;
+      // lane h of the first two gathers the codes of blocks h, 2 + h, 4 + h, 6 + h
+      uint32_t word = 0;
+      const int h = lane32 & 1;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) word |= (uint32_t)__shfl((int)code, (2 * s + h) * 4, 32) << (8 * s);
+      if (row < live && chunk < chunks) {
+        *reinterpret_cast<uint32_t*>(codes + (b * rows + row) * (size_t)ldc + chunk * 128 + lane32 * 4) = out;
+        if (lane32 < 2) scales[((b * chunks + chunk) * rows + row) * 2 + lane32] = word;
+      }
+    }
+  }
+}
+
+hipError_t launch_mx4_quantize(const void* x, bool f32, int batch, int rows, int K, int ldc,
+                               const int32_t* row_count, uint8_t* codes, uint32_t* scales, hipStream_t s) {
+  const uint32_t tiles = (uint32_t)batch * q_rgroups(rows) * q_cgroups(K), grid = std::min(tiles, kQMaxGrid);
+  if (f32)
+    mx4_quantize_kernel<true><<<grid, 256, 0, s>>>(x, tiles, rows, K, ldc, row_count, codes, scales);
+  else
+    mx4_quantize_kernel<false><<<grid, 256, 0, s>>>(x, tiles, rows, K, ldc, row_count, codes, scales);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// The values that codes stand for, exact in bf16 (two significant bits under a
+// power of two of at least 2^-128). The tiling of the quantiser: a group of 32
+// lanes reads a row's chunk, 4 bytes a lane, and writes its 512 bytes.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes,
+                                                             const uint8_t* __restrict__ scales, uint32_t tiles,
+                                                             int rows, int K, int ldc, bf16_t* __restrict__ x) {
+  const int chunks = (K + kMx4Chunk - 1) / kMx4Chunk;
+  const int lane32 = threadIdx.x & 31, group = threadIdx.x >> 5;
+  constexpr int NT = kQRows * kQChunks / 8;
+  for (uint32_t u0 = blockIdx.x; u0 < tiles; u0 += gridDim.x) {
+    const QTile tile = q_tile(u0, rows, K);
+    const size_t b = tile.b;
+    uint32_t w[NT], c[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int p = i * 8 + group, row = tile.row0 + p / kQChunks, chunk = tile.chunk0 + p % kQChunks;
+      const bool in = row < rows && chunk * kMx4Chunk + lane32 * 8 < K;
+      w[i] = c[i] = 0;
+      if (in) {
+        w[i] = *reinterpret_cast<const uint32_t*>(codes + (b * rows + row) * (size_t)ldc + chunk * 128 + lane32 * 4);
+        c[i] = scales[((b * chunks + chunk) * rows + row) * 8 + mx4_scale_byte(lane32 >> 2)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int p = i * 8 + group, row = tile.row0 + p / kQChunks, chunk = tile.chunk0 + p % kQChunks;
+      const int col = chunk * kMx4Chunk + lane32 * 8;
+      if (row >= rows || col >= K) continue;
+      uint32_t o[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t r = 0;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t n = (w[i] >> (8 * q + 4 * e)) & 15u;
+          // bf16 bits of the E2M1 value: 0, 0.5, or exponent and mantissa bit
+          // moved to place (exponent bias 1 -> 127, mantissa to the top bit)
+          const uint32_t m = n & 7u;
+          float f = m < 2u ? (m ? 0.5f : 0.0f) : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
+          f = ldexpf(f, (int)c[i] - 127);
+          if (c[i] == kMxNan) f = __uint_as_float(0x7fc00000u);
+          r |= (__float_as_uint(f) >> 16 | (n & 8u) << 12) << (16 * e);
+        }
+        o[q] = r;
+      }
+      *reinterpret_cast<uint4*>(x + (b * rows + row) * (size_t)K + col) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+  }
+}
+
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, int batch, int rows, int K, int ldc,
+                                 void* x, hipStream_t s) {
+  const uint32_t tiles = (uint32_t)batch * q_rgroups(rows) * q_cgroups(K);
+  mx4_dequantize_kernel<<<std::min(tiles, kQMaxGrid), 256, 0, s>>>(
+      codes, reinterpret_cast<const uint8_t*>(scales), tiles, rows, K, ldc,
+                                             static_cast<bf16_t*>(x));
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Expert FFN: gate/up (MXFP4 in, MXFP4 h out), then down (bf16 out), by the tile
+// schedules of the bf16 FFN (grouped_gemm.hpp).
+// ---------------------------------------------------------------------------
+template <bool DUAL, int W>
+__global__ __launch_bounds__(W* kWave) void grouped_gemm_mx4_kernel(GemmArgs a) {
+  grouped_gemm_body<W, DUAL, kMx4>(a);
+}
+
+// The MXFP4 gate/up reduction: sums the S partials of gate and up for 4
+// consecutive columns of a row per thread in split order, applies SiLU(gate) * up
+// and quantises each 32-column block (the 8 lanes of an aligned lane group; N % 32
+// == 0 keeps a group inside one block and wholly in range or out). Does nothing
+// when the GEMM before it split nothing.
+__global__ __launch_bounds__(256) void split_reduce_mx4_kernel(GemmArgs a) {
+  const int32_t* plan = a.plan;
+  const int S = plan[0], N = a.N;
+  if (S <= 1) {  // tail tiles of an unsplit launch
+    const int St = plan[2];
+    if (St <= 1) return;
+    const size_t items = (size_t)plan[3] * 256 * (plan[4] / 4);
+    for (size_t it = (size_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (size_t)gridDim.x * 256) {
+      TailItem t;
+      if (!tail_item(a.part, plan, 2, it, t)) continue;
+      const float4 g = sum_splits(t.p, t.tsz, St), u = sum_splits(t.p + St * t.tsz, t.tsz, St);
+      mx4_quant_store4(a, silu_mul_fast(g.x, u.x), silu_mul_fast(g.y, u.y), silu_mul_fast(g.z, u.z),
+                       silu_mul_fast(g.w, u.w), t.row, t.col);
+    }
+    return;
+  }
+  const int R = plan[1], n4 = N / 4;
+  const size_t items = (size_t)R * n4, sstride = (size_t)R * N, bstride = (size_t)S * R * N;
+  for (size_t it = (size_t)blockIdx.x * 256 + threadIdx.x; it < items; it += (size_t)gridDim.x * 256) {
+    const int j = (int)(it / n4), c = (int)(it % n4) * 4;
+    const float* p = a.part + (size_t)j * N + c;
+    const float4 g = sum_splits(p, sstride, S), u = sum_splits(p + bstride, sstride, S);
+    mx4_quant_store4(a, silu_mul_fast(g.x, u.x), silu_mul_fast(g.y, u.y), silu_mul_fast(g.z, u.z),
+                     silu_mul_fast(g.w, u.w), plan[kPlanHead + j], c);
+  }
+}
+
+// Workspace: counters (kCntBytes, zero before first use, as for bf16) | h codes
+// [M_cap][row bytes of I] | h scale dwords [chunks of I][M_cap][2] | split-K plan
+// | fp32 partials (split-K, or the decode schedule's slots).
+struct FfnMx4Ws {
+  size_t hq, hs, plan, part;  // byte offsets
+  long long part_cap;
+  int plan_rows;
+  size_t bytes;
+};
+
+static FfnMx4Ws ffn_mx4_ws_layout(int M_cap, int E_local, int H, int I) {
+  FfnMx4Ws w{};
+  const size_t ib = (size_t)mx4_row_bytes(I);
+  w.hq = kCntBytes;
+  w.hs = w.hq + round256(M_cap * ib);
+  w.plan = w.hs + round256(ib / 128 * M_cap * 8);
+  const long long need = (long long)kMaxSplit * M_cap * std::max(2LL * I, (long long)H);
+  w.part_cap = std::min(need, kPartCapFloats);
+  w.plan_rows = std::max(M_cap, kSmallM * E_local);
+  w.part = w.plan + round256((size_t)(kPlanHead + (size_t)w.plan_rows) * 4);
+  w.bytes = w.part + round256((size_t)std::max(w.part_cap, sk_slot_floats()) * 4);
+  return w;
+}
+
+size_t ffn_mx4_ws_bytes(int M_cap, int E_local, int H, int I) {
+  return ffn_mx4_ws_layout(M_cap, E_local, H, I).bytes;
+}
+
+static hipError_t gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const int32_t* offsets,
+                             int E_local, int H, int I, int M_cap, uint8_t* hq, uint32_t* hs, const MxSplit& sp,
+                             hipStream_t s, int rows) {
+  GemmArgs g{};
+  g.A = reinterpret_cast<const bf16_t*>(x.codes);
+  g.B0 = reinterpret_cast<const bf16_t*>(wg.codes);
+  g.B1 = reinterpret_cast<const bf16_t*>(wu.codes);
+  g.C = reinterpret_cast<bf16_t*>(hq);
+  g.offsets = offsets;
+  g.E_local = E_local;
+  g.M_cap = M_cap;
+  g.N = I;
+  g.K = mx4_row_bytes(H);
+  g.ldb = wg.ld;
+  g.a_src = x.src;
+  g.a_div = x.div;
+  g.a_T = x.T;
+  mx_split_args(g, sp);
+  g.As = x.scales;
+  g.Bs0 = wg.scales;
+  g.Bs1 = wu.scales;
+  g.Cs = hs;
+  const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
+  hipError_t e = launch_waves(waves_for(true, M_cap, E_local, I, H, rows), g, mx_grid(M_cap, E_local, I, split || g.sk),
+                              s, grouped_gemm_mx4_kernel<true, 4>, grouped_gemm_mx4_kernel<true, 8>);
+  if (e != hipSuccess || !split || sp.no_reduce) return e;
+  split_reduce_mx4_kernel<<<mx_reduce_grid(0, 0), 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+static hipError_t gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weights& w, const int32_t* offsets,
+                           int E_local, int N, int K, int M_cap, void* c, const MxSplit& sp, hipStream_t s,
+                           int rows) {
+  GemmArgs g{};
+  g.A = reinterpret_cast<const bf16_t*>(aq);
+  g.B0 = reinterpret_cast<const bf16_t*>(w.codes);
+  g.C = static_cast<bf16_t*>(c);
+  g.offsets = offsets;
+  g.E_local = E_local;
+  g.M_cap = M_cap;
+  g.N = N;
+  g.K = mx4_row_bytes(K);
+  g.ldb = w.ld;
+  mx_split_args(g, sp);
+  g.As = as;
+  g.Bs0 = w.scales;
+  const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
+  hipError_t e = launch_waves(waves_for(false, M_cap, E_local, N, K, rows), g,
+                              mx_grid(M_cap, E_local, N, split || g.sk), s, grouped_gemm_mx4_kernel<false, 4>,
+                              grouped_gemm_mx4_kernel<false, 8>);
+  if (e != hipSuccess || !split || sp.no_reduce) return e;
+  split_reduce_kernel<false><<<mx_reduce_grid(0, 0), 256, 0, s>>>(sp.part, sp.plan, N, static_cast<bf16_t*>(c));
+  return hipGetLastError();
+}
+
+hipError_t launch_gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const int32_t* offsets,
+                             int E_local, int H, int I, int M_cap, uint8_t* hq, uint32_t* hs, hipStream_t s) {
+  if (E_local == 0 || M_cap == 0) return hipSuccess;
+  return gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, MxSplit{}, s, 0);
+}
+
+hipError_t launch_gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weights& w, const int32_t* offsets,
+                           int E_local, int N, int K, int M_cap, void* c, hipStream_t s) {
+  if (E_local == 0 || M_cap == 0) return hipSuccess;
+  return gemm_mx4(aq, as, w, offsets, E_local, N, K, M_cap, c, MxSplit{}, s, 0);
+}
+
+hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const Mx4Weights& wd,
+                          const int32_t* offsets, int E_local, int H, int I, int M_cap, void* y_perm, void* ws,
+                          hipStream_t s, int rows) {
+  if (E_local == 0 || M_cap == 0) return hipSuccess;
+  const FfnMx4Ws L = ffn_mx4_ws_layout(M_cap, E_local, H, I);
+  char* w = static_cast<char*>(ws);
+  uint8_t* hq = reinterpret_cast<uint8_t*>(w + L.hq);
+  uint32_t* hs = reinterpret_cast<uint32_t*>(w + L.hs);
+  int32_t* cnt = reinterpret_cast<int32_t*>(w);
+  // as in launch_ffn: a token adds at most one row to an expert, so with the
+  // row gather the bound on an expert's rows is min(T, M_cap)
+  const bool no_reduce = (x.src != nullptr ? std::min(x.T, M_cap) : M_cap) <= kSkHostRows;
+  const MxSplit sp1{reinterpret_cast<float*>(w + L.part), L.part_cap, reinterpret_cast<int32_t*>(w + L.plan),
+                    L.plan_rows, cnt + kQueueGU, cnt + kDoneGU, cnt + kTcntGU, no_reduce, xcd_state(s)};
+  hipError_t e = gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, sp1, s, rows);
+  if (e != hipSuccess) return e;
+  const MxSplit sp2{sp1.part, sp1.part_cap, sp1.plan, sp1.plan_rows, cnt + kQueueDN, cnt + kDoneDN, cnt + kTcntDN,
+                    no_reduce, sp1.xcd};
+  return gemm_mx4(hq, hs, wd, offsets, E_local, H, I, M_cap, y_perm, sp2, s, rows);
+}
+
+}  // namespace moe

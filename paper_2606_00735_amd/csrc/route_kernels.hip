@@ -469,7 +469,8 @@ __global__ __launch_bounds__(512) void gate_topk_bf16_wide_kernel(
 #pragma unroll
     for (int j = 0; j < NI; ++j) bfr[buf][j] = lds_frag<kGateBK>(st + BT * kGateBK, (wn * NI + j) * 32 + r, chunk);
   };
-  auto mma = [&](int buf) {
+  auto mma = [&](int s) {
+    const int buf = s & 1;
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[buf], bfr[buf][j], acc[j], 0, 0, 0);
   };
