@@ -555,6 +555,95 @@ moe_status moe_load_sweep_mx(const uint8_t* xq, const uint32_t* xs, const uint8_
                              hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * The router's training step: losses that balance the experts' loads, their
+ * gradient to the router logits, and the gradients of the combine and of the
+ * router's product. With the experts frozen (in 4 bits, say) this fine-tunes the
+ * router:  moe_combine_backward -> dtopk_w, moe_balance_loss -> counts,
+ * moe_gate_backward -> dlogits, moe_router_grad -> dW_router.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * moe_balance_loss - balance loss, z loss and per-expert counts of a router.
+ *
+ * Tokens form groups of seq_len consecutive rows (0: one group of all T), a
+ * sequence each; mask (or NULL) marks the live ones (non-zero). With p[t,:] =
+ * softmax(logits[t,:]), lse[t] = log sum_e exp(logits[t,e]), and for group s of
+ * n_s live tokens c[s,e] = #{(t,j) live in s : topk_ids[t,j] == e}:
+ *   loss[0] = mean over groups with n_s > 0 of E / (k n_s^2) sum_e c[s,e] sum_t p[t,e]
+ *   loss[1] = mean over live tokens of lse[t]^2
+ * (0 without live tokens). loss[0] is sum_e f_e P_e with f_e = E c_e / (k n) and
+ * P_e the mean of p[:,e]: 1 for equal loads, up to E / k for the most skewed.
+ * What masked rows hold is not used. A row that is -inf throughout has p = 0 and
+ * lse = 0. Ids outside [0, E) are not counted.
+ *
+ * logits   [T, E] fp32 (moe_gate_topk's logits_out; 16-byte aligned)
+ * topk_ids [T, k] int32
+ * mask     [T] uint8 or NULL
+ * loss     [2] fp32
+ * counts   [groups, E] int32
+ * live     [groups + 2] int32: n_s, then the sum of all, then the number of
+ *          groups with live tokens
+ * ws       must be zero before the first call on it (every call leaves it zero,
+ *          so calls of any sizes can share one); such calls must not overlap
+ * Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), T a multiple of seq_len, T * E <=
+ * 2^40 and at most 2^23 blocks of up to 2048 / E tokens (at least 32) of a group.
+ * Sums are fp32 within a block, joined in fp64 in a fixed order: results do not
+ * depend on timing.
+ */
+moe_status moe_balance_loss(const float* logits, const int32_t* topk_ids, const uint8_t* mask,
+                            int T, int E, int k, int seq_len, float* loss, int32_t* counts,
+                            int32_t* live, void* ws, size_t* ws_bytes, hipStream_t stream);
+
+/*
+ * moe_gate_backward - gradient to the router logits.
+ *
+ * dlogits[t,e] = (live t)  dloss[0] E / (S k n_s^2) p[t,e] (c[s,e] - sum_j c[s,j] p[t,j])
+ *                        + dloss[1] 2 / n lse[t] p[t,e]
+ *              + (every t) sum over j with topk_ids[t,j] == e of
+ *                          topk_w[t,j] (dtopk_w[t,j] - sum_i topk_w[t,i] dtopk_w[t,i])
+ * where n and S are the live tokens and the groups that have some: the gradients
+ * of moe_balance_loss's losses (counts do not carry one) and of moe_gate_topk's
+ * weights.
+ *
+ * counts, live  as moe_balance_loss wrote them; T, E, k, seq_len, mask as there
+ * dloss         [2] fp32 (DEVICE): gradients of the two losses
+ * topk_w, dtopk_w [T, k] fp32, both or neither (NULL: only the losses' part)
+ * dlogits       [T, E] fp32, written completely (16-byte aligned)
+ */
+moe_status moe_gate_backward(const float* logits, const int32_t* topk_ids, const uint8_t* mask,
+                             const int32_t* counts, const int32_t* live, const float* dloss,
+                             const float* topk_w, const float* dtopk_w, int T, int E, int k,
+                             int seq_len, float* dlogits, hipStream_t stream);
+
+/*
+ * moe_combine_backward - gradient of moe_unpermute_combine.
+ *
+ * dtopk_w[t,j] = sum_h dout[t,h] y_perm[dest[t*k+j],h]  (0 where dest is not in [0, M_cap))
+ * dy_perm[dest[t*k+j],:] = round_dt( topk_w[t,j] dout[t,:] )
+ * (fp32 products and sums). Arguments as moe_unpermute_combine; dtopk_w [T, k]
+ * fp32; dy_perm [M_cap, H] dt or NULL: rows that no dest names are left alone.
+ */
+moe_status moe_combine_backward(const void* dout, const void* y_perm, const float* topk_w,
+                                const int32_t* dest, int T, int k, int H, int M_cap, moe_dtype dt,
+                                float* dtopk_w, void* dy_perm, hipStream_t stream);
+
+/*
+ * moe_router_grad - gradient of the router's product logits = x W_router^T + bias.
+ *
+ * dx        [T, H] dt or NULL  round_dt( dlogits W_router )
+ * dw_router [E, H] fp32        dlogits^T x
+ * dbias     [E]    fp32        sum_t dlogits[t,:]
+ * dlogits [T, E] fp32; x [T, H], w_router [E, H] dt. bf16: dlogits enters the MFMA
+ * as the sum of two bf16 terms (17 significant bits), sums are fp32. T == 0 writes
+ * zeros to dw_router and dbias. ws holds partial sums over ranges of tokens, added
+ * in order (results do not depend on timing); its size depends on the device's
+ * compute units. Limits: 1 <= E <= 256, H % 8 == 0 (bf16: H % 64 == 0), H <= 2^20.
+ */
+moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_router, int T, int E,
+                           int H, moe_dtype dt, void* dx, float* dw_router, float* dbias, void* ws,
+                           size_t* ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Placement control path (Section 4.2, Algorithms 1 and 2): the per-GPU
  * latency model f_g, the latency-aware greedy placement, the drift detector
  * and the incremental swap solver, for L MoE layers of E experts on G GPUs.

@@ -17,6 +17,7 @@ from ._lib import (  # noqa: F401
     MoeError,
     Mx4Tensor,
     MxTensor,
+    balance_ws_bytes,
     ffn_hidden,
     ffn_mx4_ws_bytes,
     ffn_mx_ws_bytes,
@@ -24,9 +25,12 @@ from ._lib import (  # noqa: F401
     gate_ws_bytes,
     hist_ws_bytes,
     load_library,
+    moe_balance_loss,
+    moe_combine_backward,
     moe_drift_distance,
     moe_expert_histogram_scan,
     moe_fit_latency_model,
+    moe_gate_backward,
     moe_gate_topk,
     moe_grouped_gemm_mx,
     moe_grouped_gemm_mx4,
@@ -47,9 +51,11 @@ from ._lib import (  # noqa: F401
     moe_place_greedy,
     moe_place_incremental,
     moe_placement_cost,
+    moe_router_grad,
     moe_unpermute_combine,
     moe_window_push,
     mx4_chunks,
     pad_weight_rows,
+    router_grad_ws_bytes,
     weight_row_stride,
 )

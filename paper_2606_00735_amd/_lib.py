@@ -28,7 +28,8 @@ EXPORTED = ("moe_status_string", "moe_abi_version", "moe_gate_topk", "moe_expert
             "moe_grouped_gemm_mx", "moe_grouped_swiglu_ffn_mx", "moe_load_sweep_mx",
             "moe_grouped_swiglu_ffn_gather", "moe_grouped_swiglu_ffn_gather_of",
             "moe_grouped_swiglu_ffn_noalloc", "moe_ffn_scratch_bytes", "moe_mx4_quantize", "moe_mx4_dequantize",
-            "moe_grouped_swiglu_mx4", "moe_grouped_gemm_mx4", "moe_grouped_swiglu_ffn_mx4")
+            "moe_grouped_swiglu_mx4", "moe_grouped_gemm_mx4", "moe_grouped_swiglu_ffn_mx4", "moe_balance_loss",
+            "moe_gate_backward", "moe_combine_backward", "moe_router_grad")
 
 
 class MoeError(RuntimeError):
@@ -115,6 +116,14 @@ def load_library(path: str = LIB_PATH):
     L.moe_grouped_swiglu_ffn_mx4.restype = _I
     L.moe_grouped_swiglu_ffn_mx4.argtypes = [_P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I,
                                              _I, _P, _P, _PSZ, _P]
+    L.moe_balance_loss.restype = _I
+    L.moe_balance_loss.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _PSZ, _P]
+    L.moe_gate_backward.restype = _I
+    L.moe_gate_backward.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P]
+    L.moe_combine_backward.restype = _I
+    L.moe_combine_backward.argtypes = [_P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P]
+    L.moe_router_grad.restype = _I
+    L.moe_router_grad.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _PSZ, _P]
     if L.moe_abi_version() != 3:
         raise RuntimeError("libmoe ABI version mismatch")
     _lib = L
@@ -496,6 +505,155 @@ def ffn_hidden(ws, M_cap, I, dtype):
     es = 2 if dtype == torch.bfloat16 else 4
     off = FFN_COUNTER_BYTES if dtype == torch.bfloat16 else 0
     return ws[off: off + M_cap * I * es].view(dtype).view(M_cap, I)
+
+
+# ---------------------------------------------------------------------------
+# The router's training step
+# ---------------------------------------------------------------------------
+def _mask_ptr(mask, T):
+    if mask is None:
+        return None
+    if mask.dtype == torch.bool:
+        mask = mask.view(torch.uint8)
+    if mask.numel() != T:
+        raise ValueError("mask must have one entry per token")
+    return _dev(mask, "mask", torch.uint8)
+
+
+def _groups(T, seq_len):
+    if seq_len < 0 or (seq_len > 0 and T % seq_len):
+        raise ValueError(f"the {T} tokens must be whole sequences of seq_len={seq_len}")
+    return T // seq_len if seq_len else 1
+
+
+def balance_ws_bytes(T, E, k, seq_len=0):
+    L = load_library()
+    n = ctypes.c_size_t(0)
+    st = L.moe_balance_loss(None, None, None, T, E, k, seq_len, None, None, None, None, ctypes.byref(n), None)
+    _check("moe_balance_loss", st)
+    return n.value
+
+
+def moe_balance_loss(logits, ids, mask=None, seq_len=0, ws=None, loss=None, counts=None, live=None):
+    """Balance loss and z loss of router logits [T, E] (fp32) with the selected ids
+    [T, k], and the per-expert counts. Groups of seq_len tokens (0: all of them) have
+    a balance loss each; mask [T] (bool or uint8, optional) marks live tokens.
+    Returns (loss [2] fp32, counts [groups, E] int32, live [groups + 2] int32, ws);
+    ws starts zero-filled and may serve further calls, one at a time."""
+    L = load_library()
+    T, E = logits.shape
+    k = ids.shape[1]
+    if ids.shape[0] != T:
+        raise ValueError("ids must be [T, k] for logits [T, E]")
+    G = _groups(T, seq_len)
+    need = balance_ws_bytes(T, E, k, seq_len)
+    dev = logits.device
+    if ws is None or ws.numel() < need:
+        ws = torch.zeros(need, dtype=torch.uint8, device=dev)
+    loss = torch.empty(2, dtype=torch.float32, device=dev) if loss is None else loss
+    counts = torch.empty((G, E), dtype=torch.int32, device=dev) if counts is None else counts
+    live = torch.empty(G + 2, dtype=torch.int32, device=dev) if live is None else live
+    if loss.numel() != 2 or tuple(counts.shape) != (G, E) or live.numel() != G + 2:
+        raise ValueError("loss must be [2], counts [groups, E] and live [groups + 2]")
+    n = ctypes.c_size_t(ws.numel())
+    st = L.moe_balance_loss(_dev(logits, "logits", torch.float32), _dev(ids, "ids", torch.int32), _mask_ptr(mask, T), T,
+                            E, k, seq_len, _dev(loss, "loss", torch.float32), _dev(counts, "counts", torch.int32),
+                            _dev(live, "live", torch.int32), _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
+    _check("moe_balance_loss", st)
+    return loss, counts, live, ws
+
+
+def moe_gate_backward(logits, ids, counts, live, dloss, weights=None, dweights=None, mask=None, seq_len=0, dlogits=None):
+    """Gradient to the router logits: of moe_balance_loss's two losses (dloss [2], on
+    the GPU; counts and live as it returned them) and, with dweights [T, k], of the
+    gate weights [T, k]. Returns dlogits [T, E]."""
+    L = load_library()
+    T, E = logits.shape
+    k = ids.shape[1]
+    G = _groups(T, seq_len)
+    if ids.shape[0] != T or tuple(counts.shape) != (G, E) or live.numel() != G + 2 or dloss.numel() != 2:
+        raise ValueError("ids must be [T, k], counts [groups, E], live [groups + 2] and dloss [2]")
+    if (weights is None) != (dweights is None):
+        raise ValueError("weights and dweights come together")
+    if weights is not None and (tuple(weights.shape) != (T, k) or tuple(dweights.shape) != (T, k)):
+        raise ValueError("weights and dweights must be [T, k]")
+    if dlogits is None:
+        dlogits = torch.empty((T, E), dtype=torch.float32, device=logits.device)
+    elif tuple(dlogits.shape) != (T, E):
+        raise ValueError("dlogits must be [T, E]")
+    st = L.moe_gate_backward(_dev(logits, "logits", torch.float32), _dev(ids, "ids", torch.int32), _mask_ptr(mask, T),
+                             _dev(counts, "counts", torch.int32), _dev(live, "live", torch.int32),
+                             _dev(dloss, "dloss", torch.float32), _ptr_or_null(weights, "weights", torch.float32),
+                             _ptr_or_null(dweights, "dweights", torch.float32), T, E, k, seq_len,
+                             _dev(dlogits, "dlogits", torch.float32), _stream())
+    _check("moe_gate_backward", st)
+    return dlogits
+
+
+def moe_combine_backward(dout, y_perm, weights, dest, dweights=None, dy_perm=None, need_dy=True):
+    """Gradient of moe_unpermute_combine. Returns (dweights [T, k] fp32, dy_perm [M_cap, H]
+    or None with need_dy=False); rows of dy_perm that no entry of dest names are left alone."""
+    L = load_library()
+    T, H = dout.shape
+    M_cap, k = y_perm.shape[0], weights.shape[1]
+    if tuple(weights.shape) != (T, k) or dest.numel() != T * k or y_perm.shape[1] != H:
+        raise ValueError("weights must be [T, k], dest [T * k] and y_perm [M_cap, H] for dout [T, H]")
+    if dweights is None:
+        dweights = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+    elif tuple(dweights.shape) != (T, k):
+        raise ValueError("dweights must be [T, k]")
+    if not need_dy:
+        dy_perm = None
+    elif dy_perm is None:
+        dy_perm = torch.empty_like(y_perm)
+    elif tuple(dy_perm.shape) != (M_cap, H):
+        raise ValueError("dy_perm must be [M_cap, H]")
+    st = L.moe_combine_backward(_dev(dout, "dout"), _dev(y_perm, "y_perm", dout.dtype),
+                                _dev(weights, "weights", torch.float32), _dev(dest, "dest", torch.int32), T, k, H, M_cap,
+                                _dtype_code(dout), _dev(dweights, "dweights", torch.float32),
+                                _ptr_or_null(dy_perm, "dy_perm", dout.dtype), _stream())
+    _check("moe_combine_backward", st)
+    return dweights, dy_perm
+
+
+def router_grad_ws_bytes(T, E, H, dtype):
+    L = load_library()
+    n = ctypes.c_size_t(0)
+    dt = MOE_BF16 if dtype == torch.bfloat16 else MOE_F32
+    st = L.moe_router_grad(None, None, None, T, E, H, dt, None, None, None, None, ctypes.byref(n), None)
+    _check("moe_router_grad", st)
+    return n.value
+
+
+def moe_router_grad(dlogits, x, w_router, dx=None, dw=None, dbias=None, ws=None, need_dx=True):
+    """Gradient of logits = x W^T + bias. Returns (dx [T, H] of x's type or None with
+    need_dx=False, dw [E, H] fp32, dbias [E] fp32, ws)."""
+    L = load_library()
+    T, H = x.shape
+    E = w_router.shape[0]
+    if w_router.dtype != x.dtype or tuple(w_router.shape) != (E, H) or tuple(dlogits.shape) != (T, E):
+        raise ValueError("w_router must be [E, H] with the dtype of x, and dlogits [T, E]")
+    dt = _dtype_code(x)
+    dev = x.device
+    need = router_grad_ws_bytes(T, E, H, x.dtype)
+    if ws is None or ws.numel() < need:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty_like(x)
+    elif tuple(dx.shape) != (T, H):
+        raise ValueError("dx must be [T, H]")
+    dw = torch.empty((E, H), dtype=torch.float32, device=dev) if dw is None else dw
+    dbias = torch.empty(E, dtype=torch.float32, device=dev) if dbias is None else dbias
+    if tuple(dw.shape) != (E, H) or dbias.numel() != E:
+        raise ValueError("dw must be [E, H] and dbias [E]")
+    n = ctypes.c_size_t(ws.numel())
+    st = L.moe_router_grad(_dev(dlogits, "dlogits", torch.float32), _dev(x, "x"), _dev(w_router, "w_router"), T, E, H, dt,
+                           _ptr_or_null(dx, "dx", x.dtype), _dev(dw, "dw", torch.float32),
+                           _dev(dbias, "dbias", torch.float32), _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
+    _check("moe_router_grad", st)
+    return dx, dw, dbias, ws
 
 
 # ---------------------------------------------------------------------------

@@ -87,6 +87,22 @@ hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weigh
                           const int32_t* offsets, int E_local, int H, int I, int M_cap, void* y_perm, void* ws,
                           hipStream_t s, int rows);
 
+// The router's training step (train_kernels.hip, router_grad_kernels.hip).
+// n: tokens of a group of the balance loss (T a multiple of it, n > 0)
+long long balance_blocks(int T, int E, int n);
+size_t balance_ws_bytes(int T, int E, int k, int n);
+hipError_t launch_balance_empty(int groups, int E, float* loss, int32_t* counts, int32_t* live, hipStream_t s);
+hipError_t launch_balance_loss(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n,
+                               float* loss, int32_t* counts, int32_t* live, void* ws, hipStream_t s);
+hipError_t launch_gate_backward(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n,
+                                const int32_t* counts, const int32_t* live, const float* dloss, const float* w,
+                                const float* dw, float* dz, hipStream_t s);
+hipError_t launch_combine_backward(const void* dout, const void* y, const float* w, const int32_t* dest, int T, int k,
+                                   int H, int M_cap, bool bf16, float* dw, void* dy, hipStream_t s);
+size_t router_grad_ws_bytes(int T, int E, int H, bool bf16);
+hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int T, int E, int H, bool bf16, void* dx,
+                              float* dw, float* db, void* ws, hipStream_t s);
+
 // The result of the check that block b of a launch runs on XCD b % 8, for a
 // launch on stream s, or nullptr (ffn_kernels.hip).
 const int32_t* xcd_state(hipStream_t s);

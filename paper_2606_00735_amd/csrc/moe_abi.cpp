@@ -609,6 +609,93 @@ moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs, con
                                         {wdq, wds, ld_dn}, offsets, E_local, H, I, M_cap, y_perm, ws, stream, rows));
 }
 
+// ---------------------------------------------------------------------------
+// The router's training step
+// ---------------------------------------------------------------------------
+// Tokens of a group of the balance loss: seq_len, or all of them.
+static moe_status balance_shape_ok(int T, int E, int k, int seq_len, int* n) {
+  const moe_status st = check_tk(T, k, E);
+  if (st != MOE_OK) return st;
+  if (seq_len < 0 || (seq_len > 0 && T % seq_len != 0)) return MOE_ERR_INVALID_ARG;
+  if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  *n = seq_len > 0 ? seq_len : T;
+  // blocks of a launch
+  if (moe::balance_blocks(T, E, *n) > (1LL << 23)) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+moe_status moe_balance_loss(const float* logits, const int32_t* topk_ids, const uint8_t* mask, int T, int E, int k,
+                            int seq_len, float* loss, int32_t* counts, int32_t* live, void* ws, size_t* ws_bytes,
+                            hipStream_t stream) {
+  int n = 0;
+  const moe_status st = balance_shape_ok(T, E, k, seq_len, &n);
+  if (st != MOE_OK) return st;
+  if (ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  const size_t need = moe::balance_ws_bytes(T, E, k, n);
+  if (ws == nullptr) {
+    *ws_bytes = need;
+    return MOE_OK;
+  }
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (!loss || !live || !aligned4(loss) || !aligned4(live) || !aligned16(ws)) return MOE_ERR_INVALID_ARG;
+  const int groups = seq_len > 0 ? T / seq_len : 1;
+  if (groups > 0 && (!counts || !aligned4(counts))) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return hip_status(moe::launch_balance_empty(groups, E, loss, counts, live, stream));
+  if (!logits || !topk_ids || !aligned16(logits) || !aligned4(topk_ids)) return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_balance_loss(logits, topk_ids, mask, T, E, k, n, loss, counts, live, ws, stream));
+}
+
+moe_status moe_gate_backward(const float* logits, const int32_t* topk_ids, const uint8_t* mask, const int32_t* counts,
+                             const int32_t* live, const float* dloss, const float* topk_w, const float* dtopk_w, int T,
+                             int E, int k, int seq_len, float* dlogits, hipStream_t stream) {
+  int n = 0;
+  const moe_status st = balance_shape_ok(T, E, k, seq_len, &n);
+  if (st != MOE_OK) return st;
+  if ((topk_w == nullptr) != (dtopk_w == nullptr)) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return MOE_OK;
+  if (!logits || !topk_ids || !counts || !live || !dloss || !dlogits) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(logits) || !aligned16(dlogits) || !aligned4(topk_ids) || !aligned4(counts) || !aligned4(live) ||
+      !aligned4(dloss) || !aligned4(topk_w) || !aligned4(dtopk_w))
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_gate_backward(logits, topk_ids, mask, T, E, k, n, counts, live, dloss, topk_w, dtopk_w,
+                                              dlogits, stream));
+}
+
+moe_status moe_combine_backward(const void* dout, const void* y_perm, const float* topk_w, const int32_t* dest, int T,
+                                int k, int H, int M_cap, moe_dtype dt, float* dtopk_w, void* dy_perm,
+                                hipStream_t stream) {
+  if (T < 0 || k < 1 || k > MOE_MAX_TOPK || H < 1 || M_cap < 0 || !valid_dtype(dt)) return MOE_ERR_INVALID_ARG;
+  if ((long long)T * k > INT_MAX) return MOE_ERR_UNSUPPORTED;
+  if (H % (dt == MOE_BF16 ? 8 : 4) != 0) return MOE_ERR_INVALID_ARG;
+  if (T == 0) return MOE_OK;
+  if (!dout || !topk_w || !dest || !dtopk_w || (M_cap > 0 && !y_perm)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(dout) || !aligned16(y_perm) || !aligned16(dy_perm) || !aligned4(topk_w) || !aligned4(dest) ||
+      !aligned4(dtopk_w))
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_combine_backward(dout, y_perm, topk_w, dest, T, k, H, M_cap, dt == MOE_BF16, dtopk_w,
+                                                 dy_perm, stream));
+}
+
+moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_router, int T, int E, int H,
+                           moe_dtype dt, void* dx, float* dw_router, float* dbias, void* ws, size_t* ws_bytes,
+                           hipStream_t stream) {
+  if (!valid_dtype(dt) || T < 0 || E < 1 || E > MOE_MAX_EXPERTS || H < 1 || H % 8 != 0) return MOE_ERR_INVALID_ARG;
+  if (dt == MOE_BF16 && H % 64 != 0) return MOE_ERR_UNSUPPORTED;
+  if (H > (1 << 20) || (long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  if (ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  const size_t need = moe::router_grad_ws_bytes(T, E, H, dt == MOE_BF16);
+  if (ws == nullptr) {
+    *ws_bytes = need;
+    return MOE_OK;
+  }
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (!dw_router || !dbias || !aligned16(dw_router) || !aligned4(dbias) || !aligned16(ws)) return MOE_ERR_INVALID_ARG;
+  if (T > 0 && (!dlogits || !x || !w_router)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(dlogits) || !aligned16(x) || !aligned16(w_router) || !aligned16(dx)) return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_router_grad(dlogits, x, w_router, T, E, H, dt == MOE_BF16, dx, dw_router, dbias, ws,
+                                            stream));
+}
+
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
