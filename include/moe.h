@@ -583,10 +583,10 @@ moe_status moe_load_sweep_mx(const uint8_t* xq, const uint32_t* xs, const uint8_
  * counts   [groups, E] int32
  * live     [groups + 2] int32: n_s, then the sum of all, then the number of
  *          groups with live tokens
- * ws       must be zero before the first call on it (every call leaves it zero,
- *          so calls of any sizes can share one); such calls must not overlap
+ * ws       its first 256 bytes must be zero before the first call on it (every call
+ *          leaves them zero); calls that share one, of any sizes, must not overlap
  * Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), T a multiple of seq_len, T * E <=
- * 2^40 and at most 2^23 blocks of up to 2048 / E tokens (at least 32) of a group.
+ * 2^40 and at most 2^23 blocks of 16 tokens or more of a group.
  * Sums are fp32 within a block, joined in fp64 in a fixed order: results do not
  * depend on timing.
  */
@@ -634,7 +634,7 @@ moe_status moe_combine_backward(const void* dout, const void* y_perm, const floa
  * dw_router [E, H] fp32        dlogits^T x
  * dbias     [E]    fp32        sum_t dlogits[t,:]
  * dlogits [T, E] fp32; x [T, H], w_router [E, H] dt. bf16: dlogits enters the MFMA
- * as the sum of two bf16 terms (17 significant bits), sums are fp32. T == 0 writes
+ * as a sum of bf16 terms, all 24 bits of it for dw_router and 16 for dx; sums are fp32. T == 0 writes
  * zeros to dw_router and dbias. ws holds partial sums over ranges of tokens, added
  * in order (results do not depend on timing); its size depends on the device's
  * compute units. Limits: 1 <= E <= 256, H % 8 == 0 (bf16: H % 64 == 0), H <= 2^20.

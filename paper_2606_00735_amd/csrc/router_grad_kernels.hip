@@ -1,12 +1,12 @@
 // Gradient of the router's product z = x W^T + b (gfx950): dx = dz W, dW = dz^T x,
 // db = sum_t dz.
 //
-// dz is fp32, x and W bf16, and the MFMA takes bf16 pairs: dz is split into two
-// bf16 terms, hi = bf16(dz) and lo = bf16(dz - hi), each multiplied with the exact
-// other operand and summed in fp32. What is dropped is at most 2^-18 of an element
-// of dz, 1e-6 of a result's norm. Both reductions run along a dimension that is a row index of
-// the bf16 operand (tokens of x, experts of W), so its fragments are read from LDS
-// with the transposing read.
+// dz is fp32, x and W bf16, and the MFMA takes bf16 pairs: dz is cut into bf16
+// terms, each multiplied with the exact other operand and summed in fp32. For dW,
+// fp32 like the sums, three terms hold all 24 bits of an element; for dx, rounded
+// to bf16, two are enough (they drop 2^-16 of an element). Both reductions run
+// along a dimension that is a row index of the bf16 operand (tokens of x, experts
+// of W), so its fragments are read from LDS with the transposing read.
 #include <algorithm>
 #include <type_traits>
 
@@ -17,6 +17,7 @@
 namespace moe {
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // Fragment of 32 columns x 16 rows of a bf16 tile in LDS with 256-byte rows, for
 // an operand whose reduction dimension is the tile's row: lane (c = lane % 32, h =
@@ -40,25 +41,34 @@ __device__ __forceinline__ bf16x8_t tr_frag(const char* tile, int lane, int k0, 
   return __builtin_bit_cast(bf16x8_t, v);
 }
 
-// Eight fp32 values as hi + lo bf16 fragments.
-__device__ __forceinline__ void split8(const float (&f)[8], bf16x8_t& hi, bf16x8_t& lo) {
-  uint32_t h[4], l[4];
+// Eight fp32 values as N bf16 fragments, f = sum of frag[n] up to the bits past the
+// N-th: each takes the upper 16 bits of what is left (the differences are exact), so
+// three hold every value.
+template <int N>
+__device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&frag)[N]) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    h[q] = pack_bf16x2(f[2 * q], f[2 * q + 1]);
-    l[q] = pack_bf16x2(f[2 * q] - __uint_as_float(h[q] << 16), f[2 * q + 1] - __uint_as_float(h[q] & 0xffff0000u));
+  for (int n = 0; n < N; ++n) {
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      w[q] = __builtin_amdgcn_perm(__float_as_uint(f[2 * q + 1]), __float_as_uint(f[2 * q]), 0x07060302u);
+    frag[n] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+    if (n + 1 < N)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] -= __uint_as_float(__float_as_uint(f[q]) & 0xffff0000u);
   }
-  hi = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
-  lo = as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]));
 }
 
 // ---------------------------------------------------------------------------
 // dW and db: a block sums E x 128 columns of x over its range of tokens, 32 at a
 // time: the chunk's dz rows (fp32) and x rows (128 columns) go to LDS by direct
-// loads, NS stages deep; a wave holds (EP / 2) x 64 of the tile. Each wave splits
-// the dz values of its experts as it reads them (lanes across experts: a row of
-// LDS is read without conflicts). Experts past E are computed from other rows'
-// values and not stored.
+// loads, NS stages deep. A wave holds 32 experts by all 128 columns (EP = 256), so
+// every dz value is cut into its terms once, by the wave that owns its expert, as
+// it is read (lanes across experts: a row of LDS is read without conflicts). Two
+// waves on a SIMD: one's MFMAs run while the other cuts.
+// Experts past E are computed from other rows' values and not stored. Blocks of one
+// token range follow each other by the number of ranges, so that (for 2, 4 or 8 of
+// them) an XCD works on one or a few ranges and reads their dz from its L2.
 // ---------------------------------------------------------------------------
 constexpr int kRgTok = 32;    // tokens of a chunk
 constexpr int kRgCols = 128;  // columns of x of a block
@@ -84,14 +94,17 @@ struct RgStage {
 
 // VEC: E % 4 == 0, dz rows are whole 16-byte pieces.
 template <int EP, bool VEC>
-__global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
+__global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
   using St = RgStage<EP>;
-  constexpr int MI = EP / 64, NJ = 2;  // 32-row blocks of experts, of columns per wave
+  constexpr int W = 8, WE = EP / 32, WC = W / WE;       // waves along experts, columns
+  constexpr int MI = 1, NJ = kRgCols / (32 * WC);       // 32 x 32 blocks of a wave
+  constexpr int WCOLS = kRgCols / WC;
   __shared__ __align__(16) bf16_t smem[St::BYTES * St::NS / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave >> 1, wn = wave & 1, r32 = lane & 31, h = lane >> 5;
+  const int wm = wave / WC, wn = wave % WC, r32 = lane & 31, h = lane >> 5;
   const int E = a.E, H = a.H;
-  const int c0 = (int)blockIdx.x * kRgCols, sp = (int)blockIdx.y;
+  const int sp = (int)(blockIdx.x % (unsigned)a.S), tile = (int)(blockIdx.x / (unsigned)a.S);
+  const int c0 = tile * kRgCols;
   const int chunks = (a.T + kRgTok - 1) / kRgTok;
   const int q0 = uniform_int((int)((long long)sp * chunks / a.S));
   const int q1 = uniform_int((int)((long long)(sp + 1) * chunks / a.S));
@@ -99,17 +112,17 @@ __global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
   // Direct loads. dz: 1 KB of a stage per instruction, 16 bytes a lane (VEC) or 256
   // bytes, 4 a lane; columns past E read the row's last ones. x: 4 rows of 256
   // bytes; columns past H read the row's last ones.
-  constexpr int DL = VEC ? 16 : 4, ND = St::DZ / (64 * DL * 4), NX = kRgTok * kRgCols * 2 / 4096;
+  constexpr int DL = VEC ? 16 : 4, ND = St::DZ / (64 * DL * W), NX = kRgTok * kRgCols * 2 / (1024 * W);
   constexpr int LOADS = ND + NX;
   auto issue = [&](int q, bool live, bf16_t* st, int) {
     const int t0 = (live ? q0 + q : q1 - 1) * kRgTok;
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int byte = ((i * 4 + wave) * 64 + lane) * DL;
+      const int byte = ((i * W + wave) * 64 + lane) * DL;
       const int row = byte / (EP * 4), e = min((byte % (EP * 4)) / 4, E - DL / 4);
       const int t = min(t0 + row, a.T - 1);
       const float* p = a.dz + (size_t)t * E + e;
-      const bf16_t* dst = st + (i * 4 + wave) * 64 * DL / 2;
+      const bf16_t* dst = st + (i * W + wave) * 64 * DL / 2;
       if (VEC)
         dma16(p, dst);
       else
@@ -117,10 +130,10 @@ __global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
-      const int row = (i * 4 + wave) * 4 + lane / 16, t = min(t0 + row, a.T - 1);
+      const int row = (i * W + wave) * 4 + lane / 16, t = min(t0 + row, a.T - 1);
       const int c = min(c0 + tr_swizzle(row, lane % 16) * 8, H - 8);
       const bf16_t* p = a.x + (size_t)t * H + c;
-      dma16(p, st + (St::DZ + (i * 4 + wave) * 1024) / 2);
+      dma16(p, st + (St::DZ + (i * W + wave) * 1024) / 2);
     }
   };
 
@@ -138,8 +151,8 @@ __global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
     const int left = a.T - q * kRgTok;  // tokens of this chunk
     if (left < kRgTok) {
       // past the last token: zeros, so that they add nothing
-      for (int i = left * EP + threadIdx.x; i < kRgTok * EP; i += 256) reinterpret_cast<float*>(base)[i] = 0.0f;
-      for (int i = left * 64 + threadIdx.x; i < kRgTok * 64; i += 256)
+      for (int i = left * EP + threadIdx.x; i < kRgTok * EP; i += W * kWave) reinterpret_cast<float*>(base)[i] = 0.0f;
+      for (int i = left * 64 + threadIdx.x; i < kRgTok * 64; i += W * kWave)
         reinterpret_cast<uint32_t*>(base + St::DZ)[i] = 0;
       wait_lgkmcnt0();
       lds_barrier();
@@ -150,21 +163,21 @@ __global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
     for (int s = 0; s < kRgTok / 16; ++s) {
       bf16x8_t xf[NJ];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) xf[j] = tr_frag(base + St::DZ, lane, 16 * s, wn * 64 + j * 32);
+      for (int j = 0; j < NJ; ++j) xf[j] = tr_frag(base + St::DZ, lane, 16 * s, wn * WCOLS + j * 32);
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         float f[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = dz[(16 * s + 8 * h + k) * EP + wm * (EP / 2) + i * 32 + r32];
-        bf16x8_t hi, lo;
-        split8(f, hi, lo);
+        for (int k = 0; k < 8; ++k) f[k] = dz[(16 * s + 8 * h + k) * EP + (wm * MI + i) * 32 + r32];
+        if (tile == 0)
+          db[i] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        bf16x8_t zf[3];
+        split8<3>(f, zf);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) db[i] += f[k];
+        for (int n = 0; n < 3; ++n)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          acc[0][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[j], hi, acc[0][i][j], 0, 0, 0);
-          acc[0][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[j], lo, acc[0][i][j], 0, 0, 0);
-        }
+          for (int j = 0; j < NJ; ++j)
+            acc[0][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[j], zf[n], acc[0][i][j], 0, 0, 0);
       }
     }
     wait_lgkmcnt0();  // every read of this stage returned before it is refilled
@@ -172,18 +185,27 @@ __global__ __launch_bounds__(256) void router_dw_kernel(RouterGradArgs a) {
   pipeline<St::NS, LOADS>(
       q1 - q0, smem, St::BYTES / 2, [&](int c, bool live, bf16_t* st) { issue(c, live, st, 0); }, compute);
 
-  if (blockIdx.x == 0 && wn == 0) {
+  if (tile == 0 && wn == 0) {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const float s = db[i] + __shfl_xor(db[i], 32, kWave);
-      const int e = wm * (EP / 2) + i * 32 + r32;
+      const int e = (wm * MI + i) * 32 + r32;
       if (h == 0 && e < E) a.db[(size_t)sp * E + e] = s;
     }
   }
-  // rows of the tile are experts; a wave whose 64 columns lie past H stores none
-  const int m_end = c0 + wn * 64 < H ? E : 0;
-  split_epilogue<MI, NJ, 1, EP / 2, 64>(acc, smem, 0, m_end, 0, H, wm, wn, wave, lane,
-                                        a.dw + (size_t)sp * E * H + c0, 0, false);
+  // rows of the tile are experts; columns past H (64 of the last tile's: H % 64 ==
+  // 0) are not stored. At most 64 columns of a wave at a time go through LDS.
+  constexpr int NE = NJ < 2 ? NJ : 2, EC = NE * 32;
+  static_assert(W * 32 * EC * 4 <= St::BYTES * St::NS, "the epilogue's LDS");
+#pragma unroll
+  for (int j0 = 0; j0 < NJ; j0 += NE) {
+    f32x16_t part[1][MI][NE];
+#pragma unroll
+    for (int j = 0; j < NE; ++j) part[0][0][j] = acc[0][0][j0 + j];
+    const int c = c0 + wn * WCOLS + j0 * 32;
+    split_epilogue<MI, NE, 1, MI * 32, EC>(part, smem, 0, c < H ? E : 0, c, H, wm, 0, wave, lane,
+                                           a.dw + (size_t)sp * E * H, 0, false);
+  }
 }
 
 // Sums the S partial sums in order.
@@ -201,27 +223,31 @@ __global__ __launch_bounds__(256) void router_dw_reduce_kernel(const float* __re
 }
 
 // ---------------------------------------------------------------------------
-// dx: a wave keeps the dz rows of its 32 tokens, split, in registers (EP / 16
-// fragments of either term) and multiplies them with the columns of W that its
-// block walks, 128 at a time; W comes to LDS in pieces of 64 experts x 128 columns
-// by direct loads, one stage per piece of a column tile.
+// dx: a wave keeps the dz rows of its 32 tokens, in two terms, in registers (EP / 16
+// fragments of either) and multiplies them with the columns of W that its block
+// walks, 128 at a time; W comes to LDS in pieces of 64 experts x 128 columns by
+// direct loads, NS pieces in a ring. Fragments of W are read one 16-expert step
+// ahead of the MFMAs. Blocks that walk the same columns follow each other by the
+// number of column ranges, so that (for 2, 4 or 8 of them) an XCD's L2 holds one or
+// a few ranges of W.
 // ---------------------------------------------------------------------------
 constexpr int kDxRows = 128;
 
 template <int EP, bool VEC>
-__global__ __launch_bounds__(256) void router_dx_kernel(RouterGradArgs a, int tiles, int col_split) {
+__global__ __launch_bounds__(256, 2) void router_dx_kernel(RouterGradArgs a, int tiles, int col_split) {
   constexpr int KC = EP / 64;                // pieces of a column tile
-  constexpr int NS = KC < 2 ? 2 : KC;        // stages
+  constexpr int NS = 4;                      // pieces in the ring
   constexpr int STAGE = 64 * kRgCols;        // bf16
   constexpr int OUTB = 32 * 128;             // bytes of a wave's output rows, 64 columns at a time
   __shared__ __align__(16) bf16_t smem[NS * STAGE + 4 * OUTB / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, h = lane >> 5;
   const int E = a.E, H = a.H;
-  const int row0 = (int)blockIdx.x * kDxRows + wave * 32;
-  const int tl0 = uniform_int((int)blockIdx.y * tiles / col_split);
-  const int tl1 = uniform_int(((int)blockIdx.y + 1) * tiles / col_split);
-  bf16x8_t hi[EP / 16], lo[EP / 16];
+  const int part = (int)(blockIdx.x % (unsigned)col_split);
+  const int row0 = uniform_int((int)(blockIdx.x / (unsigned)col_split) * kDxRows + wave * 32);
+  const int tl0 = uniform_int(part * tiles / col_split);
+  const int tl1 = uniform_int((part + 1) * tiles / col_split);
+  bf16x8_t zf[EP / 16][2];
   {
     const float* p = a.dz + (size_t)min(row0 + r32, a.T - 1) * E;
 #pragma unroll
@@ -236,25 +262,28 @@ __global__ __launch_bounds__(256) void router_dx_kernel(RouterGradArgs a, int ti
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = e + k < E ? p[e + k] : 0.0f;
       }
-      split8(f, hi[s], lo[s]);
+      split8<2>(f, zf[s]);
     }
   }
   // piece kc of column tile tl; 16 KB, 4 instructions a wave; rows past E read the last
   const int n = (tl1 - tl0) * KC;
-  auto issue = [&](int q, int stage) {
+  auto issue = [&](int q) {
     const int qq = q < n ? q : n - 1;
     const int tl = tl0 + qq / KC, kc = qq % KC;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = (i * 4 + wave) * 4 + lane / 16, e = min(kc * 64 + row, E - 1);
       const int c = min(tl * kRgCols + tr_swizzle(row, lane % 16) * 8, H - 8);
-      dma16(a.w + (size_t)e * H + c, smem + stage * STAGE + (i * 4 + wave) * 512);
+      dma16(a.w + (size_t)e * H + c, smem + (q % NS) * STAGE + (i * 4 + wave) * 512);
     }
   };
   wait_vmcnt<0>();
 #pragma unroll
-  for (int q = 0; q < NS - 1; ++q) issue(q, q);
+  for (int q = 0; q < NS - 1; ++q) issue(q);
   char* out = reinterpret_cast<char*>(smem + NS * STAGE) + wave * OUTB;
+  // Stores of the tile before that were issued between the loads that a wait
+  // counts: loads and stores leave the counter in the order of their issue.
+  bool stored = false;
   for (int tl = tl0; tl < tl1; ++tl) {
     f32x16_t acc[4];
 #pragma unroll
@@ -262,23 +291,34 @@ __global__ __launch_bounds__(256) void router_dx_kernel(RouterGradArgs a, int ti
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       const int q = (tl - tl0) * KC + kc;
-      const int st = KC < 2 ? q & 1 : kc;
       wait_lgkmcnt0();  // this wave's reads of the piece before returned
-      wait_vmcnt<4 * (NS - 2)>();
+      // piece q landed; younger are two pieces and, for the first three of a tile,
+      // the eight stores of the tile before
+      if (kc < 3 && stored)
+        wait_vmcnt<4 * (NS - 2) + 8>();
+      else
+        wait_vmcnt<4 * (NS - 2)>();
       lds_barrier();
-      issue(q + NS - 1, KC < 2 ? (q + 1) & 1 : (kc + NS - 1) % NS);
-      const char* base = reinterpret_cast<const char*>(smem + st * STAGE);
+      issue(q + NS - 1);
+      const char* base = reinterpret_cast<const char*>(smem + (q % NS) * STAGE);
+      bf16x8_t wf[2][4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int j = 0; j < 4; ++j) wf[0][j] = tr_frag(base, lane, 0, j * 32);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x8_t wf = tr_frag(base, lane, 16 * s, j * 32);
-          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, hi[kc * 4 + s], acc[j], 0, 0, 0);
-          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, lo[kc * 4 + s], acc[j], 0, 0, 0);
-        }
+      for (int s = 0; s < 4; ++s) {
+        if (s + 1 < 4)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wf[(s + 1) & 1][j] = tr_frag(base, lane, 16 * (s + 1), j * 32);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[s & 1][j], zf[kc * 4 + s][t], acc[j], 0, 0, 0);
+      }
     }
     // lane (r, h) holds columns 8 g + 4 h + (0..3) of each 32 of its token: to whole
     // rows of 64 columns through the wave's LDS
+    const bool whole = row0 + 32 <= a.T && (tl + 1) * kRgCols <= H;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       auto at = [](int r, int piece) { return r * 128 + ((piece ^ (r & 7)) * 16); };
@@ -292,21 +332,27 @@ __global__ __launch_bounds__(256) void router_dx_kernel(RouterGradArgs a, int ti
         }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       const int col = tl * kRgCols + half * 64;
+      u32x4_t v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = i * 8 + lane / 8, p = lane % 8;
-        const uint4 v = *reinterpret_cast<const uint4*>(out + at(row, p));
-        if (row0 + row < a.T && col < H)
-          *reinterpret_cast<uint4*>(a.dx + (size_t)(row0 + row) * H + col + p * 8) = v;
-      }
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u32x4_t*>(out + at(i * 8 + lane / 8, lane % 8));
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      bf16_t* p = a.dx + (size_t)(row0 + lane / 8) * H + col + lane % 8 * 8;
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4_t*>(p + (size_t)i * 8 * H) = v[i];
+      } else if (col < H) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (row0 + i * 8 + lane / 8 < a.T) *reinterpret_cast<u32x4_t*>(p + (size_t)i * 8 * H) = v[i];
+      }
     }
+    stored = whole;
   }
   wait_vmcnt<0>();
 }
 
 // ---------------------------------------------------------------------------
-// fp32 (small layers): plain sums, a thread per output.
+// fp32 (small layers): plain sums.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float* __restrict__ dz, const float* __restrict__ w,
                                                             int T, int E, int H, float* __restrict__ dx) {
@@ -320,29 +366,54 @@ __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float* __restr
   }
 }
 
-// thread: (token range sp, expert e, column c); column H is the bias
+// Blocks of 64 columns x 8 experts x one range of tokens: a thread sums its column
+// over every fourth token of the range (dz is the same in all lanes), and the four
+// sums of a column are joined in LDS.
 __global__ __launch_bounds__(256) void router_dw_f32_kernel(const float* __restrict__ dz, const float* __restrict__ x,
                                                             int T, int E, int H, int S, float* __restrict__ dw,
                                                             float* __restrict__ db) {
-  const size_t n = (size_t)S * E * (H + 1);
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-    const int c = (int)(i % (H + 1)), e = (int)(i / (H + 1) % E), sp = (int)(i / (H + 1) / E);
-    const int t0 = (int)((long long)sp * T / S), t1 = (int)((long long)(sp + 1) * T / S);
-    float s = 0.0f;
-    if (c < H) {
-      for (int t = t0; t < t1; ++t) s = fmaf(dz[(size_t)t * E + e], x[(size_t)t * H + c], s);
-      dw[((size_t)sp * E + e) * H + c] = s;
-    } else {
-      for (int t = t0; t < t1; ++t) s += dz[(size_t)t * E + e];
-      db[(size_t)sp * E + e] = s;
+  __shared__ float s_sum[4][9][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = (H + 63) / 64, eg = (E + 7) / 8;
+  const int tile = (int)(blockIdx.x % (unsigned)tiles), r = (int)(blockIdx.x / (unsigned)tiles);
+  const int e0 = r % eg * 8, sp = r / eg;
+  const int c = tile * 64 + lane;
+  const int t0 = (int)((long long)sp * T / S), t1 = (int)((long long)(sp + 1) * T / S);
+  float acc[8], sum[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) acc[q] = sum[q] = 0.0f;
+#pragma unroll 4
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const float xv = c < H ? x[(size_t)t * H + c] : 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float d = dz[(size_t)t * E + min(e0 + q, E - 1)];
+      acc[q] = fmaf(d, xv, acc[q]);
+      sum[q] += d;
     }
   }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) s_sum[wave][q][lane] = acc[q];
+  if (lane == 0)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s_sum[wave][8][q] = sum[q];
+  __syncthreads();
+  auto join = [&](int q, int l) { return (s_sum[0][q][l] + s_sum[1][q][l]) + (s_sum[2][q][l] + s_sum[3][q][l]); };
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int q = wave * 2 + i, e = e0 + q;
+    if (e < E && c < H) dw[((size_t)sp * E + e) * H + c] = join(q, lane);
+  }
+  if (tile == 0 && threadIdx.x < 8 && e0 + (int)threadIdx.x < E) db[(size_t)sp * E + e0 + threadIdx.x] = join(8, threadIdx.x);
 }
+
+// Blocks of router_dw_f32_kernel.
+static unsigned dw_f32_grid(int E, int H, int S) { return (unsigned)((H + 63) / 64 * ((E + 7) / 8) * S); }
 
 // Token ranges of dW: enough blocks for every CU, at least 64 tokens each.
 static int router_ranges(int T, int E, int H, bool bf16) {
   const int cus = device_cu_count();
-  const long long blocks = bf16 ? (H + kRgCols - 1) / kRgCols : ((long long)E * (H + 1) + 255) / 256;
+  const long long blocks = bf16 ? (H + kRgCols - 1) / kRgCols : dw_f32_grid(E, H, 1);
   const long long s = std::min(std::max(1LL, cus / blocks), std::max(1LL, T / 64LL));
   return (int)std::min(s, 64LL);
 }
@@ -359,7 +430,7 @@ hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int
   float* pb = S > 1 ? reinterpret_cast<float*>(static_cast<char*>(ws) + round256((size_t)S * E * H * 4)) : db;
   hipError_t e = hipSuccess;
   if (T == 0) {  // no tokens: dW and db are zero
-    router_dw_f32_kernel<<<(unsigned)(((size_t)E * (H + 1) + 255) / 256), 256, 0, s>>>(dz, nullptr, 0, E, H, 1, dw, db);
+    router_dw_f32_kernel<<<dw_f32_grid(E, H, 1), 256, 0, s>>>(dz, nullptr, 0, E, H, 1, dw, db);
     return hipGetLastError();
   }
   if (bf16) {
@@ -369,12 +440,12 @@ hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int
     auto run = [&](auto ep, auto vec) {
       constexpr int EP = decltype(ep)::value;
       constexpr bool VEC = decltype(vec)::value;
-      router_dw_kernel<EP, VEC><<<dim3((unsigned)tiles, (unsigned)S), 256, 0, s>>>(a);
+      router_dw_kernel<EP, VEC><<<(unsigned)(tiles * S), 512, 0, s>>>(a);
       e = hipGetLastError();
       if (e != hipSuccess || dx == nullptr) return;
       const int rows = (T + kDxRows - 1) / kDxRows;
       const int split = std::min(tiles, std::max(1, (2 * device_cu_count() + rows - 1) / rows));
-      router_dx_kernel<EP, VEC><<<dim3((unsigned)rows, (unsigned)split), 256, 0, s>>>(a, tiles, split);
+      router_dx_kernel<EP, VEC><<<(unsigned)(rows * split), 256, 0, s>>>(a, tiles, split);
       e = hipGetLastError();
     };
     auto by_vec = [&](auto ep) {
@@ -391,8 +462,7 @@ hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int
       by_vec(std::integral_constant<int, 256>());
   } else {
     auto grid = [](size_t n) { return (unsigned)std::min<size_t>((n + 255) / 256, 1u << 16); };
-    router_dw_f32_kernel<<<grid((size_t)S * E * (H + 1)), 256, 0, s>>>(dz, static_cast<const float*>(x), T, E, H, S,
-                                                                        pw, pb);
+    router_dw_f32_kernel<<<dw_f32_grid(E, H, S), 256, 0, s>>>(dz, static_cast<const float*>(x), T, E, H, S, pw, pb);
     e = hipGetLastError();
     if (e == hipSuccess && dx != nullptr) {
       router_dx_f32_kernel<<<grid((size_t)T * H), 256, 0, s>>>(dz, static_cast<const float*>(w), T, E, H,

@@ -45,10 +45,19 @@ __device__ __forceinline__ float group_max(float x) {
 // ---------------------------------------------------------------------------
 // Softmax rows of router logits. L lanes hold a token's row of E <= 4 L logits,
 // four consecutive experts each, so a wave works on 64 / L tokens at once and a
-// row is read as one run of 16-byte loads. A block of 4 waves takes kRowIters
-// rounds of them, all within one group (a sequence, or the whole batch).
+// row is read as one run of 16-byte loads. A block of W waves takes N rounds of
+// them, all within one group (a sequence, or the whole batch), with the loads of all
+// rounds in flight before the first is used. N is small: each launch fetches its code
+// from beyond the L2, and long unrolled code costs more than it hides.
+//
+// Exponentials and logarithms are the hardware's base-2 ones (1 ulp): with the
+// rounding of (z - max) log2 e, |z - max| 2^-24 relative in p.
 // ---------------------------------------------------------------------------
-constexpr int kRowIters = 8;
+static int lanes_of(int E) {
+  int L = 1;
+  while (4 * L < E) L *= 2;
+  return L;
+}
 
 struct RowArgs {
   const float* z;        // [T, E]
@@ -60,10 +69,10 @@ struct RowArgs {
 };
 
 // Four logits of a row, -inf past the last expert.
-__device__ __forceinline__ float4 load_logits(const float* row, int e0, int E, bool vec, bool live) {
+__device__ __forceinline__ float4 load_logits(const float* row, int e0, int E, bool vec, bool in) {
   const float ninf = -__builtin_huge_valf();
   float4 v = make_float4(ninf, ninf, ninf, ninf);
-  if (!live) return v;
+  if (!in) return v;
   if (vec) {
     if (e0 < E) v = *reinterpret_cast<const float4*>(row + e0);
   } else {
@@ -75,19 +84,51 @@ __device__ __forceinline__ float4 load_logits(const float* row, int e0, int E, b
   return v;
 }
 
+// The rows of a block: this lane's logits of every round, and whether the token
+// is there (in) and live (on). Masked rows are read as well, so that the loads
+// wait for nothing; what they hold is replaced by -inf.
+template <int L, int W, int N>
+struct Rows {
+  float4 v[N];
+  bool in[N], on[N];
+  size_t row[N];
+
+  // rounds [first, first + N) of block blk's `rounds`
+  __device__ __forceinline__ void load(const RowArgs& a, int g, int blk, int rounds, int first, int lane, int wave) {
+    constexpr int SLOTS = kWave / L;
+    const int e0 = (lane % L) * 4;
+    const bool vec = (a.E & 3) == 0;
+    uint8_t m[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int t = (blk * rounds + first + i) * W * SLOTS + wave * SLOTS + lane / L;
+      in[i] = t < a.n;
+      row[i] = (size_t)g * a.n + (in[i] ? t : 0);
+      v[i] = load_logits(a.z + row[i] * a.E, e0, a.E, vec, in[i]);
+      m[i] = a.mask != nullptr ? a.mask[row[i]] : 1;
+    }
+    const float ninf = -__builtin_huge_valf();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      on[i] = in[i] && m[i] != 0;
+      if (!on[i]) v[i] = make_float4(ninf, ninf, ninf, ninf);
+    }
+  }
+};
+
 // exp(z - max z) of the row in v, and 1 / sum and the logarithm of the sum of
 // exponentials. A row of -inf alone has no distribution: all three are 0.
 template <int L>
 __device__ __forceinline__ void row_softmax(float4& v, float& inv, float& lse) {
   const float top = group_max<L>(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
   // a NaN is not the maximum of a row, but makes its sum a NaN
-  const bool none = top == -__builtin_huge_valf();
-  const float m = none ? 0.0f : top;
-  v = make_float4(expf(v.x - m), expf(v.y - m), expf(v.z - m), expf(v.w - m));
+  const float m = top == -__builtin_huge_valf() ? 0.0f : top;
+  auto ex = [&](float z) { return __builtin_amdgcn_exp2f((z - m) * 1.4426950408889634f); };
+  v = make_float4(ex(v.x), ex(v.y), ex(v.z), ex(v.w));
   const float sum = group_sum<L>((v.x + v.y) + (v.z + v.w));
   const bool empty = sum == 0.0f;
-  inv = empty ? 0.0f : 1.0f / sum;
-  lse = empty ? 0.0f : m + logf(sum);
+  inv = empty ? 0.0f : __builtin_amdgcn_rcpf(sum);
+  lse = empty ? 0.0f : m + __builtin_amdgcn_logf(sum) * 0.6931471805599453f;
 }
 
 // ---------------------------------------------------------------------------
@@ -96,45 +137,64 @@ __device__ __forceinline__ void row_softmax(float4& v, float& inv, float& lse) {
 // so once the counts are known, one pass over the logits gives a number per
 // token, and no [E] sums have to be joined across blocks. The counts are integer
 // sums, the losses are joined by the last block in block order: results do not
-// depend on timing.
+// depend on timing. A group of at most kSelfIds ids is counted by each of its
+// blocks itself, which saves the counting launch; a larger one in up to kParts
+// parts first, whose counts each block adds up (no atomics: 8192 of them on 1024
+// counters took 9 us).
 //
-// ws: counts [groups][E], live tokens [groups] and a ticket, then two partial sums
-// per block. All of it is zero before and after a call, whatever the sizes, so
-// that calls of other sizes, whose parts lie elsewhere, can share it.
+// ws: a ticket, zero before and after a call (at the start, whatever the sizes), two
+// partial sums per block, the counts and live tokens of the parts.
 // ---------------------------------------------------------------------------
 struct LossWs {
-  int32_t* counts;
-  int32_t* live;
   int32_t* ticket;
-  float2* part;
+  uint64_t* part;   // [blocks]
+  int32_t* counts;  // [groups][parts][4 L]
+  int32_t* live;    // [groups][parts]
+  int parts;        // 0: a block counts its group itself
 };
 
-constexpr int kCountIds = 4096;  // ids that a counting block takes
+constexpr int kSelfIds = 4096;
+constexpr int kParts = 32;
 
-// Counts of a part of a group's ids: blocks (part, group).
-__global__ __launch_bounds__(256) void balance_count_kernel(RowArgs a, LossWs ws) {
+// Adds the ids of tokens [t0, t1) of group g that are live to cnt[E] and their
+// number to live (LDS), a token per thread.
+template <int THREADS>
+__device__ __forceinline__ void count_ids(const RowArgs& a, int g, int t0, int t1, int32_t* cnt, int32_t* live) {
+  constexpr int IDS = 8;  // ids of a token in flight
+  const int k = a.k;
+  int n = 0;
+  for (int t = t0 + (int)threadIdx.x; t < t1; t += THREADS) {
+    const size_t row = (size_t)g * a.n + t;
+    const uint8_t m = a.mask != nullptr ? a.mask[row] : 1;
+#pragma unroll 1
+    for (int j0 = 0; j0 < k; j0 += IDS) {
+      int e[IDS];
+#pragma unroll
+      for (int j = 0; j < IDS; ++j) e[j] = a.ids[row * k + min(j0 + j, k - 1)];
+#pragma unroll
+      for (int j = 0; j < IDS; ++j)
+        if (m != 0 && j0 + j < k && (unsigned)e[j] < (unsigned)a.E) atomicAdd(cnt + e[j], 1);
+    }
+    n += m != 0;
+  }
+  if (n > 0) atomicAdd(live, n);
+}
+
+// Counts of part blockIdx.x of a group's tokens.
+__global__ __launch_bounds__(256) void balance_count_kernel(RowArgs a, LossWs ws, int ep, int tok) {
   __shared__ int32_t s_cnt[kMaxExperts];
   __shared__ int32_t s_live;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, p = blockIdx.x;
+  const int t0 = min(p * tok, a.n), t1 = min(t0 + tok, a.n);  // p * tok < n + tok <= 2^31
   for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
-    for (int e = tid; e < a.E; e += 256) s_cnt[e] = 0;
+    s_cnt[tid] = 0;
     if (tid == 0) s_live = 0;
     __syncthreads();
-    const int tok = kCountIds / a.k;  // tokens of a part
-    const int t0 = blockIdx.x * tok, t1 = min(t0 + tok, a.n);
-    for (int t = t0 + tid; t < t1; t += 256) {
-      const size_t row = (size_t)g * a.n + t;
-      if (a.mask != nullptr && a.mask[row] == 0) continue;
-      atomicAdd(&s_live, 1);
-      for (int j = 0; j < a.k; ++j) {
-        const int e = a.ids[row * a.k + j];
-        if ((unsigned)e < (unsigned)a.E) atomicAdd(&s_cnt[e], 1);
-      }
-    }
+    count_ids<256>(a, g, t0, t1, s_cnt, &s_live);
     __syncthreads();
-    for (int e = tid; e < a.E; e += 256)
-      if (s_cnt[e] != 0) atomicAdd(ws.counts + (size_t)g * a.E + e, s_cnt[e]);
-    if (tid == 0 && s_live != 0) atomicAdd(ws.live + g, s_live);
+    const size_t at = (size_t)g * ws.parts + p;
+    if (tid < ep) ws.counts[at * ep + tid] = s_cnt[tid];
+    if (tid == 0) ws.live[at] = s_live;
     __syncthreads();
   }
 }
@@ -144,121 +204,171 @@ __device__ __forceinline__ float group_factor(int E, int k, int live) {
   return live > 0 ? (float)((double)E / ((double)k * live * live)) : 0.0f;
 }
 
-template <int L>
-__global__ __launch_bounds__(256) void balance_loss_kernel(RowArgs a, LossWs ws, float* __restrict__ loss,
+constexpr int kLossWaves = 8, kLossRounds = 8;  // of a block; kLossFlight rounds in flight
+constexpr int kLossFlight = 4;
+
+template <int L, bool SELF>
+__global__ __launch_bounds__(kLossWaves* kWave) void balance_loss_kernel(RowArgs a, LossWs ws, float* __restrict__ loss,
                                                            int32_t* __restrict__ counts, int32_t* __restrict__ live) {
-  constexpr int SLOTS = kWave / L;
-  __shared__ float2 s_part[4];
+  constexpr int W = kLossWaves, N = kLossFlight, THREADS = W * kWave;
+  __shared__ float2 s_part[W];
   __shared__ int s_last;
+  __shared__ __align__(16) int32_t s_cnt[kMaxExperts];
+  __shared__ int32_t s_live;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = (int)(blockIdx.x / a.blocks), blk = (int)(blockIdx.x - (unsigned)g * a.blocks);
   const int e0 = (lane % L) * 4;
-  const bool vec = (a.E & 3) == 0;
-  const float factor = group_factor(a.E, a.k, ws.live[g]);
-  float c[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) c[q] = e0 + q < a.E ? (float)ws.counts[(size_t)g * a.E + e0 + q] : 0.0f;
-  float bal = 0.0f, zl = 0.0f;
-  float4 v[kRowIters];
-  bool on[kRowIters];
-#pragma unroll
-  for (int i = 0; i < kRowIters; ++i) {
-    const int t = (blk * kRowIters + i) * 4 * SLOTS + wave * SLOTS + lane / L;
-    const size_t row = (size_t)g * a.n + t;
-    on[i] = t < a.n && (a.mask == nullptr || a.mask[row] != 0);
-    v[i] = load_logits(a.z + row * a.E, e0, a.E, vec, on[i]);
+  Rows<L, W, N> r;
+  r.load(a, g, blk, kLossRounds, 0, lane, wave);
+  if (tid < kMaxExperts) s_cnt[tid] = 0;
+  if (tid == 0) s_live = 0;
+  __syncthreads();
+  if (SELF) {
+    count_ids<THREADS>(a, g, 0, a.n, s_cnt, &s_live);
+  } else {
+    // four counts of a part a thread at a time
+    const int4* parts = reinterpret_cast<const int4*>(ws.counts + (size_t)g * ws.parts * (4 * L));
+#pragma unroll 2
+    for (int i = tid; i < ws.parts * L; i += THREADS) {
+      const int4 q = parts[i];
+      int32_t* s = s_cnt + (i % L) * 4;
+      if (q.x) atomicAdd(s, q.x);
+      if (q.y) atomicAdd(s + 1, q.y);
+      if (q.z) atomicAdd(s + 2, q.z);
+      if (q.w) atomicAdd(s + 3, q.w);
+    }
+    if (tid < ws.parts) atomicAdd(&s_live, ws.live[(size_t)g * ws.parts + tid]);
   }
+  __syncthreads();
+  const int n_live = s_live;
+  const int4 n4 = *reinterpret_cast<const int4*>(s_cnt + e0);  // of this lane's experts
+  const float c[4] = {(float)n4.x, (float)n4.y, (float)n4.z, (float)n4.w};
+  if (blk == 0 && tid < L) {
+    int32_t* out = counts + (size_t)g * a.E + e0;
+    if (e0 < a.E) out[0] = n4.x;
+    if (e0 + 1 < a.E) out[1] = n4.y;
+    if (e0 + 2 < a.E) out[2] = n4.z;
+    if (e0 + 3 < a.E) out[3] = n4.w;
+    if (tid == 0) __hip_atomic_store(live + g, n_live, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  float bal = 0.0f, zl = 0.0f;
+#pragma unroll 1
+  for (int first = 0;;) {
 #pragma unroll
-  for (int i = 0; i < kRowIters; ++i) {
-    float inv, lse;
-    row_softmax<L>(v[i], inv, lse);
-    const float s = group_sum<L>((c[0] * v[i].x + c[1] * v[i].y) + (c[2] * v[i].z + c[3] * v[i].w)) * inv;
-    if (on[i] && lane % L == 0) bal += s, zl += lse * lse;
+    for (int i = 0; i < N; ++i) {
+      float4& v = r.v[i];
+      float inv, lse;
+      row_softmax<L>(v, inv, lse);
+      const float s = group_sum<L>((c[0] * v.x + c[1] * v.y) + (c[2] * v.z + c[3] * v.w)) * inv;
+      if (r.on[i] && lane % L == 0) bal += s, zl += lse * lse;
+    }
+    first += N;
+    if (first >= kLossRounds || (blk * kLossRounds + first) * W * (kWave / L) >= a.n) break;
+    r.load(a, g, blk, kLossRounds, first, lane, wave);
   }
   bal = group_sum<64>(bal);
   zl = group_sum<64>(zl);
   if (lane == 0) s_part[wave] = make_float2(bal, zl);
   __syncthreads();
-  if (tid == 0) {
-    float2 p = make_float2(0.0f, 0.0f);
-    for (int w = 0; w < 4; ++w) p.x += s_part[w].x, p.y += s_part[w].y;
-    // the block's part of its group's balance loss and of the z sum, in agent
-    // scope: the last block runs on any XCD
-    uint64_t u = (uint64_t)__float_as_uint(p.x * factor) | (uint64_t)__float_as_uint(p.y) << 32;
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(ws.part + blockIdx.x), u, __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-    s_last = __hip_atomic_fetch_add(ws.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!s_last) return;
-
-  // The last block: every other one has read the counts. It hands them out,
-  // clears them for the next call and joins the partial sums.
+  const float factor = group_factor(a.E, a.k, n_live);
   double sb = 0.0, sz = 0.0;
-  long long many = 0, full = 0;
-  for (size_t i = tid; i < gridDim.x; i += 256) {
-    const uint64_t u = __hip_atomic_load(reinterpret_cast<uint64_t*>(ws.part + i), __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_AGENT);
-    sb += (double)__uint_as_float((uint32_t)u), sz += (double)__uint_as_float((uint32_t)(u >> 32));
-    ws.part[i] = make_float2(0.0f, 0.0f);
-  }
-  for (size_t i = tid; i < (size_t)a.groups * a.E; i += 256) {
-    counts[i] = ws.counts[i];
-    ws.counts[i] = 0;
-  }
-  for (int i = tid; i < a.groups; i += 256) {
-    const int n = ws.live[i];
-    live[i] = n;
-    ws.live[i] = 0;
-    many += n, full += n > 0;
-  }
-  __shared__ double s_d[256][2];
-  __shared__ long long s_n[256][2];
-  s_d[tid][0] = sb, s_d[tid][1] = sz, s_n[tid][0] = many, s_n[tid][1] = full;
-  __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if (tid < w)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) s_d[tid][q] += s_d[tid + w][q], s_n[tid][q] += s_n[tid + w][q];
+  int many = 0, full = 0;  // at most T each
+  if (gridDim.x == 1) {    // nothing to join
+    if (tid != 0) return;
+    for (int w = 0; w < W; ++w) sb += s_part[w].x, sz += s_part[w].y;
+    sb *= factor, many = n_live, full = n_live > 0;
+  } else {
+    if (tid == 0) {
+      float2 p = make_float2(0.0f, 0.0f);
+      for (int w = 0; w < W; ++w) p.x += s_part[w].x, p.y += s_part[w].y;
+      // the block's part of its group's balance loss and of the z sum, written
+      // through to where the last block, on any XCD, reads it, and there before the
+      // ticket is drawn (no fence: that would write back the XCD's whole L2)
+      const uint64_t u = (uint64_t)__float_as_uint(p.x * factor) | (uint64_t)__float_as_uint(p.y) << 32;
+      __hip_atomic_store(ws.part + blockIdx.x, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      wait_vmcnt<0>();
+      s_last = __hip_atomic_fetch_add(ws.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    }
     __syncthreads();
+    if (!s_last) return;
+    // The last block joins the sums and puts the ticket back.
+    for (size_t i = tid; i < gridDim.x; i += THREADS) {
+      const uint64_t u = __hip_atomic_load(ws.part + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sb += (double)__uint_as_float((uint32_t)u), sz += (double)__uint_as_float((uint32_t)(u >> 32));
+    }
+    for (int i = tid; i < a.groups; i += THREADS) {
+      const int n = __hip_atomic_load(live + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      many += n, full += n > 0;
+    }
+    __shared__ double s_d[THREADS][2];
+    __shared__ int2 s_n[THREADS];
+    s_d[tid][0] = sb, s_d[tid][1] = sz, s_n[tid] = make_int2(many, full);
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int q = 1; q < W; ++q) {
+      sb += s_d[tid + 64 * q][0], sz += s_d[tid + 64 * q][1];
+      many += s_n[tid + 64 * q].x, full += s_n[tid + 64 * q].y;
+    }
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) {
+      sb += __shfl_xor(sb, w, kWave), sz += __shfl_xor(sz, w, kWave);
+      many += __shfl_xor(many, w, kWave), full += __shfl_xor(full, w, kWave);
+    }
+    if (tid == 0) *ws.ticket = 0;
   }
   if (tid == 0) {
-    many = s_n[0][0], full = s_n[0][1];
-    loss[0] = full > 0 ? (float)(s_d[0][0] / (double)full) : 0.0f;
-    loss[1] = many > 0 ? (float)(s_d[0][1] / (double)many) : 0.0f;
-    live[a.groups] = (int32_t)many;
-    live[a.groups + 1] = (int32_t)full;
-    *ws.ticket = 0;
+    loss[0] = full > 0 ? (float)(sb / (double)full) : 0.0f;
+    loss[1] = many > 0 ? (float)(sz / (double)many) : 0.0f;
+    live[a.groups] = many;
+    live[a.groups + 1] = full;
   }
 }
 
-static int lanes_of(int E) {
-  int L = 1;
-  while (4 * L < E) L *= 2;
-  return L;
-}
+// Tokens of a block of the two kernels that read the logits.
+static int loss_rows(int E) { return kLossWaves * kLossRounds * (kWave / lanes_of(E)); }
+static int gate_rows(int E);
 
 // n > 0 tokens a group
-static RowArgs row_args(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n) {
-  RowArgs a{z, ids, mask, T, E, k, n, T / n, 0};
-  const int per = kRowIters * 4 * (kWave / lanes_of(E));
-  a.blocks = (n + per - 1) / per;
-  return a;
+static RowArgs row_args(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n,
+                        int rows) {
+  return {z, ids, mask, T, E, k, n, T / n, (n - 1) / rows + 1};
 }
 
 static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 long long balance_blocks(int T, int E, int n) {
   if (T == 0) return 0;
-  const RowArgs a = row_args(nullptr, nullptr, nullptr, T, E, 1, n);
-  return (long long)a.groups * a.blocks;
+  const RowArgs a = row_args(nullptr, nullptr, nullptr, T, E, 1, n, gate_rows(E));
+  return (long long)a.groups * a.blocks;  // the loss has no more
+}
+
+// Parts that a group's ids are counted in; 0: by each block.
+static int count_parts(int n, int k) {
+  const long long ids = (long long)n * k;
+  return ids <= kSelfIds ? 0 : (int)std::min<long long>(kParts, (ids + 2047) / 2048);
+}
+
+static LossWs loss_ws(const RowArgs& a, void* base, size_t* bytes) {
+  LossWs ws;
+  char* w = static_cast<char*>(base);
+  ws.parts = count_parts(a.n, a.k);
+  ws.ticket = reinterpret_cast<int32_t*>(w);
+  size_t at = 256;
+  ws.part = reinterpret_cast<uint64_t*>(w + at);
+  at += round256((size_t)a.groups * a.blocks * 8);
+  ws.counts = reinterpret_cast<int32_t*>(w + at);
+  at += round256((size_t)a.groups * ws.parts * 4 * lanes_of(a.E) * 4);
+  ws.live = reinterpret_cast<int32_t*>(w + at);
+  at += round256((size_t)a.groups * ws.parts * 4);
+  *bytes = at;
+  return ws;
 }
 
 size_t balance_ws_bytes(int T, int E, int k, int n) {
-  if (T == 0) return 256;
-  const RowArgs a = row_args(nullptr, nullptr, nullptr, T, E, k, n);
-  return round256((size_t)a.groups * E * 4) + round256(((size_t)a.groups + 1) * 4) +
-         round256((size_t)a.groups * a.blocks * 8);
+  size_t bytes = 256;
+  if (T > 0) (void)loss_ws(row_args(nullptr, nullptr, nullptr, T, E, k, n, loss_rows(E)), nullptr, &bytes);
+  return bytes;
 }
 
 // launch(std::integral_constant) for the lanes a row of E logits takes
@@ -289,21 +399,23 @@ hipError_t launch_balance_empty(int groups, int E, float* loss, int32_t* counts,
 
 hipError_t launch_balance_loss(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n,
                                float* loss, int32_t* counts, int32_t* live, void* wsp, hipStream_t s) {
-  const RowArgs a = row_args(z, ids, mask, T, E, k, n);
-  char* w = static_cast<char*>(wsp);
-  LossWs ws;
-  ws.counts = reinterpret_cast<int32_t*>(w);
-  w += round256((size_t)a.groups * E * 4);
-  ws.live = reinterpret_cast<int32_t*>(w);
-  ws.ticket = ws.live + a.groups;
-  w += round256(((size_t)a.groups + 1) * 4);
-  ws.part = reinterpret_cast<float2*>(w);
-  const int tok = kCountIds / k;
-  balance_count_kernel<<<dim3((unsigned)((n + tok - 1) / tok), (unsigned)std::min(a.groups, 4096)), 256, 0, s>>>(a, ws);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  const RowArgs a = row_args(z, ids, mask, T, E, k, n, loss_rows(E));
+  size_t bytes;
+  const LossWs ws = loss_ws(a, wsp, &bytes);
+  const bool self = ws.parts == 0;
+  if (!self) {
+    balance_count_kernel<<<dim3((unsigned)ws.parts, (unsigned)std::min(a.groups, 65535)), 256, 0, s>>>(
+        a, ws, 4 * lanes_of(E), (n - 1) / ws.parts + 1);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   by_lanes(E, [&](auto l) {
-    balance_loss_kernel<decltype(l)::value><<<(unsigned)(a.groups * a.blocks), 256, 0, s>>>(a, ws, loss, counts, live);
+    constexpr int L = decltype(l)::value;
+    const unsigned grid = (unsigned)(a.groups * a.blocks);
+    if (self)
+      balance_loss_kernel<L, true><<<grid, kLossWaves * kWave, 0, s>>>(a, ws, loss, counts, live);
+    else
+      balance_loss_kernel<L, false><<<grid, kLossWaves * kWave, 0, s>>>(a, ws, loss, counts, live);
   });
   return hipGetLastError();
 }
@@ -325,60 +437,69 @@ struct GateGradArgs {
   float* dz;               // [T, E]
 };
 
-template <int L>
+// Rounds of a block of 4 waves: few where a lane has many of a token's top-k.
+static constexpr int gate_rounds(int L) { return L >= 16 ? 4 : (L >= 4 ? 2 : 1); }
+static int gate_rows(int E) { return gate_rounds(lanes_of(E)) * 4 * (kWave / lanes_of(E)); }
+
+template <int L, bool GATE>
 __global__ __launch_bounds__(256) void gate_backward_kernel(RowArgs a, GateGradArgs b) {
-  constexpr int SLOTS = kWave / L;
-  __shared__ __align__(16) float s_row[4][SLOTS][L * 4];
+  constexpr int SLOTS = kWave / L, N = gate_rounds(L), PL = (kMaxTopk + L - 1) / L;
+  __shared__ __align__(16) float s_row[GATE ? 4 : 1][SLOTS][L * 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % L, slot = lane / L;
   const int g = (int)(blockIdx.x / a.blocks), blk = (int)(blockIdx.x - (unsigned)g * a.blocks);
   const int e0 = sub * 4;
   const bool vec = (a.E & 3) == 0;
-  float4* mine = reinterpret_cast<float4*>(&s_row[wave][slot][e0]);
-  *mine = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  Rows<L, 4, N> r;
+  r.load(a, g, blk, N, 0, lane, wave);
+  float w[N][PL], dw[N][PL];
+  int id[N][PL];
+  if (GATE) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int q = 0; q < PL; ++q) {
+        const int j = q * L + sub;
+        const bool there = r.in[i] && j < a.k;
+        const size_t at = there ? r.row[i] * a.k + j : 0;
+        w[i][q] = there ? b.w[at] : 0.0f;
+        dw[i][q] = there ? b.dw[at] : 0.0f;
+        id[i][q] = there ? a.ids[at] : -1;
+      }
+  }
   const int many = b.live[a.groups], full = b.live[a.groups + 1];
   const float gb = full > 0 ? b.dloss[0] * group_factor(a.E, a.k, b.live[g]) / (float)full : 0.0f;
   const float gz = many > 0 ? b.dloss[1] * 2.0f / (float)many : 0.0f;
   float c[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) c[q] = e0 + q < a.E ? (float)b.counts[(size_t)g * a.E + e0 + q] : 0.0f;
-  float4 v[kRowIters];
-  bool on[kRowIters];
+  float* srow = s_row[GATE ? wave : 0][slot];
+  float4* mine = reinterpret_cast<float4*>(srow + e0);
+  if (GATE) *mine = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-  for (int i = 0; i < kRowIters; ++i) {
-    const int t = (blk * kRowIters + i) * 4 * SLOTS + wave * SLOTS + slot;
-    const size_t row = (size_t)g * a.n + t;
-    on[i] = t < a.n && (a.mask == nullptr || a.mask[row] != 0);
-    v[i] = load_logits(a.z + row * a.E, e0, a.E, vec, on[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < kRowIters; ++i) {
-    const int t = (blk * kRowIters + i) * 4 * SLOTS + wave * SLOTS + slot;
-    const size_t row = (size_t)g * a.n + t;
+  for (int i = 0; i < N; ++i) {
+    float4& v = r.v[i];
     float inv, lse;
-    row_softmax<L>(v[i], inv, lse);
-    const float s = group_sum<L>((c[0] * v[i].x + c[1] * v[i].y) + (c[2] * v[i].z + c[3] * v[i].w)) * inv;
+    row_softmax<L>(v, inv, lse);
+    const float s = group_sum<L>((c[0] * v.x + c[1] * v.y) + (c[2] * v.z + c[3] * v.w)) * inv;
     const float zt = gz * lse;
-    auto grad = [&](float ex, float ce) { return on[i] ? ex * inv * (gb * (ce - s) + zt) : 0.0f; };
-    float4 d = make_float4(grad(v[i].x, c[0]), grad(v[i].y, c[1]), grad(v[i].z, c[2]), grad(v[i].w, c[3]));
-    if (b.w != nullptr) {
+    auto grad = [&](float ex, float ce) { return r.on[i] ? ex * inv * (gb * (ce - s) + zt) : 0.0f; };
+    float4 d = make_float4(grad(v.x, c[0]), grad(v.y, c[1]), grad(v.z, c[2]), grad(v.w, c[3]));
+    if (GATE) {
       float dot = 0.0f;
-      if (t < a.n)
-        for (int j = sub; j < a.k; j += L) dot += b.w[row * a.k + j] * b.dw[row * a.k + j];
+#pragma unroll
+      for (int q = 0; q < PL; ++q) dot += w[i][q] * dw[i][q];
       dot = group_sum<L>(dot);
-      if (t < a.n)
-        for (int j = sub; j < a.k; j += L) {
-          const int e = a.ids[row * a.k + j];
-          if ((unsigned)e < (unsigned)a.E)
-            atomicAdd(&s_row[wave][slot][e], b.w[row * a.k + j] * (b.dw[row * a.k + j] - dot));
-        }
+#pragma unroll
+      for (int q = 0; q < PL; ++q)
+        if ((unsigned)id[i][q] < (unsigned)a.E) atomicAdd(srow + id[i][q], w[i][q] * (dw[i][q] - dot));
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       const float4 add = *mine;
       *mine = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       d.x += add.x, d.y += add.y, d.z += add.z, d.w += add.w;
     }
-    if (t < a.n) {
-      float* out = b.dz + row * a.E;
+    if (r.in[i]) {
+      float* out = b.dz + r.row[i] * a.E;
       if (vec) {
         if (e0 < a.E) *reinterpret_cast<float4*>(out + e0) = d;
       } else {
@@ -394,10 +515,15 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(RowArgs a, GateGradA
 hipError_t launch_gate_backward(const float* z, const int32_t* ids, const uint8_t* mask, int T, int E, int k, int n,
                                 const int32_t* counts, const int32_t* live, const float* dloss, const float* w,
                                 const float* dw, float* dz, hipStream_t s) {
-  const RowArgs a = row_args(z, ids, mask, T, E, k, n);
+  const RowArgs a = row_args(z, ids, mask, T, E, k, n, gate_rows(E));
   const GateGradArgs b{counts, live, dloss, w, dw, dz};
   by_lanes(E, [&](auto l) {
-    gate_backward_kernel<decltype(l)::value><<<(unsigned)(a.groups * a.blocks), 256, 0, s>>>(a, b);
+    constexpr int L = decltype(l)::value;
+    const unsigned grid = (unsigned)(a.groups * a.blocks);
+    if (w != nullptr)
+      gate_backward_kernel<L, true><<<grid, 256, 0, s>>>(a, b);
+    else
+      gate_backward_kernel<L, false><<<grid, 256, 0, s>>>(a, b);
   });
   return hipGetLastError();
 }
