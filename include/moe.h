@@ -487,9 +487,7 @@ moe_status moe_grouped_gemm_mx4(const uint8_t* aq, const uint32_t* as, const uin
  * moe_grouped_swiglu_ffn_mx4 - the MXFP4 expert FFN: moe_grouped_swiglu_mx4 into
  * the workspace, then moe_grouped_gemm_mx4 with W_down (wdq [E_local, H,
  * 128 C(I)], wds) into y_perm [M_cap, H] bf16. Code rows are ldw_gu (W_gate,
- * W_up) and ldw_dn (W_down) bytes apart (0: dense). E: the experts of the whole
- * layer or 0 (as moe_grouped_swiglu_ffn_gather_of: with perm_src the library then
- * expects T * k / E rows an expert; the results do not depend on it).
+ * W_up) and ldw_dn (W_down) bytes apart (0: dense).
  * ws starts with 16 KiB of counters that must be zero before the first call on
  * the workspace (every call leaves them zero), then h codes [M_cap, 128 C(I)]
  * and, 256-byte aligned after them, their scales, then the split plan and the
@@ -503,7 +501,7 @@ moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs,
                                       const int32_t* perm_src, int T, int k, const uint8_t* wgq,
                                       const uint32_t* wgs, const uint8_t* wuq, const uint32_t* wus,
                                       const uint8_t* wdq, const uint32_t* wds,
-                                      const int32_t* offsets, int E, int E_local, int H, int I,
+                                      const int32_t* offsets, int E_local, int H, int I,
                                       int ldw_gu, int ldw_dn, int M_cap, void* y_perm, void* ws,
                                       size_t* ws_bytes, hipStream_t stream);
 

@@ -115,7 +115,7 @@ def load_library(path: str = LIB_PATH):
     L.moe_grouped_gemm_mx4.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P]
     L.moe_grouped_swiglu_ffn_mx4.restype = _I
     L.moe_grouped_swiglu_ffn_mx4.argtypes = [_P, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I,
-                                             _I, _P, _P, _PSZ, _P]
+                                             _P, _P, _PSZ, _P]
     L.moe_balance_loss.restype = _I
     L.moe_balance_loss.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _PSZ, _P]
     L.moe_gate_backward.restype = _I
@@ -1042,17 +1042,19 @@ def moe_grouped_gemm_mx4(a, b, offsets, c=None):
 def ffn_mx4_ws_bytes(E_local, H, I, M_cap):
     L = load_library()
     n = ctypes.c_size_t(0)
-    st = L.moe_grouped_swiglu_ffn_mx4(None, None, None, 0, 0, None, None, None, None, None, None, None, 0, E_local, H,
-                                      I, 0, 0, M_cap, None, None, ctypes.byref(n), None)
+    st = L.moe_grouped_swiglu_ffn_mx4(None, None, None, 0, 0, None, None, None, None, None, None, None, E_local, H, I,
+                                      0, 0, M_cap, None, None, ctypes.byref(n), None)
     _check("moe_grouped_swiglu_ffn_mx4", st)
     return n.value
 
 
 def moe_grouped_swiglu_ffn_mx4(x, w_gate, w_up, w_down, offsets, ws=None, y_perm=None, perm_src=None, k=1, experts=0):
     """MXFP4 expert FFN. x: Mx4Tensor [M_cap, H], or with perm_src [M_cap] (moe_permute)
-    [T, H], of which row r of the input is x[perm_src[r] // k]. ``experts``: the experts
-    of the whole layer, if known (the results are the same). Returns (y_perm [M_cap, H]
-    bf16, ws)."""
+    [T, H], of which row r of the input is x[perm_src[r] // k]. ``experts`` is there for
+    calls written like moe_grouped_swiglu_ffn_gather's: there is one kernel for all
+    loads, and nothing depends on it. Returns (y_perm [M_cap, H] bf16, ws)."""
+    if experts < 0 or (experts and experts < w_gate.shape[0]):
+        raise ValueError("experts must be 0 or at least the local experts")
     L = load_library()
     M_cap, T, src = _mx4_rows(x, perm_src, k)
     H = x.shape[1]
@@ -1073,8 +1075,8 @@ def moe_grouped_swiglu_ffn_mx4(x, w_gate, w_up, w_down, offsets, ws=None, y_perm
                                       *_mx4_dev(w_gate, "w_gate", (E_local, I, H), True),
                                       *_mx4_dev(w_up, "w_up", (E_local, I, H), True),
                                       *_mx4_dev(w_down, "w_down", (E_local, H, I), True),
-                                      _dev(offsets, "offsets", torch.int32), experts, E_local, H, I, w_gate.ld,
-                                      w_down.ld, M_cap, _dev(y_perm, "y_perm", torch.bfloat16),
+                                      _dev(offsets, "offsets", torch.int32), E_local, H, I, w_gate.ld, w_down.ld,
+                                      M_cap, _dev(y_perm, "y_perm", torch.bfloat16),
                                       _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
     _check("moe_grouped_swiglu_ffn_mx4", st)
     return y_perm, ws

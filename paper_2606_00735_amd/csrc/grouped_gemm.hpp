@@ -30,7 +30,7 @@ enum Fmt : int { kBf16, kMx8, kMx4 };
 // is what the large tile in quadrant phases needs. With W = 8 the small and mid
 // tiles run 2-7 % faster (more where few rows are there), a second wave per SIMD
 // covering the first one's LDS waits and epilogue. waves_for chooses; either
-// kernel has every class.
+// kernel has every class. MXFP4 takes 8 waves for all of them (mx4_kernels.hip).
 constexpr int kMaxWaves = 8;
 constexpr int kSmallM = 64;
 
@@ -483,20 +483,23 @@ __device__ __forceinline__ void mx4_store_scale(const GemmArgs& a, int row, int 
   if (a.N % kMx4Chunk != 0 && col / kMx4Chunk == a.N / kMx4Chunk) p[mx4_scale_byte(b + 4)] = 0;
 }
 
-// A wave's block of h = val(i, j, v) as MXFP4. The 32 values of a row and block
-// sit in lanes l and l ^ 32, four columns of each eight in either; the two swap
-// halves so that a lane stores whole blocks, 16 bytes of one row.
+// A wave's block of h = val(i, j, v) as MXFP4. The 32 values of a row and block sit
+// in lanes l and l ^ 32, four columns of each eight in either. The two swap dwords so
+// that a lane stores whole runs of a row: 16 bytes (one block: lane half hi takes
+// block hi of a pair), or 8 of them where the wave has a single block of columns.
 template <int MI, int NI, class Val>
 __device__ __forceinline__ void mx4_store_h(const GemmArgs& a, int row0, int m_end, int col0, int lane, Val&& val) {
+  static_assert(NI == 1 || NI % 2 == 0, "blocks in pairs");
   const int hi = lane >> 5;
   const size_t ldc = mx4_row_bytes(a.N);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int row = row0 + i * 32 + (lane & 31);
     if (row0 + i * 32 >= m_end) break;
+    uint8_t* out = reinterpret_cast<uint8_t*>(a.C) + (size_t)row * ldc + col0 / 2;
+    uint32_t w[NI][2];  // groups g = 0, 1 and 2, 3: columns 8 g + 4 hi + (0..3)
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int col = col0 + j * 32;
       float r[16];
       uint32_t top = 0;
 #pragma unroll
@@ -507,21 +510,34 @@ __device__ __forceinline__ void mx4_store_h(const GemmArgs& a, int row0, int m_e
       top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
       const uint32_t code = mx4_scale_code(top);
       const float sc = mx4_scale(code);
-      uint32_t w[2];  // groups g = 0, 1 and 2, 3: columns 8 g + 4 hi + (0..3)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        w[q] = e2m1x4(r[8 * q], r[8 * q + 1], r[8 * q + 2], r[8 * q + 3], sc) |
-               e2m1x4(r[8 * q + 4], r[8 * q + 5], r[8 * q + 6], r[8 * q + 7], sc) << 16;
-        if (code == kMxNan) w[q] = 0;
+        w[j][q] = e2m1x4(r[8 * q], r[8 * q + 1], r[8 * q + 2], r[8 * q + 3], sc) |
+                  e2m1x4(r[8 * q + 4], r[8 * q + 5], r[8 * q + 6], r[8 * q + 7], sc) << 16;
+        if (code == kMxNan) w[j][q] = 0;
       }
-      // lane half 0 keeps columns 0-15 and gets the partner's, half 1 columns 16-31
-      const uint32_t keep = hi ? w[1] : w[0];
-      const uint32_t other = (uint32_t)__shfl_xor((int)(hi ? w[0] : w[1]), 32, kWave);
-      const uint32_t lo = hi ? other : keep, up = hi ? keep : other;  // of lane halves 0 and 1
-      const uint2 out = make_uint2((lo & 0xFFFFu) | up << 16, lo >> 16 | (up & 0xFFFF0000u));
-      if (row < m_end) {
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(a.C) + (size_t)row * ldc + col / 2 + hi * 8) = out;
-        if (hi == 0) mx4_store_scale(a, row, col, code);
+      if (hi == 0 && row < m_end) mx4_store_scale(a, row, col0 + j * 32, code);
+    }
+    // columns [16 q, 16 q + 16) of a block from the dwords of lane halves 0 and 1
+    auto join = [](uint32_t lo, uint32_t up) {
+      return make_uint2(__builtin_amdgcn_perm(up, lo, 0x05040100u), __builtin_amdgcn_perm(up, lo, 0x07060302u));
+    };
+    if constexpr (NI == 1) {
+      const uint32_t keep = hi ? w[0][1] : w[0][0];
+      const uint32_t other = (uint32_t)__shfl_xor((int)(hi ? w[0][0] : w[0][1]), 32, kWave);
+      if (row < m_end) *reinterpret_cast<uint2*>(out + hi * 8) = hi ? join(other, keep) : join(keep, other);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NI; j += 2) {
+        uint2 half[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint32_t keep = hi ? w[j + 1][q] : w[j][q];
+          const uint32_t other = (uint32_t)__shfl_xor((int)(hi ? w[j][q] : w[j + 1][q]), 32, kWave);
+          half[q] = hi ? join(other, keep) : join(keep, other);
+        }
+        const u32x4_t v = {half[0].x, half[0].y, half[1].x, half[1].y};
+        if (row < m_end) *reinterpret_cast<u32x4_t*>(out + j * 16 + hi * 16) = v;
       }
     }
   }
@@ -530,13 +546,9 @@ __device__ __forceinline__ void mx4_store_h(const GemmArgs& a, int row0, int m_e
 // A wave's WM x WN block of h = val(i, j, v) as MXFP8: the 32 values of a row
 // and block sit in lanes l and l ^ 32; codes through store_block, one scale
 // code byte per row and block.
-template <int F, int MI, int NI, int WM, int WN, class Val>
+template <int MI, int NI, int WM, int WN, class Val>
 __device__ __forceinline__ void mx_store_h(const GemmArgs& a, bf16_t* smem, int row0, int m_end, int col0, int wave,
                                            int lane, Val&& val) {
-  if constexpr (F == kMx4) {
-    mx4_store_h<MI, NI>(a, row0, m_end, col0, lane, val);
-    return;
-  }
   uint32_t codes[MI][NI][4];
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
@@ -747,7 +759,7 @@ __device__ __forceinline__ void gemm_tile_mx(const GemmArgs& a, bf16_t* smem, in
   // Epilogue: output layout as in gemm_tile (lane l: row l % 32, columns
   // 8 g + 4 h + (0..3) of each 32-column block).
   if constexpr (DUAL) {
-    mx_store_h<kMx8, MI, NI, WM, WN>(
+    mx_store_h<MI, NI, WM, WN>(
         a, smem, m0 + wm * WM, m_end, n0 + wn * WN, wave, lane,
         [&](int i, int j, int v) { return silu_mul_fast(acc[0][i][j][v], acc[NB - 1][i][j][v]); });
   } else {
@@ -795,14 +807,14 @@ __device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, i
   constexpr int RPI = 8, LA = AR / (RPI * W), LB = BN / (RPI * W);
   uint32_t offA[LA], offB[LB];
 #pragma unroll
-  for (int t = 0; t < LA; ++t) {
-    const int r = (t * W + wave) * RPI + lane / 8;
-    offA[t] = (uint32_t)a_row(r) * (uint32_t)K + (uint32_t)(swz_chunk<kBK>(r, lane % 8) * 16);
-  }
-#pragma unroll
   for (int t = 0; t < LB; ++t) {
     const int r = (t * W + wave) * RPI + lane / 8;
     offB[t] = (uint32_t)(r * LDB + swz_chunk<kBK>(r, lane % 8) * 16);
+  }
+#pragma unroll
+  for (int t = 0; t < LA; ++t) {
+    const int r = (t * W + wave) * RPI + lane / 8;
+    offA[t] = (uint32_t)a_row(r) * (uint32_t)K + (uint32_t)(swz_chunk<kBK>(r, lane % 8) * 16);
   }
   // Scale dwords: load u of wave w takes those of stage rows [32 (u W + w), +32),
   // all in one operand (AR and BN are multiples of 32), as in gemm_tile_mx.
@@ -836,7 +848,8 @@ __device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, i
       for (int j = 0; j < NI; ++j) acc[b][i][j] = f32x16_t{};
 
   // A placeholder load (live == false) re-reads the last chunk, which is in
-  // the cache by then, so loads never leave the operands.
+  // the cache by then, so loads never leave the operands. The weights go first: the
+  // rows may wait for the gather's indices.
   if (kc1 < 0) kc1 = nK;
   constexpr int KS = 4;
   auto issue = [&](int kc, bool live, bf16_t* st, int part) {
@@ -846,17 +859,16 @@ __device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, i
     constexpr int LS = W * RPI * 128;  // LDS bytes between a wave's loads
     auto mine = [&](int t) { return part < 0 || (St::NS > 2 ? t * KS / St::LOADS : 0) == part; };
 #pragma unroll
-    for (int t = 0; t < LA; ++t)
-      if (mine(t)) dma16a(uniform_ptr(A + (size_t)kcl * 128), offA[t], l0 + t * LS);
-#pragma unroll
     for (int t = 0; t < LB; ++t)
-      if (mine(LA + t)) dma16a(uniform_ptr(B0 + (size_t)kcl * 128), offB[t], l0 + AR * 128 + t * LS);
+      if (mine(t)) dma16a(uniform_ptr(B0 + (size_t)kcl * 128), offB[t], l0 + AR * 128 + t * LS);
     if (DUAL) {
 #pragma unroll
       for (int t = 0; t < LB; ++t)
-        if (mine(LA + LB + t))
-          dma16a(uniform_ptr(B1 + (size_t)kcl * 128), offB[t], l0 + (AR + BN) * 128 + t * LS);
+        if (mine(LB + t)) dma16a(uniform_ptr(B1 + (size_t)kcl * 128), offB[t], l0 + (AR + BN) * 128 + t * LS);
     }
+#pragma unroll
+    for (int t = 0; t < LA; ++t)
+      if (mine(NB * LB + t)) dma16a(uniform_ptr(A + (size_t)kcl * 128), offA[t], l0 + t * LS);
 #pragma unroll
     for (int u = 0; u < St::SLOADS; ++u)
       if (mine(LA + NB * LB + u))
@@ -957,18 +969,14 @@ __device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, i
 // ---------------------------------------------------------------------------
 constexpr int kSlotRows = 128;
 constexpr int kSlotElems = kSlotRows * kBK;  // bf16 elements: 16 KB
-template <int F>
+template <bool MX>
 struct BigStages {
   static constexpr int SCALE_OFF = 8 * kSlotElems;                     // elements: after the 8 slots
-  static constexpr int SB = F == kMx4 ? 8 : 4;                         // scale bytes of a row and chunk
-  static constexpr int BYTES = 8 * kSlotElems * 2 + (F != kBf16 ? 8 * kSlotRows * SB : 0);
-  static constexpr int LOADS = F != kBf16 ? 5 : 4;  // loads per wave per slot
+  static constexpr int BYTES = 8 * kSlotElems * 2 + (MX ? 8 * kSlotRows * 4 : 0);
+  static constexpr int LOADS = MX ? 5 : 4;  // loads per wave per slot
 };
 
-// MXFP4 takes the bf16 tile's steps (a chunk is four k-steps of 16-byte pieces in
-// both) with the scaled MFMA; the scale dword of a lane's row and half serves all
-// four k-steps of a chunk.
-template <bool DUAL, int F>
+template <bool DUAL, bool MX>
 __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e, int m0, int m_end, int n0,
                                          int kc0 = 0, int kc1 = -1, float* pbase = nullptr, size_t pstride = 0,
                                          int pld = 0, int pcol0 = 0) {
@@ -976,9 +984,8 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // them stay in SGPRs
   e = uniform_int(e), m0 = uniform_int(m0), m_end = uniform_int(m_end), n0 = uniform_int(n0);
   kc0 = uniform_int(kc0), kc1 = uniform_int(kc1);
-  using St = BigStages<F>;
-  constexpr bool MX = F != kBf16;
-  constexpr int EB = MX ? 1 : 2;           // bytes per unit of K and ldb
+  using St = BigStages<MX>;
+  constexpr int EB = MX ? 1 : 2;           // bytes per element
   constexpr int CB = 128;                  // bytes of a row per chunk
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
@@ -988,18 +995,16 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   if (kc1 < 0) kc1 = nKt;
   const int nK = kc1 - kc0;
   const int a_rows = m_end - m0;
-  const bool gather = F != kMx8 && a.a_src != nullptr;
+  const bool gather = !MX && a.a_src != nullptr;
   const size_t ldbB = (size_t)a.ldb * EB;  // bytes between weight rows
   const char* A = reinterpret_cast<const char*>(a.A) + (gather ? 0 : (size_t)m0 * K * EB);
   const char* B0 = reinterpret_cast<const char*>(a.B0) + ((size_t)e * N + n0) * ldbB;
   const char* B1 = DUAL ? reinterpret_cast<const char*>(a.B1) + ((size_t)e * N + n0) * ldbB : B0 + 64 * ldbB;
   const char *SA = nullptr, *SB0 = nullptr, *SB1 = nullptr;
-  const size_t sa_rows = gather ? (size_t)a.a_T : (size_t)a.M_cap;  // rows of the A scales
   if (MX) {
-    constexpr int DW = St::SB / 4;  // scale dwords of a row and chunk
-    SA = reinterpret_cast<const char*>(a.As + (gather ? 0 : (size_t)m0 * DW));
-    SB0 = reinterpret_cast<const char*>(a.Bs0 + ((size_t)e * nKt * N + n0) * DW);
-    SB1 = DUAL ? reinterpret_cast<const char*>(a.Bs1 + ((size_t)e * nKt * N + n0) * DW) : SB0 + 64 * St::SB;
+    SA = reinterpret_cast<const char*>(a.As + m0);
+    SB0 = reinterpret_cast<const char*>(a.Bs0 + (size_t)e * nKt * N + n0);
+    SB1 = DUAL ? reinterpret_cast<const char*>(a.Bs1 + (size_t)e * nKt * N + n0) : SB0 + 64 * 4;
   }
 
   // Slot row q of A half h is tile row 128 (q / 64) + 64 h + q % 64; of B
@@ -1023,24 +1028,14 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // scale dwords: waves 0 and 2 load slot rows [0, 64), waves 1 and 3 rows
   // [64, 128) (the same values to the same place twice)
   uint32_t soffA[2], soffB = 0;
-  if constexpr (F == kMx4) {
-    // two dwords a row: wave w loads slot rows [32 w, +32)
-    const int q = wave * 32 + (lane >> 1);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      int rr = min((q >> 6) * 128 + h * 64 + (q & 63), a_rows - 1);
-      if (gather) rr = min(max(a.a_src[m0 + rr] / a.a_div, 0), a.a_T - 1);
-      soffA[h] = (uint32_t)rr * 8u + (lane & 1) * 4u;
-    }
-    soffB = (uint32_t)(DUAL ? q : (q >> 6) * 128 + (q & 63)) * 8u + (lane & 1) * 4u;
-  } else if (MX) {
+  if (MX) {
     soffA[0] = (uint32_t)min((wave & 1) * 128 + lane, a_rows - 1) * 4u;
     soffA[1] = (uint32_t)min((wave & 1) * 128 + 64 + lane, a_rows - 1) * 4u;
     soffB = (uint32_t)((wave & 1) * (DUAL ? 64 : 128) + lane) * 4u;
   }
 
   const uint32_t lds0 = lds_addr(smem) + wave * 8 * CB;
-  const uint32_t ldss = lds_addr(smem) + St::SCALE_OFF * 2 + (F == kMx4 ? wave : wave & 1) * 256;
+  const uint32_t ldss = lds_addr(smem) + St::SCALE_OFF * 2 + (wave & 1) * 256;
   // load t of slot w (0, 1: A halves; 2, 3: B halves) of chunk kc
   auto issue = [&](int w, int kc, int t) {
     // past the last chunk: a placeholder load of one line
@@ -1051,8 +1046,8 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
            ((kc & 1) * 4 + w) * (kSlotElems * 2) + t * 32 * CB);
     if (MX && t == 3) {
       const char* sbase = w < 2 ? SA : (w == 2 ? SB0 : SB1);
-      dma4a(sbase + (size_t)kcl * (w < 2 ? sa_rows : (size_t)N) * St::SB, w < 2 ? soffA[w & 1] : soffB,
-            ldss + ((kc & 1) * 4 + w) * (kSlotRows * St::SB));
+      dma4a(sbase + (size_t)kcl * (w < 2 ? a.M_cap : N) * 4, w < 2 ? soffA[w & 1] : soffB,
+            ldss + ((kc & 1) * 4 + w) * (kSlotRows * 4));
     }
   };
   auto issue_slot = [&](int w, int kc) {
@@ -1062,7 +1057,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
   // fragments: 16-byte piece 2 q + hi of the lane's row, q = 0..3 (bf16: the
   // k-step q; MXFP8: pieces 2 s and 2 s + 1 are k-step s)
   uint4 fr[4][2][4];     // [slot][32-row block][piece]
-  uint32_t sc[4][2];     // MXFP8: scale dword of the row, shifted to this lane's block; MXFP4: of the row and lane half
+  uint32_t sc[4][2];     // MXFP8: scale dword of the row, shifted to this lane's block
   uint32_t fofA[4], fofB[4];  // byte offset of the lane's piece in slot 0
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -1075,12 +1070,10 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     fr[w][i][q] = *reinterpret_cast<const uint4*>(lds + (w < 2 ? fofA[q] : fofB[q]) +
                                                   ((kc & 1) * 4 + w) * (kSlotElems * 2) + i * 32 * CB);
   };
-  const uint32_t sofA = (uint32_t)(wm * 64 + r32) * St::SB + (F == kMx4 ? hi * 4 : 0);
-  const uint32_t sofB = (uint32_t)(wn * 64 + r32) * St::SB + (F == kMx4 ? hi * 4 : 0);
+  const uint32_t sofA = (uint32_t)(wm * 64 + r32) * 4, sofB = (uint32_t)(wn * 64 + r32) * 4;
   auto reads = [&](int w, int kc, int i) {
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(
-        lds + (w < 2 ? sofA : sofB) + St::SCALE_OFF * 2 + ((kc & 1) * 4 + w) * (kSlotRows * St::SB) + i * 32 * St::SB);
-    sc[w][i] = F == kMx4 ? v : v >> (8 * hi);
+    sc[w][i] = *reinterpret_cast<const uint32_t*>(lds + (w < 2 ? sofA : sofB) + St::SCALE_OFF * 2 +
+                                                  ((kc & 1) * 4 + w) * (kSlotRows * 4) + i * 128) >> (8 * hi);
   };
 
   f32x16_t acc[2][2][2][2];  // [A half][B half][row block][column block]
@@ -1094,9 +1087,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
         for (int j = 0; j < 2; ++j) acc[h][b][i][j] = f32x16_t{};
 
   auto mma = [&](int ha, int hb, int i, int j, int q) {
-    if constexpr (F == kMx4) {
-      acc[ha][hb][i][j] = mfma_mx4(q, fr[2 + hb][j][q], fr[ha][i][q], acc[ha][hb][i][j], sc[2 + hb][j], sc[ha][i]);
-    } else if constexpr (F == kBf16) {
+    if constexpr (!MX) {
       acc[ha][hb][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fr[2 + hb][j][q]), as_bf16x8(fr[ha][i][q]),
                                                                   acc[ha][hb][i][j], 0, 0, 0);
     } else {
@@ -1124,14 +1115,13 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     for (int t = 0; t < 4; ++t) {
       // four bf16 (or two MXFP8) MFMAs, one load and, in the first half of
       // the phase, four LDS reads
-      if constexpr (F != kMx8) {
+      if constexpr (!MX) {
         mma(ha, hb, 0, 0, t);
         mma(ha, hb, 0, 1, t);
         issue(iw, ic, t);
         if (t < 2) {
           readf(rw, rc, 0, 2 * t);
           readf(rw, rc, 1, 2 * t);
-          if constexpr (F == kMx4) reads(rw, rc, t);
         }
         mma(ha, hb, 1, 0, t);
         mma(ha, hb, 1, 1, t);
@@ -1139,7 +1129,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
           readf(rw, rc, 0, 2 * t + 1);
           readf(rw, rc, 1, 2 * t + 1);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, F == kMx4 ? 2 : 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -1229,7 +1219,7 @@ __device__ __forceinline__ void big_tile(const GemmArgs& a, bf16_t* smem, int e,
     return;
   }
   if constexpr (DUAL && MX) {
-    mx_store_h<F, 4, 2, 128, 64>(a, smem, m0 + wm * 128, m_end, n0 + wn * 64, wave, lane, [&](int i, int j, int v) {
+    mx_store_h<4, 2, 128, 64>(a, smem, m0 + wm * 128, m_end, n0 + wn * 64, wave, lane, [&](int i, int j, int v) {
       return silu_mul_fast(acc[i >> 1][0][i & 1][j][v], acc[i >> 1][1][i & 1][j][v]);
     });
   } else if constexpr (DUAL) {
@@ -1253,7 +1243,7 @@ struct GemmShapes {
   // dual: 128 columns per matrix; single: 128 or 256 columns (see the kernel)
   static constexpr int BNW = DUAL ? 128 : 256;
   static constexpr int b0 = Stages<64, BNW, DUAL, W>::BYTES, b1 = Stages<128, BNW, DUAL, W>::BYTES;
-  static constexpr int b2 = W == 4 ? BigStages<kBf16>::BYTES : Stages<256, BNW, DUAL, 8>::BYTES;
+  static constexpr int b2 = W == 4 ? BigStages<false>::BYTES : Stages<256, BNW, DUAL, 8>::BYTES;
   static constexpr int b3 = DUAL ? 0 : Stages<256, 128, false, W>::BYTES;
   static constexpr int m01 = b0 > b1 ? b0 : b1, m23 = b2 > b3 ? b2 : b3;
   static constexpr int kSmem = (m01 > m23 ? m01 : m23) / 2;  // bf16 elements
@@ -1343,7 +1333,7 @@ template <bool DUAL, int W, int F>
 struct MxShapes {
   static constexpr int BNW = DUAL ? 128 : 256;
   static constexpr int b0 = MxStages<64, BNW, DUAL, W, F>::BYTES, b1 = MxStages<128, BNW, DUAL, W, F>::BYTES;
-  static constexpr int b2 = W == 4 ? BigStages<F>::BYTES : MxStages<256, BNW, DUAL, 8, F>::BYTES;
+  static constexpr int b2 = W == 4 ? BigStages<true>::BYTES : MxStages<256, BNW, DUAL, 8, F>::BYTES;
   static constexpr int b3 = DUAL ? 0 : MxStages<256, 128, false, W, F>::BYTES;
   static constexpr int b4 = MxStages<64, 128, DUAL, W, F>::BYTES, b5 = MxStages<128, 128, DUAL, W, F>::BYTES;
   static constexpr int m01 = b0 > b1 ? b0 : b1, m23 = b2 > b3 ? b2 : b3, m45 = b4 > b5 ? b4 : b5;
@@ -1400,12 +1390,7 @@ __device__ __forceinline__ void run_tile(const GemmArgs& a, bf16_t* smem, int cl
           gemm_tile<W, 256, BN, 4, DUAL>(a, smem, e, m0, m_end, n0);
       }
     } else if constexpr (DUAL || WIDE) {
-      big_tile<DUAL, F>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
-    } else if constexpr (F == kMx4) {
-      if (pbase != nullptr)
-        gemm_tile_mx4<W, 256, BN, 2, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
-      else
-        gemm_tile_mx4<W, 256, BN, 2, DUAL>(a, smem, e, m0, m_end, n0);
+      big_tile<DUAL, F == kMx8>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);
     } else if constexpr (F == kMx8) {
       if (pbase != nullptr)
         gemm_tile_mx<W, 256, BN, 2, DUAL, true>(a, smem, e, m0, m_end, n0, kc0, kc1, pbase, ps, pld, pcol0);

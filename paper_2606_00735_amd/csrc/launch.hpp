@@ -85,7 +85,7 @@ hipError_t launch_gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weigh
 size_t ffn_mx4_ws_bytes(int M_cap, int E_local, int H, int I);
 hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const Mx4Weights& wd,
                           const int32_t* offsets, int E_local, int H, int I, int M_cap, void* y_perm, void* ws,
-                          hipStream_t s, int rows);
+                          hipStream_t s);
 
 // The router's training step (train_kernels.hip, router_grad_kernels.hip).
 // n: tokens of a group of the balance loss (T a multiple of it, n > 0)

@@ -583,12 +583,11 @@ moe_status moe_grouped_gemm_mx4(const uint8_t* aq, const uint32_t* as, const uin
 moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs, const int32_t* perm_src, int T, int k,
                                       const uint8_t* wgq, const uint32_t* wgs, const uint8_t* wuq,
                                       const uint32_t* wus, const uint8_t* wdq, const uint32_t* wds,
-                                      const int32_t* offsets, int E, int E_local, int H, int I, int ldw_gu,
-                                      int ldw_dn, int M_cap, void* y_perm, void* ws, size_t* ws_bytes,
-                                      hipStream_t stream) {
+                                      const int32_t* offsets, int E_local, int H, int I, int ldw_gu, int ldw_dn,
+                                      int M_cap, void* y_perm, void* ws, size_t* ws_bytes, hipStream_t stream) {
   moe_status st = mx_gemm_shape_ok(E_local, I, H, M_cap);
   if (st != MOE_OK) return st;
-  if (E < 0 || E > MOE_MAX_EXPERTS || (E > 0 && E < E_local) || ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  if (ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
   int ld_gu = 0, ld_dn = 0;
   if ((st = mx4_row_stride(ldw_gu, H, &ld_gu)) != MOE_OK || (st = mx4_row_stride(ldw_dn, I, &ld_dn)) != MOE_OK)
     return st;
@@ -603,10 +602,8 @@ moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs, con
   if (!mx_operand_ok(xq, xs) || !mx_operand_ok(wgq, wgs) || !mx_operand_ok(wuq, wus) || !mx_operand_ok(wdq, wds) ||
       !y_perm || !aligned16(y_perm) || !aligned16(ws) || !offsets || !aligned4(offsets))
     return MOE_ERR_INVALID_ARG;
-  // rows an expert is expected to have, as in moe_grouped_swiglu_ffn_gather_of
-  const int rows = E > 0 && perm_src != nullptr ? (int)std::max(1LL, (long long)T * k / E) : 0;
   return hip_status(moe::launch_ffn_mx4({xq, xs, perm_src, k, T}, {wgq, wgs, ld_gu}, {wuq, wus, ld_gu},
-                                        {wdq, wds, ld_dn}, offsets, E_local, H, I, M_cap, y_perm, ws, stream, rows));
+                                        {wdq, wds, ld_dn}, offsets, E_local, H, I, M_cap, y_perm, ws, stream));
 }
 
 // ---------------------------------------------------------------------------

@@ -178,9 +178,20 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, i
 // Expert FFN: gate/up (MXFP4 in, MXFP4 h out), then down (bf16 out), by the tile
 // schedules of the bf16 FFN (grouped_gemm.hpp).
 // ---------------------------------------------------------------------------
-template <bool DUAL, int W>
-__global__ __launch_bounds__(W* kWave) void grouped_gemm_mx4_kernel(GemmArgs a) {
-  grouped_gemm_body<W, DUAL, kMx4>(a);
+// 8 waves for every tile: the 256-row tile in quadrant phases on 4 waves that bf16
+// and MXFP8 take for large experts was no faster at 4 bits (FFN us, 4 / 8 waves, 8
+// experts of 1024 rows, H = 4096, I = 14336: 891 / 893; 32 of 512 rows, H = 7168, I =
+// 2048: 597 / 587; 128 of 512 rows, H = 2048, I = 768: 353 / 353). A tile's K loop is
+// a quarter as long, and what stands around it counts for more: per 256 x 256 tile a
+// product of 8192 x 8192 over K took 14.5 us + K / 16384 x 102 us (5.4 PFLOP/s in
+// the loop), the dual one 10.6 + K / 16384 x 112 us: the outputs' stores (128 KB a CU
+// at once, 7 us at the memory's rate) and SiLU and quantisation (1250 vector and 256
+// transcendental instructions a wave, 5 us). Loading the next tile's first chunks
+// before the epilogue gained nothing (888 / 890): the K loop's waits then count the
+// stores, which leave the counter in order.
+template <bool DUAL>
+__global__ __launch_bounds__(8 * kWave) void grouped_gemm_mx4_kernel(GemmArgs a) {
+  grouped_gemm_body<8, DUAL, kMx4>(a);
 }
 
 // The MXFP4 gate/up reduction: sums the S partials of gate and up for 4
@@ -245,7 +256,7 @@ size_t ffn_mx4_ws_bytes(int M_cap, int E_local, int H, int I) {
 
 static hipError_t gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const int32_t* offsets,
                              int E_local, int H, int I, int M_cap, uint8_t* hq, uint32_t* hs, const MxSplit& sp,
-                             hipStream_t s, int rows) {
+                             hipStream_t s) {
   GemmArgs g{};
   g.A = reinterpret_cast<const bf16_t*>(x.codes);
   g.B0 = reinterpret_cast<const bf16_t*>(wg.codes);
@@ -266,16 +277,15 @@ static hipError_t gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4We
   g.Bs1 = wu.scales;
   g.Cs = hs;
   const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
-  hipError_t e = launch_waves(waves_for(true, M_cap, E_local, I, H, rows), g, mx_grid(M_cap, E_local, I, split || g.sk),
-                              s, grouped_gemm_mx4_kernel<true, 4>, grouped_gemm_mx4_kernel<true, 8>);
+  grouped_gemm_mx4_kernel<true><<<mx_grid(M_cap, E_local, I, split || g.sk), 8 * kWave, 0, s>>>(g);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split || sp.no_reduce) return e;
   split_reduce_mx4_kernel<<<mx_reduce_grid(0, 0), 256, 0, s>>>(g);
   return hipGetLastError();
 }
 
 static hipError_t gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weights& w, const int32_t* offsets,
-                           int E_local, int N, int K, int M_cap, void* c, const MxSplit& sp, hipStream_t s,
-                           int rows) {
+                           int E_local, int N, int K, int M_cap, void* c, const MxSplit& sp, hipStream_t s) {
   GemmArgs g{};
   g.A = reinterpret_cast<const bf16_t*>(aq);
   g.B0 = reinterpret_cast<const bf16_t*>(w.codes);
@@ -290,9 +300,8 @@ static hipError_t gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weigh
   g.As = as;
   g.Bs0 = w.scales;
   const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
-  hipError_t e = launch_waves(waves_for(false, M_cap, E_local, N, K, rows), g,
-                              mx_grid(M_cap, E_local, N, split || g.sk), s, grouped_gemm_mx4_kernel<false, 4>,
-                              grouped_gemm_mx4_kernel<false, 8>);
+  grouped_gemm_mx4_kernel<false><<<mx_grid(M_cap, E_local, N, split || g.sk), 8 * kWave, 0, s>>>(g);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split || sp.no_reduce) return e;
   split_reduce_kernel<false><<<mx_reduce_grid(0, 0), 256, 0, s>>>(sp.part, sp.plan, N, static_cast<bf16_t*>(c));
   return hipGetLastError();
@@ -301,18 +310,18 @@ static hipError_t gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weigh
 hipError_t launch_gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const int32_t* offsets,
                              int E_local, int H, int I, int M_cap, uint8_t* hq, uint32_t* hs, hipStream_t s) {
   if (E_local == 0 || M_cap == 0) return hipSuccess;
-  return gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, MxSplit{}, s, 0);
+  return gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, MxSplit{}, s);
 }
 
 hipError_t launch_gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weights& w, const int32_t* offsets,
                            int E_local, int N, int K, int M_cap, void* c, hipStream_t s) {
   if (E_local == 0 || M_cap == 0) return hipSuccess;
-  return gemm_mx4(aq, as, w, offsets, E_local, N, K, M_cap, c, MxSplit{}, s, 0);
+  return gemm_mx4(aq, as, w, offsets, E_local, N, K, M_cap, c, MxSplit{}, s);
 }
 
 hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weights& wu, const Mx4Weights& wd,
                           const int32_t* offsets, int E_local, int H, int I, int M_cap, void* y_perm, void* ws,
-                          hipStream_t s, int rows) {
+                          hipStream_t s) {
   if (E_local == 0 || M_cap == 0) return hipSuccess;
   const FfnMx4Ws L = ffn_mx4_ws_layout(M_cap, E_local, H, I);
   char* w = static_cast<char*>(ws);
@@ -324,11 +333,11 @@ hipError_t launch_ffn_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4Weigh
   const bool no_reduce = (x.src != nullptr ? std::min(x.T, M_cap) : M_cap) <= kSkHostRows;
   const MxSplit sp1{reinterpret_cast<float*>(w + L.part), L.part_cap, reinterpret_cast<int32_t*>(w + L.plan),
                     L.plan_rows, cnt + kQueueGU, cnt + kDoneGU, cnt + kTcntGU, no_reduce, xcd_state(s)};
-  hipError_t e = gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, sp1, s, rows);
+  hipError_t e = gateup_mx4(x, wg, wu, offsets, E_local, H, I, M_cap, hq, hs, sp1, s);
   if (e != hipSuccess) return e;
   const MxSplit sp2{sp1.part, sp1.part_cap, sp1.plan, sp1.plan_rows, cnt + kQueueDN, cnt + kDoneDN, cnt + kTcntDN,
                     no_reduce, sp1.xcd};
-  return gemm_mx4(hq, hs, wd, offsets, E_local, H, I, M_cap, y_perm, sp2, s, rows);
+  return gemm_mx4(hq, hs, wd, offsets, E_local, H, I, M_cap, y_perm, sp2, s);
 }
 
 }  // namespace moe

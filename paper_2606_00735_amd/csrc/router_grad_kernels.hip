@@ -17,7 +17,6 @@
 namespace moe {
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 // Fragment of 32 columns x 16 rows of a bf16 tile in LDS with 256-byte rows, for
 // an operand whose reduction dimension is the tile's row: lane (c = lane % 32, h =

@@ -36,16 +36,16 @@ def test_quantize_checks(L, x, dt, batch, rows, K, ld, rc, codes, want):
         assert L.moe_mx4_dequantize(codes, FAKE, batch, rows, K, ld, x, None) == want
 
 
-def _ffn(L, src=None, T=0, k=0, E=0, E_local=2, H=256, I=128, ldg=0, ldd=0, M=16, y=FAKE, ws=FAKE, n=1 << 40, x=FAKE):
+def _ffn(L, src=None, T=0, k=0, E_local=2, H=256, I=128, ldg=0, ldd=0, M=16, y=FAKE, ws=FAKE, n=1 << 40, x=FAKE):
     n = ctypes.c_size_t(n)
-    st = L.moe_grouped_swiglu_ffn_mx4(x, FAKE, src, T, k, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, E, E_local, H, I, ldg,
+    st = L.moe_grouped_swiglu_ffn_mx4(x, FAKE, src, T, k, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, E_local, H, I, ldg,
                                       ldd, M, y, ws, ctypes.byref(n), None)
     return st, n.value
 
 
 @pytest.mark.parametrize("args,want", [
     (dict(E_local=-1), INVALID), (dict(E_local=257), UNSUPPORTED), (dict(H=200), UNSUPPORTED), (dict(I=64), UNSUPPORTED),
-    (dict(M=-1), INVALID), (dict(E=1), INVALID), (dict(E=300), INVALID), (dict(ldg=100), INVALID), (dict(ldd=8), INVALID),
+    (dict(M=-1), INVALID), (dict(ldg=100), INVALID), (dict(ldd=8), INVALID),
     (dict(src=FAKE, T=0, k=2), INVALID), (dict(src=FAKE, T=4, k=0), INVALID), (dict(src=FAKE, T=4, k=17), INVALID),
     (dict(src=ODD, T=2 ** 25, k=1), UNSUPPORTED), (dict(src=ctypes.c_void_p(0x10002), T=4, k=1), INVALID),
     (dict(n=100), WORKSPACE), (dict(y=NULL), INVALID), (dict(x=ODD), INVALID), (dict(ws=ODD), INVALID),

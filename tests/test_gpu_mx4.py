@@ -421,5 +421,5 @@ def test_refusals():
     assert e.value.status == 3
     with pytest.raises(moe.MoeError):
         moe.moe_grouped_swiglu_ffn_mx4(t, w, w, wd, off, perm_src=torch.zeros(4, dtype=torch.int32, device=DEV), k=0)
-    with pytest.raises(moe.MoeError):
+    with pytest.raises(ValueError):
         moe.moe_grouped_swiglu_ffn_mx4(t, w, w, wd, off, experts=1)
