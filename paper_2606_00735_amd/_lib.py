@@ -539,17 +539,17 @@ def moe_balance_loss(logits, ids, mask=None, seq_len=0, ws=None, loss=None, coun
     [T, k], and the per-expert counts. Groups of seq_len tokens (0: all of them) have
     a balance loss each; mask [T] (bool or uint8, optional) marks live tokens.
     Returns (loss [2] fp32, counts [groups, E] int32, live [groups + 2] int32, ws);
-    ws starts zero-filled and may serve further calls, one at a time."""
+    ws (balance_ws_bytes of them, zero-filled at first) may serve further calls, one at
+    a time."""
     L = load_library()
     T, E = logits.shape
     k = ids.shape[1]
     if ids.shape[0] != T:
         raise ValueError("ids must be [T, k] for logits [T, E]")
     G = _groups(T, seq_len)
-    need = balance_ws_bytes(T, E, k, seq_len)
     dev = logits.device
-    if ws is None or ws.numel() < need:
-        ws = torch.zeros(need, dtype=torch.uint8, device=dev)
+    if ws is None:
+        ws = torch.zeros(balance_ws_bytes(T, E, k, seq_len), dtype=torch.uint8, device=dev)
     loss = torch.empty(2, dtype=torch.float32, device=dev) if loss is None else loss
     counts = torch.empty((G, E), dtype=torch.int32, device=dev) if counts is None else counts
     live = torch.empty(G + 2, dtype=torch.int32, device=dev) if live is None else live
@@ -627,7 +627,7 @@ def router_grad_ws_bytes(T, E, H, dtype):
 
 def moe_router_grad(dlogits, x, w_router, dx=None, dw=None, dbias=None, ws=None, need_dx=True):
     """Gradient of logits = x W^T + bias. Returns (dx [T, H] of x's type or None with
-    need_dx=False, dw [E, H] fp32, dbias [E] fp32, ws)."""
+    need_dx=False, dw [E, H] fp32, dbias [E] fp32, ws); ws has router_grad_ws_bytes."""
     L = load_library()
     T, H = x.shape
     E = w_router.shape[0]
@@ -635,9 +635,8 @@ def moe_router_grad(dlogits, x, w_router, dx=None, dw=None, dbias=None, ws=None,
         raise ValueError("w_router must be [E, H] with the dtype of x, and dlogits [T, E]")
     dt = _dtype_code(x)
     dev = x.device
-    need = router_grad_ws_bytes(T, E, H, x.dtype)
-    if ws is None or ws.numel() < need:
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    if ws is None:
+        ws = torch.empty(router_grad_ws_bytes(T, E, H, x.dtype), dtype=torch.uint8, device=dev)
     if not need_dx:
         dx = None
     elif dx is None:
@@ -912,23 +911,21 @@ class Mx4Tensor:
     def __init__(self, codes, scales, K):
         if codes.dtype != torch.uint8 or scales.dtype != torch.int32:
             raise ValueError("MXFP4 codes are uint8 and scales int32")
-        C = mx4_chunks(K)
-        if K < 1 or K % 32 or codes.dim() not in (2, 3) or codes.shape[-1] != 128 * C:
+        lead, C = tuple(codes.shape), (K + 255) // 256
+        if K < 1 or K % 32 or len(lead) not in (2, 3) or lead[-1] != 128 * C:
             raise ValueError("codes must be [R, 128 C] or [B, R, 128 C], C = ceil(K / 256), K a multiple of 32")
-        R = codes.shape[-2]
-        if tuple(scales.shape) != tuple(codes.shape[:-2]) + (C, R, 2):
+        R = lead[-2]
+        if tuple(scales.shape) != lead[:-2] + (C, R, 2):
             raise ValueError("scales must be [.., C, R, 2] for codes [.., R, 128 C]")
         if scales.device != codes.device:
             raise ValueError("codes and scales must be on one device")
-        ld = codes.stride(-2) if R > 1 and codes.numel() > 0 else 128 * C
-        if codes.numel() > 0 and (codes.stride(-1) != 1 or ld < 128 * C or
-                                  (codes.dim() == 3 and codes.shape[0] > 1 and codes.stride(0) != R * ld)):
-            raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
+        ld = 128 * C
+        if not codes.is_contiguous():
+            ld = codes.stride(-2) if R > 1 else 128 * C
+            if codes.stride(-1) != 1 or ld < 128 * C or (len(lead) == 3 and lead[0] > 1 and codes.stride(0) != R * ld):
+                raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
         self.codes, self.scales, self.K, self.ld = codes, scales, K, ld
-
-    @property
-    def shape(self):
-        return tuple(self.codes.shape[:-1]) + (self.K,)
+        self.shape = lead[:-1] + (K,)
 
 
 def moe_mx4_quantize(x, out=None, row_count=None, ld=None):

@@ -96,7 +96,7 @@ template <int EP, bool VEC>
 __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
   using St = RgStage<EP>;
   constexpr int W = 8, WE = EP / 32, WC = W / WE;       // waves along experts, columns
-  constexpr int MI = 1, NJ = kRgCols / (32 * WC);       // 32 x 32 blocks of a wave
+  constexpr int NJ = kRgCols / (32 * WC);               // 32 x 32 blocks of a wave
   constexpr int WCOLS = kRgCols / WC;
   __shared__ __align__(16) bf16_t smem[St::BYTES * St::NS / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -110,87 +110,87 @@ __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
 
   // Direct loads. dz: 1 KB of a stage per instruction, 16 bytes a lane (VEC) or 256
   // bytes, 4 a lane; columns past E read the row's last ones. x: 4 rows of 256
-  // bytes; columns past H read the row's last ones.
+  // bytes; columns past H read the row's last ones. Rows past T read the last.
   constexpr int DL = VEC ? 16 : 4, ND = St::DZ / (64 * DL * W), NX = kRgTok * kRgCols * 2 / (1024 * W);
   constexpr int LOADS = ND + NX;
-  auto issue = [&](int q, bool live, bf16_t* st, int) {
-    const int t0 = (live ? q0 + q : q1 - 1) * kRgTok;
+  static_assert(LOADS * (St::NS - 2) < 64, "loads that a wait counts");
+  uint32_t dcol[ND], xcol[NX];
+#pragma unroll
+  for (int i = 0; i < ND; ++i) dcol[i] = (uint32_t)min(((i * W + wave) * 64 + lane) * DL % (EP * 4), E * 4 - DL);
+#pragma unroll
+  for (int i = 0; i < NX; ++i)
+    xcol[i] = (uint32_t)min(c0 + tr_swizzle((i * W + wave) * 4 + lane / 16, lane % 16) * 8, H - 8) * 2u;
+  auto issue = [&](int q, bool live, bf16_t* st, int part) {
+    if (part > 0) return;  // all at once
+    const int t0 = (live ? q0 + q : q1 - 1) * kRgTok, last = a.T - 1 - t0;
+    const void* dz = uniform_ptr(a.dz + (size_t)t0 * E);
+    const void* x = uniform_ptr(a.x + (size_t)t0 * H);
+    const uint32_t lds = lds_addr(st);
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int byte = ((i * W + wave) * 64 + lane) * DL;
-      const int row = byte / (EP * 4), e = min((byte % (EP * 4)) / 4, E - DL / 4);
-      const int t = min(t0 + row, a.T - 1);
-      const float* p = a.dz + (size_t)t * E + e;
-      const bf16_t* dst = st + (i * W + wave) * 64 * DL / 2;
+      const int row = ((i * W + wave) * 64 + lane) * DL / (EP * 4);
+      const uint32_t off = (uint32_t)min(row, last) * (uint32_t)(E * 4) + dcol[i];
       if (VEC)
-        dma16(p, dst);
+        dma16a(dz, off, lds + (i * W + wave) * 64 * DL);
       else
-        dma4(p, dst);
+        dma4a(dz, off, lds + (i * W + wave) * 64 * DL);
     }
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
-      const int row = (i * W + wave) * 4 + lane / 16, t = min(t0 + row, a.T - 1);
-      const int c = min(c0 + tr_swizzle(row, lane % 16) * 8, H - 8);
-      const bf16_t* p = a.x + (size_t)t * H + c;
-      dma16(p, st + (St::DZ + (i * W + wave) * 1024) / 2);
+      const int row = (i * W + wave) * 4 + lane / 16;
+      dma16a(x, (uint32_t)min(row, last) * (uint32_t)(H * 2) + xcol[i], lds + St::DZ + (i * W + wave) * 1024);
     }
   };
 
-  f32x16_t acc[1][MI][NJ];
-  float db[MI];
+  f32x16_t acc[NJ];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    db[i] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[0][i][j] = f32x16_t{};
-  }
-  int q = q0;
-  auto compute = [&](bf16_t* st) {
-    char* base = reinterpret_cast<char*>(st);
-    const int left = a.T - q * kRgTok;  // tokens of this chunk
-    if (left < kRgTok) {
-      // past the last token: zeros, so that they add nothing
-      for (int i = left * EP + threadIdx.x; i < kRgTok * EP; i += W * kWave) reinterpret_cast<float*>(base)[i] = 0.0f;
-      for (int i = left * 64 + threadIdx.x; i < kRgTok * 64; i += W * kWave)
-        reinterpret_cast<uint32_t*>(base + St::DZ)[i] = 0;
-      wait_lgkmcnt0();
-      lds_barrier();
-    }
-    ++q;
+  for (int j = 0; j < NJ; ++j) acc[j] = f32x16_t{};
+  float db = 0.0f;
+  const int e_lane = wm * 32 + r32;  // this lane's expert
+  // Raw operands of a 16-token step are read one step ahead, across chunks too
+  // (pipeline_xk); a step cuts its dz values and multiplies.
+  float f[2][8];
+  bf16x8_t xf[2][NJ];
+  auto read = [&](const bf16_t* st, int s, int buf) {
+    const char* base = reinterpret_cast<const char*>(st);
     const float* dz = reinterpret_cast<const float*>(base);
 #pragma unroll
-    for (int s = 0; s < kRgTok / 16; ++s) {
-      bf16x8_t xf[NJ];
+    for (int k = 0; k < 8; ++k) f[buf][k] = dz[(16 * s + 8 * h + k) * EP + e_lane];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) xf[j] = tr_frag(base + St::DZ, lane, 16 * s, wn * WCOLS + j * 32);
+    for (int j = 0; j < NJ; ++j) xf[buf][j] = tr_frag(base + St::DZ, lane, 16 * s, wn * WCOLS + j * 32);
+  };
+  int left = a.T - q0 * kRgTok;  // tokens from the present step on
+  auto mma = [&](int s) {
+    const int buf = s & 1;
+    if (left < 16) {
+      // past the last token: zeros on both sides, so that they add nothing
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        float f[8];
+      for (int k = 0; k < 8; ++k) f[buf][k] = 8 * h + k < left ? f[buf][k] : 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = dz[(16 * s + 8 * h + k) * EP + (wm * MI + i) * 32 + r32];
-        if (tile == 0)
-          db[i] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-        bf16x8_t zf[3];
-        split8<3>(f, zf);
+      for (int j = 0; j < NJ; ++j) {
+        u32x4_t v = __builtin_bit_cast(u32x4_t, xf[buf][j]);
 #pragma unroll
-        for (int n = 0; n < 3; ++n)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            acc[0][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[j], zf[n], acc[0][i][j], 0, 0, 0);
+        for (int k = 0; k < 4; ++k)
+          v[k] &= (8 * h + 2 * k < left ? 0xffffu : 0u) | (8 * h + 2 * k + 1 < left ? 0xffff0000u : 0u);
+        xf[buf][j] = __builtin_bit_cast(bf16x8_t, v);
       }
     }
-    wait_lgkmcnt0();  // every read of this stage returned before it is refilled
+    left -= 16;
+    if (tile == 0)
+      db += ((f[buf][0] + f[buf][1]) + (f[buf][2] + f[buf][3])) + ((f[buf][4] + f[buf][5]) + (f[buf][6] + f[buf][7]));
+    bf16x8_t zf[3];
+    split8<3>(f[buf], zf);
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[buf][j], zf[n], acc[j], 0, 0, 0);
   };
-  pipeline<St::NS, LOADS>(
-      q1 - q0, smem, St::BYTES / 2, [&](int c, bool live, bf16_t* st) { issue(c, live, st, 0); }, compute);
+  pipeline_xk<St::NS, LOADS, kRgTok / 16>(q1 - q0, smem, St::BYTES / 2, issue, read, mma, [] {});
 
   if (tile == 0 && wn == 0) {
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const float s = db[i] + __shfl_xor(db[i], 32, kWave);
-      const int e = (wm * MI + i) * 32 + r32;
-      if (h == 0 && e < E) a.db[(size_t)sp * E + e] = s;
-    }
+    const float s = db + __shfl_xor(db, 32, kWave);
+    if (h == 0 && e_lane < E) a.db[(size_t)sp * E + e_lane] = s;
   }
   // rows of the tile are experts; columns past H (64 of the last tile's: H % 64 ==
   // 0) are not stored. At most 64 columns of a wave at a time go through LDS.
@@ -198,12 +198,12 @@ __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
   static_assert(W * 32 * EC * 4 <= St::BYTES * St::NS, "the epilogue's LDS");
 #pragma unroll
   for (int j0 = 0; j0 < NJ; j0 += NE) {
-    f32x16_t part[1][MI][NE];
+    f32x16_t part[1][1][NE];
 #pragma unroll
-    for (int j = 0; j < NE; ++j) part[0][0][j] = acc[0][0][j0 + j];
+    for (int j = 0; j < NE; ++j) part[0][0][j] = acc[j0 + j];
     const int c = c0 + wn * WCOLS + j0 * 32;
-    split_epilogue<MI, NE, 1, MI * 32, EC>(part, smem, 0, c < H ? E : 0, c, H, wm, 0, wave, lane,
-                                           a.dw + (size_t)sp * E * H, 0, false);
+    split_epilogue<1, NE, 1, 32, EC>(part, smem, 0, c < H ? E : 0, c, H, wm, 0, wave, lane,
+                                     a.dw + (size_t)sp * E * H, 0, false);
   }
 }
 

@@ -67,3 +67,78 @@ def test_ffn_workspace_query(L):
 ])
 def test_gemm_checks(L, N, K, ldb, M, c, want):
     assert L.moe_grouped_gemm_mx4(FAKE, FAKE, FAKE, FAKE, FAKE, 1, N, K, ldb, M, c, None) == want
+
+
+# ---------------------------------------------------------------- the router's training step
+def _loss(L, T=64, E=8, k=2, seq=0, z=FAKE, ids=FAKE, mask=NULL, loss=FAKE, counts=FAKE, live=FAKE, ws=FAKE, n=1 << 40):
+    n = ctypes.c_size_t(n)
+    return L.moe_balance_loss(z, ids, mask, T, E, k, seq, loss, counts, live, ws, ctypes.byref(n), None), n.value
+
+
+@pytest.mark.parametrize("args,want", [
+    (dict(T=-1), INVALID), (dict(E=0), INVALID), (dict(E=257), INVALID), (dict(k=0), INVALID), (dict(k=9), INVALID),
+    (dict(E=32, k=17), INVALID), (dict(seq=-1), INVALID), (dict(seq=5), INVALID), (dict(T=2 ** 31 - 1, k=2), UNSUPPORTED),
+    (dict(T=2 ** 24, seq=1), UNSUPPORTED), (dict(n=16), WORKSPACE), (dict(z=NULL), INVALID), (dict(z=ODD), INVALID),
+    (dict(ids=ctypes.c_void_p(2)), INVALID), (dict(loss=NULL), INVALID), (dict(counts=NULL), INVALID),
+    (dict(live=NULL), INVALID), (dict(ws=ODD), INVALID), (dict(T=0, loss=NULL), INVALID),
+])
+def test_balance_loss_checks(L, args, want):
+    assert _loss(L, **args)[0] == want
+
+
+def test_balance_loss_workspace_query(L):
+    for T, E, k, seq in ((0, 8, 2, 0), (64, 8, 2, 0), (16384, 256, 8, 4096), (5000, 60, 4, 1)):
+        st, n = _loss(L, T=T, E=E, k=k, seq=seq, ws=NULL)
+        assert st == 0 and n >= 256 and n % 256 == 0
+        assert _loss(L, T=T, E=E, k=k, seq=seq, n=n - 1)[0] == WORKSPACE
+
+
+def _gate(L, T=64, E=8, k=2, seq=0, z=FAKE, w=NULL, dw=NULL, dz=FAKE, live=FAKE):
+    return L.moe_gate_backward(z, FAKE, NULL, FAKE, live, FAKE, w, dw, T, E, k, seq, dz, None)
+
+
+@pytest.mark.parametrize("args,want", [
+    (dict(T=-1), INVALID), (dict(k=9), INVALID), (dict(seq=7), INVALID), (dict(w=FAKE), INVALID), (dict(dw=FAKE), INVALID),
+    (dict(z=NULL), INVALID), (dict(z=ODD), INVALID), (dict(dz=NULL), INVALID), (dict(dz=ODD), INVALID),
+    (dict(live=NULL), INVALID), (dict(T=2 ** 24, seq=1), UNSUPPORTED), (dict(T=0, z=NULL, dz=NULL), 0),
+])
+def test_gate_backward_checks(L, args, want):
+    assert _gate(L, **args) == want
+
+
+def _combine(L, T=4, k=2, H=64, M=8, dt=1, do=FAKE, y=FAKE, w=FAKE, dw=FAKE, dy=FAKE):
+    return L.moe_combine_backward(do, y, w, FAKE, T, k, H, M, dt, dw, dy, None)
+
+
+@pytest.mark.parametrize("args,want", [
+    (dict(T=-1), INVALID), (dict(k=0), INVALID), (dict(k=17), INVALID), (dict(H=0), INVALID), (dict(H=12), INVALID),
+    (dict(H=6, dt=0), INVALID), (dict(M=-1), INVALID), (dict(dt=5), INVALID), (dict(T=2 ** 30, k=4), UNSUPPORTED),
+    (dict(do=NULL), INVALID), (dict(y=NULL), INVALID), (dict(w=NULL), INVALID), (dict(dw=NULL), INVALID),
+    (dict(do=ODD), INVALID), (dict(y=ODD), INVALID), (dict(dy=ODD), INVALID), (dict(T=0, do=NULL), 0),
+])
+def test_combine_backward_checks(L, args, want):
+    assert _combine(L, **args) == want
+
+
+def _router(L, T=4, E=8, H=64, dt=1, dz=FAKE, x=FAKE, w=FAKE, dx=FAKE, dw=FAKE, db=FAKE, ws=FAKE, n=1 << 40):
+    n = ctypes.c_size_t(n)
+    return L.moe_router_grad(dz, x, w, T, E, H, dt, dx, dw, db, ws, ctypes.byref(n), None), n.value
+
+
+@pytest.mark.parametrize("args,want", [
+    (dict(T=-1), INVALID), (dict(E=0), INVALID), (dict(E=257), INVALID), (dict(H=0), INVALID), (dict(H=60), INVALID),
+    (dict(H=72), UNSUPPORTED), (dict(H=(1 << 20) + 64), UNSUPPORTED), (dict(dt=3), INVALID), (dict(n=16), WORKSPACE),
+    (dict(dz=NULL), INVALID), (dict(x=NULL), INVALID), (dict(w=NULL), INVALID), (dict(dw=NULL), INVALID),
+    (dict(db=NULL), INVALID), (dict(dz=ODD), INVALID), (dict(x=ODD), INVALID), (dict(dx=ODD), INVALID),
+    (dict(dw=ODD), INVALID), (dict(ws=ODD), INVALID),
+])
+def test_router_grad_checks(L, args, want):
+    assert _router(L, **args)[0] == want
+
+
+def test_router_grad_workspace_query(L):
+    st, n = _router(L, T=16384, E=256, H=7168, ws=NULL)
+    assert st == 0 and n >= 2 * 256 * 7168 * 4  # at least two ranges of tokens
+    assert _router(L, T=16384, E=256, H=7168, n=n - 1)[0] == WORKSPACE
+    st, n = _router(L, T=8, ws=NULL)
+    assert st == 0 and n == 256
