@@ -269,12 +269,17 @@ __device__ __forceinline__ void pipeline(int nK, bf16_t* smem, int stage_elems, 
 // its MFMAs wait behind them. part < 0 asks for all parts at once (prologue). A
 // consumer whose loads all leave in part 0 (the router, two-stage tiles, MXFP8
 // on 8 waves) does nothing for the others.
-template <int NS, int LOADS, int KS, bool MMA_FIRST = false, class Issue, class Read, class Mma, class Mix>
+//
+// DRAIN = false leaves what the wave has in flight (a tile's stores) in the count:
+// it is older than the loads, so the waits only take longer, and the first loads
+// need not wait for it.
+template <int NS, int LOADS, int KS, bool MMA_FIRST = false, bool DRAIN = true, class Issue, class Read, class Mma,
+          class Mix>
 __device__ __forceinline__ void pipeline_xk(int nK, bf16_t* smem, int stage_elems, Issue&& issue, Read&& read,
                                             Mma&& mma, Mix&& mix) {
   static_assert(NS >= 2 && NS <= 8, "stages");
   static_assert(KS >= 2 && KS % 2 == 0, "k-steps per chunk");
-  wait_vmcnt<0>();  // nothing older (e.g. a previous tile's stores) is left in the count
+  if (DRAIN) wait_vmcnt<0>();  // nothing older (e.g. a previous tile's stores) is left in the count
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) issue(i, i < nK, smem + i * stage_elems, -1);
   wait_vmcnt<LOADS * (NS - 2)>();  // chunk 0 landed

@@ -916,7 +916,7 @@ __device__ __forceinline__ void gemm_tile_mx4(const GemmArgs& a, bf16_t* smem, i
     if (NMFMA > PAIRS) __builtin_amdgcn_sched_group_barrier(0x008, NMFMA - PAIRS, 0);
     if (NREAD > PAIRS) __builtin_amdgcn_sched_group_barrier(0x100, NREAD - PAIRS, 0);
   };
-  pipeline_xk<St::NS, St::LOADS, KS, true>(kc1 - kc0, smem, St::STAGE / 2, issue, read, mma, mix);
+  pipeline_xk<St::NS, St::LOADS, KS, true, false>(kc1 - kc0, smem, St::STAGE / 2, issue, read, mma, mix);
 
   if (SPLIT) {
     split_epilogue<MI, NI, NB, WM, WN, COH>(acc, smem, m0, m_end, pcol0, pld, wm, wn, wave, lane, pbase, pstride,
@@ -1436,17 +1436,31 @@ __device__ __forceinline__ void tile_rc(int local, int n_mt, int n_nt, int& mt, 
   }
 }
 
-// UNI: `tile` is the same in every lane of the wave.
-template <bool UNI = true>
+// UNI: `tile` is the same in every lane of the wave. WIDE: the search by all lanes at
+// once instead of by bisection (needs UNI).
+template <bool UNI = true, bool WIDE = false>
 __device__ __forceinline__ TileRef decode_tile(int tile, int E, const int* s_start, const int* s_row0,
                                                const int* s_rows, int cols, int N) {
   auto uni = [](int v) { return UNI ? uniform_int(v) : v; };
   // last expert whose first tile is <= tile (experts with no tiles share
   // their start with the next one, so the last match is the owner)
-  int lo = 0, hi = E - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (uni(s_start[mid]) <= tile) lo = mid; else hi = mid - 1;
+  int lo = 0;
+  if constexpr (WIDE) {
+    static_assert(UNI, "one tile a wave");
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+#pragma unroll
+    for (int q = 0; q < kMaxExperts / kWave; ++q) {
+      const int e = q * kWave + lane;
+      n += (int)__popcll(__ballot(e < E && s_start[e] <= tile));
+    }
+    lo = uni(n) - 1;
+  } else {
+    int hi = E - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (uni(s_start[mid]) <= tile) lo = mid; else hi = mid - 1;
+    }
   }
   TileRef t;
   t.e = lo;
@@ -1656,7 +1670,7 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
     const int t = (int)sk_div(u, nK);
     const int kc0 = (int)(u - (long long)t * nK);
     const int kc1 = (int)min((long long)nK, kc0 + (u_end - u));
-    const TileRef tr = decode_tile(t, a.E_local, s_start, s_row0, s_rows, cols, a.N);
+    const TileRef tr = decode_tile<true, F == kMx4>(t, a.E_local, s_start, s_row0, s_rows, cols, a.N);
     const int cls = tile_class(tr.left);
     if (kc0 == 0 && kc1 == nK) {
       if constexpr (!DUAL) {
@@ -1887,7 +1901,7 @@ __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
       ps = St * tsz;
       pld = cols;
     } else {
-      t = decode_tile(item, E, s_start, s_row0, s_rows, cols, a.N);
+      t = decode_tile<true, F == kMx4>(item, E, s_start, s_row0, s_rows, cols, a.N);
     }
     const int cls = tile_class(t.left);
     if constexpr (!DUAL) {
