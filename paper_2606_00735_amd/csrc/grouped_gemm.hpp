@@ -1534,6 +1534,14 @@ __device__ __forceinline__ void mx4_quant_store4(const GemmArgs& a, float h0, fl
 // ld_coh4). Which of the two does not change a bit of the results.
 // ---------------------------------------------------------------------------
 constexpr int kSkMinChunks = 2;  // K chunks per block share, at least (when the launch has as many)
+// The same for MXFP4 launches with an expert of more than kSkPrefRows rows, and of
+// more than kSmallM: a K loop a quarter as long is cut into fewer shares, and the sums
+// that a cut moves grow with the rows. FFN us with 2 / 4 / 8 chunks at least, one
+// expert, H = 7168, I = 2048: 1 row 20.6 / 20.3 / 25, 17 rows 25.7 / 23.5 / 27.2, 64 rows
+// 37.4 / 30.9 / 31.8, 128 rows 52.7 / 43.5 / 42.5; H = 4096, I = 14336: 100 rows 60.8 /
+// 60.8 / 52.4; H = 2048, I = 768: 8 experts of 1 row 21.9 / 23.1 / 28.3, 16 of 20 rows
+// 32.3 / 28.5 / 24.5, 4 of 24 rows 25.1 / 26.5 / 29.7.
+constexpr int kSkMinChunksMx4 = 4, kSkMinChunksMx4Big = 8;
 // Largest expert for which the decode schedule is preferred when a
 // reduction launch follows anyway (same-process A/B, one to eight
 // Mixtral-shaped experts: faster up to 13-16 rows, 3-10 % slower at 29-32).
@@ -1555,8 +1563,8 @@ struct SkPart {
   // the block whose share holds unit x
   __device__ int block_of(long long x) const { return b0 + (int)(sk_div((x - u0 + 1) * Ga + U - 1, U) - 1); }
 };
-__device__ __forceinline__ long long sk_blocks(long long U, long long G) {
-  return max(1LL, min(G, U / kSkMinChunks));  // every block with work takes >= kSkMinChunks
+__device__ __forceinline__ long long sk_blocks(long long U, long long G, int min_chunks) {
+  return max(1LL, min(G, U / min_chunks));  // every block with work takes >= min_chunks
 }
 
 // Sum of the nc contributors' slots of a split tile (rows [m0, m_end) of C,
@@ -1626,7 +1634,8 @@ __device__ __forceinline__ void sk_fixup(const GemmArgs& a, int m0, int m_end, i
 // halves the tiles, and so the pipeline fills, of short-K launches.
 template <int W, bool DUAL, int F>
 __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem, int T0, const int* s_start,
-                                                const int* s_row0, const int* s_rows, bool xcd_ok, bool wide) {
+                                                const int* s_row0, const int* s_rows, bool xcd_ok, bool wide,
+                                                int min_chunks) {
   constexpr int NB = DUAL ? 2 : 1;
   const int cols = wide ? 256 : 128;
   __shared__ int s_last;
@@ -1638,7 +1647,7 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
   // T0 * 8 stays far inside int: T0 <= E_local * N / 128 here
   SkPart P;
   P.U = (long long)T0 * nK;
-  P.Ga = sk_blocks(P.U, G);
+  P.Ga = sk_blocks(P.U, G, min_chunks);
   P.u0 = 0;
   P.b0 = 0;
   // per XCD when the tiles divide evenly over the XCDs (shares then differ
@@ -1650,7 +1659,7 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
     float big = 0.0f;
     for (int x = 0; x < 8; ++x) {
       const long long ux = (long long)((T0 * (x + 1) >> 3) - (T0 * x >> 3)) * nK;
-      if (ux > 0) big = fmaxf(big, ceilf((float)ux / (float)sk_blocks(ux, gx)));
+      if (ux > 0) big = fmaxf(big, ceilf((float)ux / (float)sk_blocks(ux, gx, min_chunks)));
     }
     per_xcd = big <= ceilf((float)P.U / (float)P.Ga) + 1.0f;
   }
@@ -1658,7 +1667,7 @@ __device__ __forceinline__ void decode_schedule(const GemmArgs& a, bf16_t* smem,
     const int x = b & 7;
     const long long t_lo = T0 * x >> 3, t_hi = T0 * (x + 1) >> 3;
     P.U = (t_hi - t_lo) * nK;
-    P.Ga = sk_blocks(P.U, gx);
+    P.Ga = sk_blocks(P.U, gx, min_chunks);
     P.u0 = t_lo * nK;
     P.b0 = x * gx;
   }
@@ -1781,6 +1790,8 @@ __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
     // With fewer tiles, wider ones only split more (one expert: up to 70 %
     // slower)
     const bool dwide = !DUAL && (a.N % 256) == 0 && T0 / 2 >= G;
+    const int min_chunks = F != kMx4 ? kSkMinChunks
+                                     : (n_big > 0 ? kSkMinChunksMx4Big : (sc.n_pref > 0 ? kSkMinChunksMx4 : kSkMinChunks));
     if (tid < E) s_start[tid] = dwide ? sc.tiles0 / 2 : sc.tiles0;
     if (tid == 0) s_xcd = xcd;
     if (blockIdx.x == 0 && tid == 0 && a.plan != nullptr) {
@@ -1788,7 +1799,8 @@ __device__ __forceinline__ void grouped_gemm_body(const GemmArgs& a) {
       a.plan[2] = 1;
     }
     __syncthreads();
-    decode_schedule<W, DUAL, F>(a, smem, dwide ? T0 / 2 : T0, s_start, s_row0, s_rows, uniform_int(s_xcd) == 1, dwide);
+    decode_schedule<W, DUAL, F>(a, smem, dwide ? T0 / 2 : T0, s_start, s_row0, s_rows, uniform_int(s_xcd) == 1, dwide,
+                                min_chunks);
     return;
   }
 
