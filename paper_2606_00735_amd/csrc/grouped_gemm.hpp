@@ -472,6 +472,14 @@ __device__ __forceinline__ f32x16_t mfma_mx4(int q, uint4 b, uint4 a, f32x16_t a
   }
 }
 
+// 16 x 16 x 128: lane (r, g), g = lane / 16, supplies 32 consecutive elements of row r
+// and their code in byte q of its scale register.
+template <int Q>
+__device__ __forceinline__ f32x4_t mfma_mx4_16(uint4 b, uint4 a, f32x4_t acc, uint32_t sb, uint32_t sa) {
+  auto f4 = [](uint4 v) { return int32x8_t{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0}; };
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f4(b), f4(a), acc, 4, 4, Q, (int)sb, Q, (int)sa);
+}
+
 // The scale code of block `col / 32` of h row `row`. The last chunk of a row of
 // an odd number of 128 columns is half empty: its other four blocks get code 0
 // (any finite code: the other operand of the product that reads them holds
@@ -1540,7 +1548,8 @@ constexpr int kSkMinChunks = 2;  // K chunks per block share, at least (when the
 // expert, H = 7168, I = 2048: 1 row 20.6 / 20.3 / 25, 17 rows 25.7 / 23.5 / 27.2, 64 rows
 // 37.4 / 30.9 / 31.8, 128 rows 52.7 / 43.5 / 42.5; H = 4096, I = 14336: 100 rows 60.8 /
 // 60.8 / 52.4; H = 2048, I = 768: 8 experts of 1 row 21.9 / 23.1 / 28.3, 16 of 20 rows
-// 32.3 / 28.5 / 24.5, 4 of 24 rows 25.1 / 26.5 / 29.7.
+// 32.3 / 28.5 / 24.5, 4 of 24 rows 25.1 / 26.5 / 29.7. (Launches of at most 128 rows
+// and 128 MB of weights have a kernel of their own.)
 constexpr int kSkMinChunksMx4 = 4, kSkMinChunksMx4Big = 8;
 // Largest expert for which the decode schedule is preferred when a
 // reduction launch follows anyway (same-process A/B, one to eight

@@ -226,6 +226,173 @@ __global__ __launch_bounds__(256) void split_reduce_mx4_kernel(GemmArgs a) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// The FFN of few rows (a token's experts): latency. No LDS ring, no partial sums
+// across blocks: a block takes 16 rows of an expert by 64 weight rows (32 columns of
+// gate and up, or 64 of down), its 8 waves 32 weight rows x a quarter of K each,
+// straight from memory to the operand registers of the 16 x 16 x 128 MFMA, kFewBatch
+// chunks of a row in flight; the quarters' sums meet in LDS, in order. Every wave
+// finds the block's expert itself, from the offsets.
+//
+// Bound by the latency of offsets, rows and weights, one after the other, about 5 us a
+// launch; by the load path of the CUs that have a block when there are few; by memory
+// from some 100 MB on, where the decode schedule's ring keeps more in flight. FFN us
+// (bytes of the gate/up codes), the decode schedule / this: H = 2048, I = 768, 8 experts
+// of 1 row (13 MB) 22.4 / 11.0, 32 of 2 (50 MB) 28.1 / 23.5, 64 of 1 (101 MB) 45.4 /
+// 43.7, 128 of 8 (201 MB) 81 / 84, 16 of 64 29.5 / 45.2; H = 7168, I = 2048, 1 of 1
+// (15 MB) 21.0 / 16.9, 1 of 64 31.4 / 24.0, 1 of 128 43.4 / 40.1, 8 of 1 (117 MB) 52.6 /
+// 45.7, 8 of 14 57.8 / 64.5, 32 of 4 (470 MB) 153 / 166; H = 4096, I = 14336, 1 of 1 (59
+// MB) 32.2 / 33.0, 2 of 60 62.9 / 171, 8 of 8 (470 MB) 146 / 175. Two chunks in flight instead of four: 17.3 for 16.9, 46.1
+// for 45.7.
+// ---------------------------------------------------------------------------
+constexpr int kFewTile = 16;   // rows of a tile
+constexpr int kFewSplit = 4;   // parts of K
+constexpr int kFewBatch = 4;   // chunks in flight a wave
+
+// Sum of x over this lane and the lanes below.
+__device__ __forceinline__ int lane_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the next row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper 32
+  return x;
+}
+
+template <bool DUAL>
+__global__ __launch_bounds__(8 * kWave, 2) void mx4_few_rows_kernel(GemmArgs a) {
+  constexpr int COLS = DUAL ? 32 : 64, Q = kMaxExperts / kWave;
+  __shared__ f32x4_t s_sum[8][2][kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = wave & 1, ks = wave >> 1;  // columns, part of K
+  const int r16 = lane & 15, g = lane >> 4;
+  const int E = a.E_local, N = a.N, K = a.K, nK = K / kMxChunk;
+
+  // row tiles of the experts up to lane's (q * 64 + lane), clamped as in grouped_gemm_body
+  int row0[Q], rows[Q], upto[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int e = q * kWave + lane;
+    const int o0 = a.offsets[min(e, E)], o1 = a.offsets[min(e + 1, E)];
+    row0[q] = min(max(o0, 0), a.M_cap);
+    rows[q] = e < E ? min(max(o1, row0[q]), a.M_cap) - row0[q] : 0;
+  }
+  int total = 0;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    upto[q] = total + lane_prefix((rows[q] + kFewTile - 1) / kFewTile);
+    total = __builtin_amdgcn_readlane(upto[q], kWave - 1);
+  }
+  const unsigned ct = (unsigned)N / COLS;
+  const bool gather = a.a_src != nullptr;
+  const size_t sa_rows = gather ? (size_t)a.a_T : (size_t)a.M_cap;
+  for (unsigned item = blockIdx.x; item < (unsigned)total * ct; item += gridDim.x) {
+    const int j = uniform_int((int)(item / ct)), n0 = (int)(item - (unsigned)j * ct) * COLS;
+    int e = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) e += (int)__popcll(__ballot(upto[q] <= j));
+    e = uniform_int(e);
+    int m0 = 0, n_rows = 0, before = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      if (e / kWave == q) {
+        m0 = __builtin_amdgcn_readlane(row0[q], e % kWave);
+        n_rows = __builtin_amdgcn_readlane(rows[q], e % kWave);
+        before = __builtin_amdgcn_readlane(upto[q], e % kWave) - (n_rows + kFewTile - 1) / kFewTile;
+      }
+    const int skip = (j - before) * kFewTile;
+    m0 += skip, n_rows = min(n_rows - skip, kFewTile);
+
+    // Piece 4 t + g of a row's chunk for k-step t; its scale is byte 2 t + g / 2 of
+    // dword g % 2.
+    const int m = m0 + min(r16, n_rows - 1);
+    const int row = gather ? min(max(a.a_src[m] / a.a_div, 0), a.a_T - 1) : m;
+    const uint32_t offB = (uint32_t)(r16 * a.ldb + g * 16), offSB = (uint32_t)(r16 * 2 + (g & 1));
+    const char *B[2], *A = reinterpret_cast<const char*>(a.A) + (size_t)row * K + g * 16;
+    const uint32_t *SB[2], *SA = a.As + (size_t)row * 2 + (g & 1);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const size_t n = n0 + (DUAL ? cg * 16 : cg * 32 + b * 16);
+      B[b] = reinterpret_cast<const char*>(DUAL && b ? a.B1 : a.B0) + ((size_t)e * N + n) * a.ldb;
+      SB[b] = (DUAL && b ? a.Bs1 : a.Bs0) + ((size_t)e * nK * N + n) * 2;
+    }
+    f32x4_t acc[2] = {f32x4_t{}, f32x4_t{}};
+    const int c_end = (ks + 1) * nK / kFewSplit;
+#pragma unroll 1
+    for (int c = ks * nK / kFewSplit; c < c_end; c += kFewBatch) {
+      uint4 w[kFewBatch][2][2], x[kFewBatch][2];
+      uint32_t sw[kFewBatch][2], sx[kFewBatch];
+#pragma unroll
+      for (int u = 0; u < kFewBatch; ++u) {
+        const size_t cc = (size_t)min(c + u, c_end - 1);  // past the part: a repeated, unused load
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) w[u][b][t] = *reinterpret_cast<const uint4*>(B[b] + cc * 128 + t * 64 + offB);
+          sw[u][b] = SB[b][cc * N * 2 + offSB];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) x[u][t] = *reinterpret_cast<const uint4*>(A + cc * 128 + t * 64);
+        sx[u] = SA[cc * sa_rows * 2];
+      }
+#pragma unroll
+      for (int u = 0; u < kFewBatch; ++u) {
+        if (c + u >= c_end) break;
+        const uint32_t sa = sx[u] >> (8 * (g >> 1));
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint32_t sb = sw[u][b] >> (8 * (g >> 1));
+          acc[b] = mfma_mx4_16<0>(w[u][b][0], x[u][0], acc[b], sb, sa);
+          acc[b] = mfma_mx4_16<2>(w[u][b][1], x[u][1], acc[b], sb, sa);
+        }
+      }
+    }
+    // lane (r, g) holds columns 4 g + (0..3) of row r
+    s_sum[wave][0][lane] = acc[0];
+    s_sum[wave][1][lane] = acc[1];
+    __syncthreads();
+    auto sum = [&](int half, int b, int at) {
+      f32x4_t s = s_sum[half][b][at];
+#pragma unroll
+      for (int p = 1; p < kFewSplit; ++p) s += s_sum[p * 2 + half][b][at];
+      return s;
+    };
+    if constexpr (DUAL) {
+      const int r = tid >> 3, c4 = tid & 7, at = (c4 & 3) * 16 + r;
+      if (r < n_rows) {
+        const f32x4_t gt = sum(c4 >> 2, 0, at), up = sum(c4 >> 2, 1, at);
+        mx4_quant_store4(a, silu_mul_fast(gt[0], up[0]), silu_mul_fast(gt[1], up[1]), silu_mul_fast(gt[2], up[2]),
+                         silu_mul_fast(gt[3], up[3]), m0 + r, n0 + c4 * 4);
+      }
+    } else {
+      const int r = tid >> 4, c4 = tid & 15;
+      if (r < n_rows) {
+        const f32x4_t v = sum(c4 >> 3, (c4 >> 2) & 1, (c4 & 3) * 16 + r);
+        *reinterpret_cast<uint2*>(a.C + (size_t)(m0 + r) * N + n0 + c4 * 4) =
+            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      }
+    }
+    __syncthreads();  // before the next item's sums
+  }
+}
+
+// Row tiles that `rows` rows of E_local experts can make, at most.
+static int few_tiles(int rows, int E_local) {
+  const int n = std::min(rows, E_local);
+  return n + (rows - n) / kFewTile;
+}
+// Whether a launch takes it: at most kFewRows rows and, however they fall on the
+// experts, kFewBytes of weight codes, an expert's as often as it has row tiles.
+constexpr int kFewRows = 128;
+constexpr long long kFewBytes = 128LL << 20;
+static bool few_rows(int rows, int E_local, int N, int K, int matrices) {
+  return rows <= kFewRows && (long long)few_tiles(rows, E_local) * N * mx4_row_bytes(K) * matrices <= kFewBytes;
+}
+static unsigned few_grid(int rows, int E_local, int N, int cols) {
+  return (unsigned)std::min<long long>((long long)few_tiles(rows, E_local) * (N / cols), 8LL * device_cu_count());
+}
+
 // Workspace: counters (kCntBytes, zero before first use, as for bf16) | h codes
 // [M_cap][row bytes of I] | h scale dwords [chunks of I][M_cap][2] | split-K plan
 // | fp32 partials (split-K, or the decode schedule's slots).
@@ -276,6 +443,10 @@ static hipError_t gateup_mx4(const Mx4Rows& x, const Mx4Weights& wg, const Mx4We
   g.Bs0 = wg.scales;
   g.Bs1 = wu.scales;
   g.Cs = hs;
+  if (few_rows(M_cap, E_local, I, H, 2)) {
+    mx4_few_rows_kernel<true><<<few_grid(M_cap, E_local, I, 32), 8 * kWave, 0, s>>>(g);
+    return hipGetLastError();
+  }
   const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
   grouped_gemm_mx4_kernel<true><<<mx_grid(M_cap, E_local, I, split || g.sk), 8 * kWave, 0, s>>>(g);
   const hipError_t e = hipGetLastError();
@@ -299,6 +470,10 @@ static hipError_t gemm_mx4(const uint8_t* aq, const uint32_t* as, const Mx4Weigh
   mx_split_args(g, sp);
   g.As = as;
   g.Bs0 = w.scales;
+  if (few_rows(M_cap, E_local, N, K, 1)) {
+    mx4_few_rows_kernel<false><<<few_grid(M_cap, E_local, N, 64), 8 * kWave, 0, s>>>(g);
+    return hipGetLastError();
+  }
   const bool split = sp.plan != nullptr && g.K / kMxChunk >= 2 * kMinSplitChunks;
   grouped_gemm_mx4_kernel<false><<<mx_grid(M_cap, E_local, N, split || g.sk), 8 * kWave, 0, s>>>(g);
   const hipError_t e = hipGetLastError();

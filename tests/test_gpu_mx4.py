@@ -299,6 +299,54 @@ def test_ffn(H, I, rows):
     assert vh.shape[0] == M_cap
 
 
+FEW_CASES = [
+    # H, I, rows per expert: calls of at most 128 rows and little weight. K of one chunk
+    # and not a multiple of one, h rows that end inside a chunk, tiles of 16 rows with
+    # ragged ends, experts past a wavefront's 64, more tiles than a grid holds, and the
+    # first call with a row too many
+    (128, 128, [1]),
+    (384, 640, [0, 0, 2, 0]),
+    (2048, 768, [1, 15, 16, 17, 33]),
+    (7168, 256, [128]),
+    (1152, 384, [0] * 63 + [5, 1] + [0] * 62 + [2, 0, 3]),
+    (256, 1024, [1, 0] * 127 + [1, 0]),
+    (256, 2048, [0, 1] * 100 + [28]),
+    (2048, 384, [100, 29]),
+]
+
+
+@pytest.mark.parametrize("H,I,rows", FEW_CASES)
+def test_ffn_few_rows(H, I, rows):
+    banner("ffn few", H, I, len(rows), sum(rows))
+    r = np.random.default_rng(H + I + len(rows))
+    m = sum(rows)
+    x = moe.moe_mx4_quantize(torch.from_numpy(r.standard_normal((m, H))).float().to(DEV))
+    w, off = make_ffn(r, H, I, len(rows)), offsets_of(rows)
+    y, ws = moe.moe_grouped_swiglu_ffn_mx4(x, *w, off)
+    check_ffn(x, None, 1, w, rows, y, ws, m, I)
+    # each half by itself does the same work
+    h = moe.moe_grouped_swiglu_mx4(x, w[0], w[1], off)
+    q1, q2 = unpacked(h), unpacked(ffn_h(ws, m, I))
+    assert np.array_equal(q1[0], q2[0]) and np.array_equal(q1[1], q2[1])
+    assert torch.equal(moe.moe_grouped_gemm_mx4(h, w[2], off), y)
+
+
+@pytest.mark.parametrize("m", [5, 20, 100])
+def test_ffn_few_rows_empty_and_foreign_offsets(m):
+    """No rows at all; and offsets that run backwards or out of the buffer, which every
+    expert reads clamped to it: the last writer of a row wins, all values stay finite."""
+    banner("ffn few offsets", m)
+    r = np.random.default_rng(m)
+    x = moe.moe_mx4_quantize(torch.from_numpy(r.standard_normal((m, 512))).float().to(DEV))
+    w = make_ffn(r, 512, 384, 3)
+    y = torch.full((m, 512), float("nan"), dtype=torch.bfloat16, device=DEV)
+    moe.moe_grouped_swiglu_ffn_mx4(x, *w, offsets_of([0, 0, 0]), y_perm=y)
+    assert torch.isnan(y).all()
+    off = torch.tensor([-7, m, 1, 1 << 30], dtype=torch.int32, device=DEV)
+    moe.moe_grouped_swiglu_ffn_mx4(x, *w, off, y_perm=y)
+    assert torch.isfinite(y.float()).all()
+
+
 def route(r, T, k, E, E_local):
     ids = np.stack([r.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
     emap = np.full(E, -1, np.int32)
