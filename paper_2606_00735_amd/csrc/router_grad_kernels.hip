@@ -65,6 +65,10 @@ __device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&frag)[N]) {
 // every dz value is cut into its terms once, by the wave that owns its expert, as
 // it is read (lanes across experts: a row of LDS is read without conflicts). Two
 // waves on a SIMD: one's MFMAs run while the other cuts.
+// Bound by the chip's power: 16384 tokens, H = 7168, E = 256 take 192-243 us (60
+// GFLOP, three times that on the MFMAs: 0.74-0.94 PFLOP/s), MFMAs busy 59 % at 1.42
+// GHz. Two terms lost bits (relative error 2.5e-6 for 2e-7); the 60 GFLOP alone take
+// 390 us at the rate of a large fp32 product.
 // Experts past E are computed from other rows' values and not stored. Blocks of one
 // token range follow each other by the number of ranges, so that (for 2, 4 or 8 of
 // them) an XCD works on one or a few ranges and reads their dz from its L2.
@@ -207,7 +211,8 @@ __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
   }
 }
 
-// Sums the S partial sums in order.
+// Sums the S partial sums in order: 4 of 256 x 7168 (37 MB) 9.5 us, from the last-level
+// cache.
 __global__ __launch_bounds__(256) void router_dw_reduce_kernel(const float* __restrict__ part,
                                                                const float* __restrict__ pdb, int E, int H, int S,
                                                                float* __restrict__ dw, float* __restrict__ db) {
@@ -228,7 +233,9 @@ __global__ __launch_bounds__(256) void router_dw_reduce_kernel(const float* __re
 // direct loads, NS pieces in a ring. Fragments of W are read one 16-expert step
 // ahead of the MFMAs. Blocks that walk the same columns follow each other by the
 // number of column ranges, so that (for 2, 4 or 8 of them) an XCD's L2 holds one or
-// a few ranges of W.
+// a few ranges of W. 16384 tokens, H = 7168, E = 256: 110-135 us (60 GFLOP, twice that
+// on the MFMAs, and 235 MB written), MFMAs busy 60 % at 1.71 GHz: power, then the
+// stores.
 // ---------------------------------------------------------------------------
 constexpr int kDxRows = 128;
 
@@ -351,7 +358,8 @@ __global__ __launch_bounds__(256, 2) void router_dx_kernel(RouterGradArgs a, int
 }
 
 // ---------------------------------------------------------------------------
-// fp32 (small layers): plain sums.
+// fp32 (small layers): plain sums. 64 tokens, H = 128, E = 8: dW 4.2 us, dx 3.1 us,
+// a launch and a chain of load latencies each.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float* __restrict__ dz, const float* __restrict__ w,
                                                             int T, int E, int H, float* __restrict__ dx) {

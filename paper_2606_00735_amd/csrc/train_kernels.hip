@@ -142,6 +142,10 @@ __device__ __forceinline__ void row_softmax(float4& v, float& inv, float& lse) {
 // parts first, whose counts each block adds up (no atomics: 8192 of them on 1024
 // counters took 9 us).
 //
+// 16384 tokens of 256 experts in 4 groups (16.8 MB of logits): counts 6.2 us, loss 12 to
+// 14, where the copy rate alone would take 4: a launch, counts, logits and the join
+// follow each other, each a latency. 64 tokens of 8 experts in one launch of 5.4 us.
+//
 // ws: a ticket, zero before and after a call (at the start, whatever the sizes), two
 // partial sums per block, the counts and live tokens of the parts.
 // ---------------------------------------------------------------------------
@@ -426,7 +430,9 @@ hipError_t launch_balance_loss(const float* z, const int32_t* ids, const uint8_t
 // and of the gate weights w = softmax of the selected logits, for every token,
 //   w_j (dw_j - sum_i w_i dw_i) at expert ids_j.
 // One pass: logits in, gradient out. The selected experts' terms reach the lanes
-// that hold them through one row of LDS per token, which is zero between uses.
+// that hold them through one row of LDS per token, which is zero between uses. 16384
+// tokens of 256 experts, top 8 (35 MB): 10.6-12 us, 2.9-3.3 TB/s, bound by the launch's
+// ramp, one round of load latencies and the stores.
 // ---------------------------------------------------------------------------
 struct GateGradArgs {
   const int32_t* counts;   // [groups, E]
@@ -532,7 +538,8 @@ hipError_t launch_gate_backward(const float* z, const int32_t* ids, const uint8_
 // Gradient of the combine out[t] = sum_j w_tj y[dest_tj]: dw_tj = <dout_t,
 // y[dest_tj]> (0 for a remote assignment) and dy[dest_tj] = w_tj dout_t. One
 // wave per token reads its dout row once and each of its expert rows once; fp32
-// products and sums.
+// products and sums. Copy bound: 16384 tokens, a shard of 32 of 256 experts, H = 7168
+// (630 MB) 132-135 us, 4.7 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kCombineGradVecs = 4;  // 16-byte pieces of a row per lane in flight
 
