@@ -950,8 +950,8 @@ def moe_mx4_quantize(x, out=None, row_count=None, ld=None):
         if row_count.numel() != 1 or row_count.dtype != torch.int32 or not row_count.is_cuda or x.dim() != 2:
             raise ValueError("row_count must be one device int32 (for x [R, K])")
         rc = row_count.data_ptr()
-    st = L.moe_mx4_quantize(_dev(x, "x"), _dtype_code(x), B, R, K, out.ld, rc, _mx_codes(out.codes, "codes"),
-                            _dev(out.scales, "scales", torch.int32), _stream())
+    st = L.moe_mx4_quantize(_dev(x, "x"), _dtype_code(x), B, R, K, out.ld, rc, *_mx4_dev(out, "out", out.shape, True),
+                            _stream())
     _check("moe_mx4_quantize", st)
     return out
 
@@ -966,22 +966,27 @@ def moe_mx4_dequantize(t, out=None):
     elif tuple(out.shape) != t.shape:
         raise ValueError(f"out must have shape {t.shape}")
     B, (R, K) = (1 if len(t.shape) == 2 else t.shape[0]), t.shape[-2:]
-    st = L.moe_mx4_dequantize(_mx_codes(t.codes, "codes"), _dev(t.scales, "scales", torch.int32), B, R, K, t.ld,
-                              _dev(out, "out", torch.bfloat16), _stream())
+    st = L.moe_mx4_dequantize(*_mx4_dev(t, "t", t.shape, True), B, R, K, t.ld, _dev(out, "out", torch.bfloat16),
+                              _stream())
     _check("moe_mx4_dequantize", st)
     return out
 
 
 def _mx4_dev(t, name, shape, padded=False):
     """Pointers of an MXFP4 operand; only weight operands (padded=True) may have
-    padded code rows."""
+    padded code rows. (Types and layout were checked when the Mx4Tensor was made.)"""
     if not isinstance(t, Mx4Tensor):
         raise TypeError(f"{name} must be an Mx4Tensor")
-    if t.shape != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {t.shape}")
-    if not padded and t.ld != t.codes.shape[-1]:
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {t.shape}")
+    codes, scales = t.codes, t.scales
+    if not padded and t.ld != codes.shape[-1]:
         raise ValueError(f"{name} must have dense code rows")
-    return _mx_codes(t.codes, name + ".codes"), _dev(t.scales, name + ".scales", torch.int32)
+    if not codes.is_cuda:
+        raise ValueError(f"{name}.codes must be on the GPU (libmoe has no CPU path)")
+    if not scales.is_contiguous():
+        raise ValueError(f"{name}.scales must be contiguous")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def _mx4_rows(x, perm_src, k):
