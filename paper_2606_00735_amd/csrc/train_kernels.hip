@@ -86,19 +86,19 @@ __device__ __forceinline__ float4 load_logits(const float* row, int e0, int E, b
 
 // The rows of a block: this lane's logits of every round, and whether the token
 // is there (in) and live (on). Masked rows are read as well, so that the loads
-// wait for nothing; what they hold is replaced by -inf.
+// wait for nothing; settle, which waits for them, replaces what they hold by -inf.
 template <int L, int W, int N>
 struct Rows {
   float4 v[N];
   bool in[N], on[N];
   size_t row[N];
+  uint8_t m[N];
 
   // rounds [first, first + N) of block blk's `rounds`
   __device__ __forceinline__ void load(const RowArgs& a, int g, int blk, int rounds, int first, int lane, int wave) {
     constexpr int SLOTS = kWave / L;
     const int e0 = (lane % L) * 4;
     const bool vec = (a.E & 3) == 0;
-    uint8_t m[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int t = (blk * rounds + first + i) * W * SLOTS + wave * SLOTS + lane / L;
@@ -107,6 +107,8 @@ struct Rows {
       v[i] = load_logits(a.z + row[i] * a.E, e0, a.E, vec, in[i]);
       m[i] = a.mask != nullptr ? a.mask[row[i]] : 1;
     }
+  }
+  __device__ __forceinline__ void settle() {
     const float ninf = -__builtin_huge_valf();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -230,18 +232,25 @@ __global__ __launch_bounds__(kLossWaves* kWave) void balance_loss_kernel(RowArgs
   if (SELF) {
     count_ids<THREADS>(a, g, 0, a.n, s_cnt, &s_live);
   } else {
-    // four counts of a part a thread at a time
+    // four counts of a part at a time, all of a thread's in flight
+    constexpr int C = (kParts * L + THREADS - 1) / THREADS;
     const int4* parts = reinterpret_cast<const int4*>(ws.counts + (size_t)g * ws.parts * (4 * L));
-#pragma unroll 2
-    for (int i = tid; i < ws.parts * L; i += THREADS) {
-      const int4 q = parts[i];
-      int32_t* s = s_cnt + (i % L) * 4;
-      if (q.x) atomicAdd(s, q.x);
-      if (q.y) atomicAdd(s + 1, q.y);
-      if (q.z) atomicAdd(s + 2, q.z);
-      if (q.w) atomicAdd(s + 3, q.w);
+    int4 q[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int at = i * THREADS + tid;
+      q[i] = at < ws.parts * L ? parts[at] : make_int4(0, 0, 0, 0);
     }
-    if (tid < ws.parts) atomicAdd(&s_live, ws.live[(size_t)g * ws.parts + tid]);
+    const int n = tid < ws.parts ? ws.live[(size_t)g * ws.parts + tid] : 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      int32_t* s = s_cnt + ((i * THREADS + tid) % L) * 4;
+      if (q[i].x) atomicAdd(s, q[i].x);
+      if (q[i].y) atomicAdd(s + 1, q[i].y);
+      if (q[i].z) atomicAdd(s + 2, q[i].z);
+      if (q[i].w) atomicAdd(s + 3, q[i].w);
+    }
+    if (n != 0) atomicAdd(&s_live, n);
   }
   __syncthreads();
   const int n_live = s_live;
@@ -258,6 +267,12 @@ __global__ __launch_bounds__(kLossWaves* kWave) void balance_loss_kernel(RowArgs
   float bal = 0.0f, zl = 0.0f;
 #pragma unroll 1
   for (int first = 0;;) {
+    // the next rounds' loads leave before these are used
+    first += N;
+    const bool more = first < kLossRounds && (blk * kLossRounds + first) * W * (kWave / L) < a.n;
+    Rows<L, W, N> next;
+    if (more) next.load(a, g, blk, kLossRounds, first, lane, wave);
+    r.settle();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float4& v = r.v[i];
@@ -266,9 +281,8 @@ __global__ __launch_bounds__(kLossWaves* kWave) void balance_loss_kernel(RowArgs
       const float s = group_sum<L>((c[0] * v.x + c[1] * v.y) + (c[2] * v.z + c[3] * v.w)) * inv;
       if (r.on[i] && lane % L == 0) bal += s, zl += lse * lse;
     }
-    first += N;
-    if (first >= kLossRounds || (blk * kLossRounds + first) * W * (kWave / L) >= a.n) break;
-    r.load(a, g, blk, kLossRounds, first, lane, wave);
+    if (!more) break;
+    r = next;
   }
   bal = group_sum<64>(bal);
   zl = group_sum<64>(zl);
@@ -481,6 +495,7 @@ __global__ __launch_bounds__(256) void gate_backward_kernel(RowArgs a, GateGradA
   float* srow = s_row[GATE ? wave : 0][slot];
   float4* mine = reinterpret_cast<float4*>(srow + e0);
   if (GATE) *mine = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  r.settle();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float4& v = r.v[i];
