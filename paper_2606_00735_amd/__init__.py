@@ -6,7 +6,10 @@ expert FFN, weighted combine, and the per-expert latency-vs-load sweep from
 which the per-GPU performance model f_g(n) is fitted, and ViBE's placement
 control path on top of it (latency-aware greedy placement, drift detector,
 incremental swap solver), and an MXFP8 (FP8 E4M3 with E8M0 block
-scales) variant of the expert FFN. Every step runs in the
+scales) variant of the expert FFN. For training a router over frozen 4-bit
+experts there are an MXFP4 (E2M1) expert FFN, the balance and z losses with
+per-expert counts, and the gradients of the gate, the combine and the router's
+product. Every step runs in the
 HIP kernels of ``libmoe.so`` (C ABI in ``include/moe.h``); this package only
 marshals torch tensors into those calls.
 """

@@ -245,8 +245,8 @@ __global__ __launch_bounds__(256) void split_reduce_mx4_kernel(GemmArgs a) {
 // chunks of a row in flight; the quarters' sums meet in LDS, in order. Every wave
 // finds the block's expert itself, from the offsets.
 //
-// Bound by the latency of offsets, rows and weights, one after the other, about 5 us a
-// launch; by the load path of the CUs that have a block when there are few; by memory
+// Bound by the latency of offsets, rows and weights, one after the other, 5 us a launch
+// (7 with cold operands); by the load path of the CUs that have a block when there are few; by memory
 // from some 100 MB on, where the decode schedule's ring keeps more in flight. FFN us
 // (bytes of the gate/up codes), the decode schedule / this: H = 2048, I = 768, 8 experts
 // of 1 row (13 MB) 22.4 / 11.0, 32 of 2 (50 MB) 28.1 / 23.5, 64 of 1 (101 MB) 45.4 /

@@ -144,8 +144,8 @@ __device__ __forceinline__ void row_softmax(float4& v, float& inv, float& lse) {
 // parts first, whose counts each block adds up (no atomics: 8192 of them on 1024
 // counters took 9 us).
 //
-// 16384 tokens of 256 experts in 4 groups (16.8 MB of logits): counts 6.2 us, loss 12 to
-// 14, where the copy rate alone would take 4: a launch, counts, logits and the join
+// 16384 tokens of 256 experts in 4 groups (16.8 MB of logits): counts 6.2 us, loss 11 to
+// 13, where the copy rate alone would take 4: a launch, counts, logits and the join
 // follow each other, each a latency. 64 tokens of 8 experts in one launch of 5.4 us.
 //
 // ws: a ticket, zero before and after a call (at the start, whatever the sizes), two
@@ -445,7 +445,7 @@ hipError_t launch_balance_loss(const float* z, const int32_t* ids, const uint8_t
 //   w_j (dw_j - sum_i w_i dw_i) at expert ids_j.
 // One pass: logits in, gradient out. The selected experts' terms reach the lanes
 // that hold them through one row of LDS per token, which is zero between uses. 16384
-// tokens of 256 experts, top 8 (35 MB): 10.6-12 us, 2.9-3.3 TB/s, bound by the launch's
+// tokens of 256 experts, top 8 (35 MB): 11-12 us, 3 TB/s, bound by the launch's
 // ramp, one round of load latencies and the stores.
 // ---------------------------------------------------------------------------
 struct GateGradArgs {
