@@ -242,23 +242,26 @@ __global__ __launch_bounds__(256) void split_reduce_mx4_kernel(GemmArgs a) {
 // across blocks: a block takes 16 rows of an expert by 64 weight rows (32 columns of
 // gate and up, or 64 of down), its 8 waves 32 weight rows x a quarter of K each,
 // straight from memory to the operand registers of the 16 x 16 x 128 MFMA, kFewBatch
-// chunks of a row in flight; the quarters' sums meet in LDS, in order. Every wave
-// finds the block's expert itself, from the offsets.
+// chunks of a row a step; the quarters' sums meet in LDS, in order. Every wave finds
+// the block's expert itself, from the offsets.
 //
-// Bound by the latency of offsets, rows and weights, one after the other, 5 us a launch
-// (7 with cold operands); by the load path of the CUs that have a block when there are few; by memory
-// from some 100 MB on, where the decode schedule's ring keeps more in flight. FFN us
-// (bytes of the gate/up codes), the decode schedule / this: H = 2048, I = 768, 8 experts
-// of 1 row (13 MB) 22.4 / 11.0, 32 of 2 (50 MB) 28.1 / 23.5, 64 of 1 (101 MB) 45.4 /
-// 43.7, 128 of 8 (201 MB) 81 / 84, 16 of 64 29.5 / 45.2; H = 7168, I = 2048, 1 of 1
-// (15 MB) 21.0 / 16.9, 1 of 64 31.4 / 24.0, 1 of 128 43.4 / 40.1, 8 of 1 (117 MB) 52.6 /
-// 45.7, 8 of 14 57.8 / 64.5, 32 of 4 (470 MB) 153 / 166; H = 4096, I = 14336, 1 of 1 (59
-// MB) 32.2 / 33.0, 2 of 60 62.9 / 171, 8 of 8 (470 MB) 146 / 175. Two chunks in flight instead of four: 17.3 for 16.9, 46.1
-// for 45.7.
+// Bound by the latency of offsets, rows and weights, one after the other, 5 us a
+// launch (7 with cold operands); by the load path of the CUs that have a block when
+// there are few; by memory from some 100 MB on, where the decode schedule's ring keeps
+// more in flight. FFN us (bytes of the gate/up codes), the decode schedule / this: H =
+// 2048, I = 768, 8 experts of 1 row (13 MB) 22.4 / 10.9, 32 of 2 (50 MB) 28.1 / 23.5, 64
+// of 1 (101 MB) 45.4 / 41.8, 128 of 8 (201 MB) 81 / 84, 16 of 64 29.5 / 45.2; H = 7168,
+// I = 2048, 1 of 1 (15 MB) 21.0 / 17.1, 1 of 64 31.4 / 24.1, 1 of 128 43.4 / 40.1, 8 of 1
+// (117 MB) 52.6 / 45.7, 8 of 14 57.8 / 64.5, 32 of 4 (470 MB) 153 / 166; H = 4096, I =
+// 14336, 1 of 1 (59 MB) 32.2 / 33.0, 2 of 60 62.9 / 171, 8 of 8 (470 MB) 146 / 175.
+// A step of two chunks instead of four: 17.3 for 16.9, 46.1 for 45.7. At most 80
+// registers, so that a CU holds three blocks: 64 experts of 1 row 41.8 for 44.0 with
+// two; with 64 registers (four blocks, some spilt) 56, with all of a step's loads issued
+// before its first product (160 registers, one block) 79.
 // ---------------------------------------------------------------------------
 constexpr int kFewTile = 16;   // rows of a tile
 constexpr int kFewSplit = 4;   // parts of K
-constexpr int kFewBatch = 4;   // chunks in flight a wave
+constexpr int kFewBatch = 4;   // chunks of a wave's step
 
 // Sum of x over this lane and the lanes below.
 __device__ __forceinline__ int lane_prefix(int x) {
@@ -272,7 +275,7 @@ __device__ __forceinline__ int lane_prefix(int x) {
 }
 
 template <bool DUAL>
-__global__ __launch_bounds__(8 * kWave, 2) void mx4_few_rows_kernel(GemmArgs a) {
+__global__ __launch_bounds__(8 * kWave, 6) void mx4_few_rows_kernel(GemmArgs a) {
   constexpr int COLS = DUAL ? 32 : 64, Q = kMaxExperts / kWave;
   __shared__ f32x4_t s_sum[8][2][kWave];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
