@@ -632,12 +632,13 @@ moe_status moe_combine_backward(const void* dout, const void* y_perm, const floa
  * dw_router [E, H] fp32        dlogits^T x
  * dbias     [E]    fp32        sum_t dlogits[t,:]
  * dlogits [T, E] fp32; x [T, H], w_router [E, H] dt. bf16: dlogits enters the MFMA
- * as a sum of bf16 terms, all 24 bits of it for dw_router and 16 for dx; sums are fp32. T == 0 writes
+ * as a sum of bf16 terms, all 24 bits of it for dw_router and rounded by at most 2^-17
+ * of an element for dx; sums are fp32. T == 0 writes
  * zeros to dw_router and dbias. ws holds partial sums over ranges of tokens, added
  * in order (results do not depend on timing); its size depends on the device's
  * compute units. As in any such product, a row of x that is not finite makes dw_router
  * NaN even where its dlogits are 0: rows of masked tokens must hold numbers. An
- * infinite dlogits gives NaN.
+ * infinite dlogits gives NaN in dw_router.
  * Limits: 1 <= E <= 256, H % 8 == 0 (bf16: H % 64 == 0), H <= 2^20.
  */
 moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_router, int T, int E,

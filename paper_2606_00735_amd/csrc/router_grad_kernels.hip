@@ -4,9 +4,13 @@
 // dz is fp32, x and W bf16, and the MFMA takes bf16 pairs: dz is cut into bf16
 // terms, each multiplied with the exact other operand and summed in fp32. For dW,
 // fp32 like the sums, three terms hold all 24 bits of an element; for dx, rounded
-// to bf16, two are enough (they drop 2^-16 of an element). Both reductions run
-// along a dimension that is a row index of the bf16 operand (tokens of x, experts
-// of W), so its fragments are read from LDS with the transposing read.
+// to bf16 (2^-9 of its value), two rounded to nearest are enough: they are off by at
+// most 2^-17 of an element, in either direction. (Cut off, as the three are, two would
+// lose up to 2^-15, always towards zero, which shows where dx is small beside its
+// terms: rows of dz sum to nearly nothing, and the rows of W may have much in common.)
+// Both reductions run along a dimension that is a row index of the bf16 operand
+// (tokens of x, experts of W), so its fragments are read from LDS with the
+// transposing read.
 #include <algorithm>
 #include <type_traits>
 
@@ -40,22 +44,37 @@ __device__ __forceinline__ bf16x8_t tr_frag(const char* tile, int lane, int k0, 
   return __builtin_bit_cast(bf16x8_t, v);
 }
 
-// Eight fp32 values as N bf16 fragments, f = sum of frag[n] up to the bits past the
-// N-th: each takes the upper 16 bits of what is left (the differences are exact), so
-// three hold every value.
-template <int N>
-__device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&frag)[N]) {
+// Eight fp32 values as three bf16 fragments, f = sum of frag[n]: each takes the upper
+// 16 bits of what is left (the differences are exact).
+__device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&frag)[3]) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
+  for (int n = 0; n < 3; ++n) {
     uint32_t w[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       w[q] = __builtin_amdgcn_perm(__float_as_uint(f[2 * q + 1]), __float_as_uint(f[2 * q]), 0x07060302u);
     frag[n] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
-    if (n + 1 < N)
+    if (n + 1 < 3)
 #pragma unroll
       for (int q = 0; q < 8; ++q) f[q] -= __uint_as_float(__float_as_uint(f[q]) & 0xffff0000u);
   }
+}
+
+// Eight fp32 values as two bf16 fragments: f rounded to nearest, and what that left
+// (exact in fp32), rounded to nearest. The first stays within bf16's finite range, so
+// that a value which would round up to infinity does not.
+__device__ __forceinline__ void split8_nearest(const float (&f)[8], bf16x8_t (&frag)[2]) {
+  constexpr float kMaxBf16 = 0x1.fep127f;
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    hi[q] = pack_bf16x2(__builtin_amdgcn_fmed3f(f[2 * q], -kMaxBf16, kMaxBf16),
+                        __builtin_amdgcn_fmed3f(f[2 * q + 1], -kMaxBf16, kMaxBf16));
+    lo[q] = pack_bf16x2(f[2 * q] - __uint_as_float(hi[q] << 16),
+                        f[2 * q + 1] - __uint_as_float(hi[q] & 0xffff0000u));
+  }
+  frag[0] = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
+  frag[1] = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
 }
 
 // ---------------------------------------------------------------------------
@@ -183,7 +202,7 @@ __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
     if (tile == 0)
       db += ((f[buf][0] + f[buf][1]) + (f[buf][2] + f[buf][3])) + ((f[buf][4] + f[buf][5]) + (f[buf][6] + f[buf][7]));
     bf16x8_t zf[3];
-    split8<3>(f[buf], zf);
+    split8(f[buf], zf);
 #pragma unroll
     for (int n = 0; n < 3; ++n)
 #pragma unroll
@@ -268,7 +287,7 @@ __global__ __launch_bounds__(256, 2) void router_dx_kernel(RouterGradArgs a, int
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = e + k < E ? p[e + k] : 0.0f;
       }
-      split8<2>(f, zf[s]);
+      split8_nearest(f, zf[s]);
     }
   }
   // piece kc of column tile tl; 16 KB, 4 instructions a wave; rows past E read the last
