@@ -900,32 +900,55 @@ def mx4_chunks(K):
     return (K + 255) // 256
 
 
+def _mx4_layout(codes, scales, K):
+    """(shape, row stride of the codes in bytes) of an MXFP4 operand; raises ValueError
+    for codes and scales that are none."""
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.int32:
+        raise ValueError("MXFP4 codes are uint8 and scales int32")
+    n, row = codes.dim(), (K + 255) // 256 * 128
+    if n == 2:
+        R, got = codes.shape
+        shape, want = (R, K), (row // 128, R, 2)
+    elif n == 3:
+        B, R, got = codes.shape
+        shape, want = (B, R, K), (B, row // 128, R, 2)
+    else:
+        got = -1
+    if got != row or K < 1 or K % 32:
+        raise ValueError("codes must be [R, 128 C] or [B, R, 128 C], C = ceil(K / 256), K a multiple of 32")
+    if scales.shape != want or not scales.is_contiguous():
+        raise ValueError("scales must be [.., C, R, 2] and contiguous for codes [.., R, 128 C]")
+    if scales.get_device() != codes.get_device():
+        raise ValueError("codes and scales must be on one device")
+    if codes.is_contiguous():
+        return shape, row
+    ld = codes.stride(-2) if R > 1 else row
+    if codes.stride(-1) != 1 or ld < row or (n == 3 and B > 1 and codes.stride(0) != R * ld):
+        raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
+    return shape, ld
+
+
 class Mx4Tensor:
     """An MXFP4 operand of shape [.., R, K]: E2M1 codes [.., R, 128 C] uint8 (two a
     byte, the even element in the low half; C = ceil(K / 256), the rows padded with
     zero codes) and scale dwords [.., C, R, 2] int32 (byte s of dword (k, r, h): the
     E8M0 code of elements [256 k + 64 s + 32 h, +32) of row r). The codes may be a
     view with padded rows (row stride ld bytes, matrices R * ld apart), which weight
-    operands accept."""
+    operands accept. An operand keeps its codes and scales; what they hold may change,
+    their sizes may not (a call refuses what was resized since)."""
+
+    __slots__ = ("_codes", "_scales", "_K", "_shape", "_ld", "_codes_n", "_scales_n")
 
     def __init__(self, codes, scales, K):
-        if codes.dtype != torch.uint8 or scales.dtype != torch.int32:
-            raise ValueError("MXFP4 codes are uint8 and scales int32")
-        lead, C = tuple(codes.shape), (K + 255) // 256
-        if K < 1 or K % 32 or len(lead) not in (2, 3) or lead[-1] != 128 * C:
-            raise ValueError("codes must be [R, 128 C] or [B, R, 128 C], C = ceil(K / 256), K a multiple of 32")
-        R = lead[-2]
-        if tuple(scales.shape) != lead[:-2] + (C, R, 2):
-            raise ValueError("scales must be [.., C, R, 2] for codes [.., R, 128 C]")
-        if scales.device != codes.device:
-            raise ValueError("codes and scales must be on one device")
-        ld = 128 * C
-        if not codes.is_contiguous():
-            ld = codes.stride(-2) if R > 1 else 128 * C
-            if codes.stride(-1) != 1 or ld < 128 * C or (len(lead) == 3 and lead[0] > 1 and codes.stride(0) != R * ld):
-                raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
-        self.codes, self.scales, self.K, self.ld = codes, scales, K, ld
-        self.shape = lead[:-1] + (K,)
+        self._shape, self._ld = _mx4_layout(codes, scales, K)
+        self._codes, self._scales, self._K = codes, scales, K
+        self._codes_n, self._scales_n = codes.numel(), scales.numel()
+
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
+    K = property(lambda self: self._K)
+    shape = property(lambda self: self._shape)
+    ld = property(lambda self: self._ld)
 
 
 def moe_mx4_quantize(x, out=None, row_count=None, ld=None):
@@ -943,15 +966,15 @@ def moe_mx4_quantize(x, out=None, row_count=None, ld=None):
                             device=x.device)[..., :row]
         out = Mx4Tensor(codes, torch.empty(tuple(x.shape[:-2]) + (mx4_chunks(K), R, 2), dtype=torch.int32,
                                            device=x.device), K)
-    elif out.shape != tuple(x.shape):
-        raise ValueError(f"out must have shape {tuple(x.shape)}, got {out.shape}")
+    shape, ldc, codes, scales = _mx4(out, "out")
+    if shape != tuple(x.shape):
+        raise ValueError(f"out must have shape {tuple(x.shape)}, got {shape}")
     rc = None
     if row_count is not None:
         if row_count.numel() != 1 or row_count.dtype != torch.int32 or not row_count.is_cuda or x.dim() != 2:
             raise ValueError("row_count must be one device int32 (for x [R, K])")
         rc = row_count.data_ptr()
-    st = L.moe_mx4_quantize(_dev(x, "x"), _dtype_code(x), B, R, K, out.ld, rc, *_mx4_dev(out, "out", out.shape, True),
-                            _stream())
+    st = L.moe_mx4_quantize(_dev(x, "x"), _dtype_code(x), B, R, K, ldc, rc, codes, scales, _stream())
     _check("moe_mx4_quantize", st)
     return out
 
@@ -959,66 +982,64 @@ def moe_mx4_quantize(x, out=None, row_count=None, ld=None):
 def moe_mx4_dequantize(t, out=None):
     """The values (bf16) that an Mx4Tensor stands for."""
     L = load_library()
-    if not isinstance(t, Mx4Tensor):
-        raise TypeError("t must be an Mx4Tensor")
+    shape, ld, codes, scales = _mx4(t, "t")
     if out is None:
-        out = torch.empty(t.shape, dtype=torch.bfloat16, device=t.codes.device)
-    elif tuple(out.shape) != t.shape:
-        raise ValueError(f"out must have shape {t.shape}")
-    B, (R, K) = (1 if len(t.shape) == 2 else t.shape[0]), t.shape[-2:]
-    st = L.moe_mx4_dequantize(*_mx4_dev(t, "t", t.shape, True), B, R, K, t.ld, _dev(out, "out", torch.bfloat16),
-                              _stream())
+        out = torch.empty(shape, dtype=torch.bfloat16, device=t.codes.device)
+    elif tuple(out.shape) != shape:
+        raise ValueError(f"out must have shape {shape}")
+    B, (R, K) = (1 if len(shape) == 2 else shape[0]), shape[-2:]
+    st = L.moe_mx4_dequantize(codes, scales, B, R, K, ld, _dev(out, "out", torch.bfloat16), _stream())
     _check("moe_mx4_dequantize", st)
     return out
 
 
-def _mx4_dev(t, name, shape, padded=False):
-    """Pointers of an MXFP4 operand; only weight operands (padded=True) may have
-    padded code rows. (Types and layout were checked when the Mx4Tensor was made.)"""
+def _mx4(t, name, dims=0):
+    """(shape, row stride, pointers of codes and scales) of an MXFP4 operand."""
     if not isinstance(t, Mx4Tensor):
         raise TypeError(f"{name} must be an Mx4Tensor")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {t.shape}")
-    codes, scales = t.codes, t.scales
-    if not padded and t.ld != codes.shape[-1]:
+    codes, scales, shape, ld = t._codes, t._scales, t._shape, t._ld
+    if dims and len(shape) != dims:
+        raise TypeError(f"{name} must have {dims} dimensions")
+    # dense codes and scales of as many elements as at first are as they were checked
+    # then; all others (and padded rows) are looked at whole
+    if not (codes.is_contiguous() and scales.is_contiguous() and codes.numel() == t._codes_n
+            and scales.numel() == t._scales_n and codes.dtype is torch.uint8 and scales.dtype is torch.int32):
+        if _mx4_layout(codes, scales, t._K) != (shape, ld):
+            raise ValueError(f"{name}: codes must be of the size that the Mx4Tensor was made with")
+    if not (codes.is_cuda and scales.is_cuda):
+        raise ValueError(f"{name} must be on the GPU (libmoe has no CPU path)")
+    return shape, ld, codes.data_ptr(), scales.data_ptr()
+
+
+def _mx4_rows(t, name):
+    """The same of rows of activations [R, K]: only weights may have padded code rows."""
+    shape, ld, codes, scales = _mx4(t, name, 2)
+    if ld != t._codes.shape[1]:
         raise ValueError(f"{name} must have dense code rows")
-    if not codes.is_cuda:
-        raise ValueError(f"{name}.codes must be on the GPU (libmoe has no CPU path)")
-    if not scales.is_contiguous():
-        raise ValueError(f"{name}.scales must be contiguous")
-    return codes.data_ptr(), scales.data_ptr()
-
-
-def _mx4_rows(x, perm_src, k):
-    """(M_cap, T, perm_src pointer) of an expert input that is x itself or gathered from it."""
-    if not isinstance(x, Mx4Tensor) or len(x.shape) != 2:
-        raise TypeError("x must be a two-dimensional Mx4Tensor")
-    if perm_src is None:
-        return x.shape[0], x.shape[0], None
-    return perm_src.numel(), x.shape[0], _dev(perm_src, "perm_src", torch.int32)
+    return shape, codes, scales
 
 
 def moe_grouped_swiglu_mx4(x, w_gate, w_up, offsets, h=None, perm_src=None, k=1):
     """Gate/up half of the MXFP4 FFN: h = MXFP4(silu(x Wg^T) * (x Wu^T)) per local
     expert. With perm_src (moe_permute) row r of the input is x[perm_src[r] // k]."""
     L = load_library()
-    M_cap, T, src = _mx4_rows(x, perm_src, k)
-    H = x.shape[1]
-    E_local, I, _ = w_gate.shape
-    if offsets.numel() != E_local + 1:
-        raise ValueError("offsets must have E_local + 1 entries")
-    dev = x.codes.device
+    (T, H), xq, xs = _mx4_rows(x, "x")
+    M_cap, src = (T, None) if perm_src is None else (perm_src.numel(), _dev(perm_src, "perm_src", torch.int32))
+    (E_local, I, Hw), ld, gq, gs = _mx4(w_gate, "w_gate", 3)
+    if Hw != H or offsets.numel() != E_local + 1:
+        raise ValueError("w_gate must be [E_local, I, H] for x [.., H], and offsets must have E_local + 1 entries")
+    up_shape, ld_up, uq, us = _mx4(w_up, "w_up", 3)
+    if up_shape != (E_local, I, H) or ld_up != ld:
+        raise ValueError("w_up must have the shape and the row stride of w_gate")
     if h is None:
-        C = mx4_chunks(I)
+        C, dev = mx4_chunks(I), x.codes.device
         h = Mx4Tensor(torch.empty((M_cap, 128 * C), dtype=torch.uint8, device=dev),
                       torch.empty((C, M_cap, 2), dtype=torch.int32, device=dev), I)
-    if w_up.ld != w_gate.ld:
-        raise ValueError("w_gate and w_up must have the same row stride")
-    st = L.moe_grouped_swiglu_mx4(*_mx4_dev(x, "x", (T, H)), src, T, k,
-                                  *_mx4_dev(w_gate, "w_gate", (E_local, I, H), True),
-                                  *_mx4_dev(w_up, "w_up", (E_local, I, H), True),
-                                  _dev(offsets, "offsets", torch.int32), E_local, H, I, w_gate.ld, M_cap,
-                                  *_mx4_dev(h, "h", (M_cap, I)), _stream())
+    h_shape, hq, hs = _mx4_rows(h, "h")
+    if h_shape != (M_cap, I):
+        raise ValueError(f"h must have shape {(M_cap, I)}, got {h_shape}")
+    st = L.moe_grouped_swiglu_mx4(xq, xs, src, T, k, gq, gs, uq, us, _dev(offsets, "offsets", torch.int32), E_local, H,
+                                  I, ld, M_cap, hq, hs, _stream())
     _check("moe_grouped_swiglu_mx4", st)
     return h
 
@@ -1026,16 +1047,15 @@ def moe_grouped_swiglu_mx4(x, w_gate, w_up, offsets, h=None, perm_src=None, k=1)
 def moe_grouped_gemm_mx4(a, b, offsets, c=None):
     """Grouped MXFP4 GEMM: c[R] = bf16(a[R] b[l]^T) per local expert l."""
     L = load_library()
-    M_cap, K = a.shape
-    E_local, N, _ = b.shape
-    if offsets.numel() != E_local + 1:
-        raise ValueError("offsets must have E_local + 1 entries")
+    (M_cap, K), aq, sa = _mx4_rows(a, "a")
+    (E_local, N, Kb), ld, bq, sb = _mx4(b, "b", 3)
+    if Kb != K or offsets.numel() != E_local + 1:
+        raise ValueError("b must be [E_local, N, K] for a [.., K], and offsets must have E_local + 1 entries")
     if c is None:
         c = torch.empty((M_cap, N), dtype=torch.bfloat16, device=a.codes.device)
     elif tuple(c.shape) != (M_cap, N):
         raise ValueError(f"c must be [{M_cap}, {N}]")
-    st = L.moe_grouped_gemm_mx4(*_mx4_dev(a, "a", (M_cap, K)), *_mx4_dev(b, "b", (E_local, N, K), True),
-                                _dev(offsets, "offsets", torch.int32), E_local, N, K, b.ld, M_cap,
+    st = L.moe_grouped_gemm_mx4(aq, sa, bq, sb, _dev(offsets, "offsets", torch.int32), E_local, N, K, ld, M_cap,
                                 _dev(c, "c", torch.bfloat16), _stream())
     _check("moe_grouped_gemm_mx4", st)
     return c
@@ -1055,30 +1075,29 @@ def moe_grouped_swiglu_ffn_mx4(x, w_gate, w_up, w_down, offsets, ws=None, y_perm
     [T, H], of which row r of the input is x[perm_src[r] // k]. ``experts`` is there for
     calls written like moe_grouped_swiglu_ffn_gather's: there is one kernel for all
     loads, and nothing depends on it. Returns (y_perm [M_cap, H] bf16, ws)."""
-    if experts < 0 or (experts and experts < w_gate.shape[0]):
-        raise ValueError("experts must be 0 or at least the local experts")
     L = load_library()
-    M_cap, T, src = _mx4_rows(x, perm_src, k)
-    H = x.shape[1]
-    E_local, I, _ = w_gate.shape
-    if offsets.numel() != E_local + 1:
-        raise ValueError("offsets must have E_local + 1 entries")
-    dev = x.codes.device
-    if ws is None:
-        ws = torch.zeros(ffn_mx4_ws_bytes(E_local, H, I, M_cap), dtype=torch.uint8, device=dev)  # counters start at zero
+    (T, H), xq, xs = _mx4_rows(x, "x")
+    M_cap, src = (T, None) if perm_src is None else (perm_src.numel(), _dev(perm_src, "perm_src", torch.int32))
+    (E_local, I, Hw), ld_gu, gq, gs = _mx4(w_gate, "w_gate", 3)
+    if experts < 0 or (experts and experts < E_local):
+        raise ValueError("experts must be 0 or at least the local experts")
+    if Hw != H or offsets.numel() != E_local + 1:
+        raise ValueError("w_gate must be [E_local, I, H] for x [.., H], and offsets must have E_local + 1 entries")
+    up_shape, ld_up, uq, us = _mx4(w_up, "w_up", 3)
+    if up_shape != (E_local, I, H) or ld_up != ld_gu:
+        raise ValueError("w_up must have the shape and the row stride of w_gate")
+    dn_shape, ld_dn, dq, ds = _mx4(w_down, "w_down", 3)
+    if dn_shape != (E_local, H, I):
+        raise ValueError(f"w_down must have shape {(E_local, H, I)}, got {dn_shape}")
+    if ws is None:  # counters start at zero
+        ws = torch.zeros(ffn_mx4_ws_bytes(E_local, H, I, M_cap), dtype=torch.uint8, device=x.codes.device)
     if y_perm is None:
-        y_perm = torch.empty((M_cap, H), dtype=torch.bfloat16, device=dev)
+        y_perm = torch.empty((M_cap, H), dtype=torch.bfloat16, device=x.codes.device)
     elif tuple(y_perm.shape) != (M_cap, H):
         raise ValueError(f"y_perm must be [{M_cap}, {H}]")
     n = ctypes.c_size_t(ws.numel())
-    if w_up.ld != w_gate.ld:
-        raise ValueError("w_gate and w_up must have the same row stride")
-    st = L.moe_grouped_swiglu_ffn_mx4(*_mx4_dev(x, "x", (T, H)), src, T, k,
-                                      *_mx4_dev(w_gate, "w_gate", (E_local, I, H), True),
-                                      *_mx4_dev(w_up, "w_up", (E_local, I, H), True),
-                                      *_mx4_dev(w_down, "w_down", (E_local, H, I), True),
-                                      _dev(offsets, "offsets", torch.int32), E_local, H, I, w_gate.ld, w_down.ld,
-                                      M_cap, _dev(y_perm, "y_perm", torch.bfloat16),
+    st = L.moe_grouped_swiglu_ffn_mx4(xq, xs, src, T, k, gq, gs, uq, us, dq, ds, _dev(offsets, "offsets", torch.int32),
+                                      E_local, H, I, ld_gu, ld_dn, M_cap, _dev(y_perm, "y_perm", torch.bfloat16),
                                       _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
     _check("moe_grouped_swiglu_ffn_mx4", st)
     return y_perm, ws
