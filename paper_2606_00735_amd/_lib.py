@@ -922,8 +922,10 @@ def _mx4_layout(codes, scales, K):
         raise ValueError("codes and scales must be on one device")
     if codes.is_contiguous():
         return shape, row
-    ld = codes.stride(-2) if R > 1 else row
-    if codes.stride(-1) != 1 or ld < row or (n == 3 and B > 1 and codes.stride(0) != R * ld):
+    # matrices of one row have no stride between rows: theirs is that between the matrices
+    many = n == 3 and B > 1
+    ld = codes.stride(-2) if R > 1 else (codes.stride(0) if many else row)
+    if codes.stride(-1) != 1 or ld < row or (many and codes.stride(0) != R * ld):
         raise ValueError("MXFP4 codes must be dense or rows padded to a common stride")
     return shape, ld
 

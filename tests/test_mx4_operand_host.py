@@ -70,3 +70,20 @@ def test_operands_keep_what_they_were_made_of(name):
 def test_operands_on_the_cpu_are_refused():
     with pytest.raises(ValueError, match="GPU"):
         moe.moe_mx4_dequantize(operand((4,), 256))
+
+
+@pytest.mark.parametrize("B,R,ld", [(3, 1, 160), (1, 1, 160), (1, 4, 160), (3, 4, 160), (3, 1, 128)])
+def test_padded_rows(B, R, ld):
+    """Rows ld bytes apart, in batches and matrices of one as well."""
+    codes = torch.zeros((B, R, ld), dtype=torch.uint8)[..., :128]
+    scales = torch.zeros((B, 1, R, 2), dtype=torch.int32)
+    t = moe.Mx4Tensor(codes, scales, 256)
+    assert t.shape == (B, R, 256) and t.ld == (ld if B * R > 1 else 128)
+
+
+def test_rows_that_are_not_a_common_stride_apart_are_refused():
+    with pytest.raises(ValueError, match="common stride"):  # matrices of one row that overlap
+        moe.Mx4Tensor(torch.zeros(400, dtype=torch.uint8).as_strided((3, 1, 128), (100, 100, 1)),
+                      torch.zeros((3, 1, 1, 2), dtype=torch.int32), 256)
+    with pytest.raises(ValueError, match="common stride"):  # room between the matrices
+        moe.Mx4Tensor(torch.zeros((3, 8, 128), dtype=torch.uint8)[:, :4], torch.zeros((3, 1, 4, 2), dtype=torch.int32), 256)
