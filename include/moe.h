@@ -584,7 +584,7 @@ moe_status moe_load_sweep_mx(const uint8_t* xq, const uint32_t* xs, const uint8_
  * ws       its first 256 bytes must be zero before the first call on it (every call
  *          leaves them zero); calls that share one, of any sizes, must not overlap
  * Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), T a multiple of seq_len, T * E <=
- * 2^40 and at most 2^23 blocks of 16 tokens or more of a group.
+ * 2^40 and fewer than 2^23 blocks of 16 tokens or more of a group.
  * Sums are fp32 within a block, joined in fp64 in a fixed order: results do not
  * depend on timing.
  */

@@ -616,8 +616,9 @@ static moe_status balance_shape_ok(int T, int E, int k, int seq_len, int* n) {
   if (seq_len < 0 || (seq_len > 0 && T % seq_len != 0)) return MOE_ERR_INVALID_ARG;
   if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
   *n = seq_len > 0 ? seq_len : T;
-  // blocks of a launch
-  if (moe::balance_blocks(T, E, *n) > (1LL << 23)) return MOE_ERR_UNSUPPORTED;
+  // blocks of a launch: those of the loss have 512 threads, and a launch has less than
+  // 2^32. It also keeps T 255 away from 2^31, so that no token index passes it.
+  if (moe::balance_blocks(T, E, *n) >= (1LL << 23)) return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
 }
 

@@ -191,7 +191,8 @@ __global__ __launch_bounds__(256) void balance_count_kernel(RowArgs a, LossWs ws
   __shared__ int32_t s_cnt[kMaxExperts];
   __shared__ int32_t s_live;
   const int tid = threadIdx.x, p = blockIdx.x;
-  const int t0 = min(p * tok, a.n), t1 = min(t0 + tok, a.n);  // p * tok < n + tok <= 2^31
+  // less than 2^31 (as count_ids' steps past t1 are): n <= 2^31 - 256 (moe_abi.cpp)
+  const int t0 = min(p * tok, a.n), t1 = min(t0 + tok, a.n);
   for (int g = blockIdx.y; g < a.groups; g += gridDim.y) {
     s_cnt[tid] = 0;
     if (tid == 0) s_live = 0;
