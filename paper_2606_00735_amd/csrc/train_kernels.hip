@@ -558,6 +558,7 @@ hipError_t launch_gate_backward(const float* z, const int32_t* ids, const uint8_
 // (630 MB) 132-135 us, 4.7 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kCombineGradVecs = 4;  // 16-byte pieces of a row per lane in flight
+constexpr unsigned kCombineGradTokens = 1u << 25;  // of a launch
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void combine_backward_kernel(const uint4* __restrict__ dout,
@@ -565,11 +566,11 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const uint4* __re
                                                                const float* __restrict__ w,
                                                                const int32_t* __restrict__ dest, int T, int k,
                                                                int row_vecs, int M_cap, float* __restrict__ dw,
-                                                               uint4* __restrict__ dy) {
+                                                               uint4* __restrict__ dy, unsigned first) {
   constexpr int U = kCombineGradVecs, N = BF16 ? 8 : 4;
   const int lane = threadIdx.x & 63;
-  const int t = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (t >= T) return;
+  const unsigned t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) + first;
+  if (t >= (unsigned)T) return;
   // assignment j sits in lane j
   int d = -1;
   float wt = 0.0f;
@@ -649,15 +650,21 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const uint4* __re
 
 hipError_t launch_combine_backward(const void* dout, const void* y, const float* w, const int32_t* dest, int T, int k,
                                    int H, int M_cap, bool bf16, float* dw, void* dy, hipStream_t s) {
-  const unsigned grid = (unsigned)((T + 3) / 4);
-  if (bf16)
-    combine_backward_kernel<true><<<grid, 256, 0, s>>>(static_cast<const uint4*>(dout), static_cast<const uint4*>(y),
-                                                       w, dest, T, k, H / 8, M_cap, dw, static_cast<uint4*>(dy));
-  else
-    combine_backward_kernel<false><<<grid, 256, 0, s>>>(static_cast<const uint4*>(dout),
-                                                        static_cast<const uint4*>(y), w, dest, T, k, H / 4, M_cap, dw,
-                                                        static_cast<uint4*>(dy));
-  return hipGetLastError();
+  // a launch has less than 2^32 threads: more than kCombineGradTokens tokens take several
+  for (unsigned first = 0; first < (unsigned)T; first += kCombineGradTokens) {
+    const unsigned grid = (std::min((unsigned)T - first, kCombineGradTokens) - 1) / 4 + 1;
+    if (bf16)
+      combine_backward_kernel<true><<<grid, 256, 0, s>>>(static_cast<const uint4*>(dout),
+                                                         static_cast<const uint4*>(y), w, dest, T, k, H / 8, M_cap, dw,
+                                                         static_cast<uint4*>(dy), first);
+    else
+      combine_backward_kernel<false><<<grid, 256, 0, s>>>(static_cast<const uint4*>(dout),
+                                                          static_cast<const uint4*>(y), w, dest, T, k, H / 4, M_cap,
+                                                          dw, static_cast<uint4*>(dy), first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace moe

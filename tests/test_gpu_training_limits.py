@@ -49,3 +49,32 @@ def test_balance_at_the_block_limit(T, seq):
     want = 2 * lse * torch.tensor([0.25, 0.75], device=DEV)
     for at in (slice(0, 300), slice(T // 2, T // 2 + 300), slice(T - 300, T)):
         assert ((d[at] - want).abs() <= 128 * U * want).all()
+
+
+@pytest.mark.parametrize("T", [2 ** 25, 2 ** 25 + 1, 2 ** 26 + 5, 2 ** 31 - 1])
+def test_combine_backward_of_many_tokens(T):
+    """All remote but some tokens at the ends and around every 2^25-th: dw = <dout, y>."""
+    banner("combine limit", T)
+    H = 4
+    at = sorted({a for b in range(0, T + 2 ** 25, 2 ** 25) for a in (b - 1, b, b + 3) if 0 <= a < T} | {T - 4, T - 1})
+    n = len(at)
+    r = torch.Generator(device=DEV)
+    r.manual_seed(T)
+    where = torch.tensor(at, device=DEV)
+    y = torch.randn((n, H), generator=r, device=DEV)
+    do = torch.randn((n, H), generator=r, device=DEV)
+    w = torch.rand(n, generator=r, device=DEV)
+    order = torch.randperm(n, generator=r, device=DEV)
+    dout = torch.ones((T, H), device=DEV)
+    dout[where] = do
+    dest = torch.full((T,), -1, dtype=torch.int32, device=DEV)
+    dest[where] = order.int()
+    weights = torch.zeros((T, 1), device=DEV)
+    weights[where, 0] = w
+    dw = torch.full((T, 1), 7.0, device=DEV)
+    _, dy = moe.moe_combine_backward(dout, y, weights, dest, dweights=dw)
+    want, size = (do.double() * y[order].double()).sum(1), (do * y[order]).abs().sum(1)
+    assert ((dw[where, 0].double() - want).abs() <= 4 * U * size).all()
+    assert torch.equal(dy[order], w.unsqueeze(1) * do)
+    dw[where] = 0.0
+    assert not dw.any()
