@@ -127,7 +127,7 @@ __global__ __launch_bounds__(512) void router_dw_kernel(RouterGradArgs a) {
   const int E = a.E, H = a.H;
   const int sp = (int)(blockIdx.x % (unsigned)a.S), tile = (int)(blockIdx.x / (unsigned)a.S);
   const int c0 = tile * kRgCols;
-  const int chunks = (a.T + kRgTok - 1) / kRgTok;
+  const int chunks = (a.T - 1) / kRgTok + 1;
   const int q0 = uniform_int((int)((long long)sp * chunks / a.S));
   const int q1 = uniform_int((int)((long long)(sp + 1) * chunks / a.S));
 
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256, 2) void router_dx_kernel(RouterGradArgs a, int
     }
     // lane (r, h) holds columns 8 g + 4 h + (0..3) of each 32 of its token: to whole
     // rows of 64 columns through the wave's LDS
-    const bool whole = row0 + 32 <= a.T && (tl + 1) * kRgCols <= H;
+    const bool whole = a.T - row0 >= 32 && (tl + 1) * kRgCols <= H;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       auto at = [](int r, int piece) { return r * 128 + ((piece ^ (r & 7)) * 16); };
@@ -404,12 +404,12 @@ __global__ __launch_bounds__(256) void router_dw_f32_kernel(const float* __restr
   const int tile = (int)(blockIdx.x % (unsigned)tiles), r = (int)(blockIdx.x / (unsigned)tiles);
   const int e0 = r % eg * 8, sp = r / eg;
   const int c = tile * 64 + lane;
-  const int t0 = (int)((long long)sp * T / S), t1 = (int)((long long)(sp + 1) * T / S);
+  const unsigned t0 = (unsigned)((long long)sp * T / S), t1 = (unsigned)((long long)(sp + 1) * T / S);
   float acc[8], sum[8];
 #pragma unroll
   for (int q = 0; q < 8; ++q) acc[q] = sum[q] = 0.0f;
 #pragma unroll 4
-  for (int t = t0 + wave; t < t1; t += 4) {
+  for (unsigned t = t0 + wave; t < t1; t += 4) {  // unsigned: the last step passes T <= 2^31 - 1
     const float xv = c < H ? x[(size_t)t * H + c] : 0.0f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
@@ -469,7 +469,7 @@ hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int
       router_dw_kernel<EP, VEC><<<(unsigned)(tiles * S), 512, 0, s>>>(a);
       e = hipGetLastError();
       if (e != hipSuccess || dx == nullptr) return;
-      const int rows = (T + kDxRows - 1) / kDxRows;
+      const int rows = (T - 1) / kDxRows + 1;
       const int split = std::min(tiles, std::max(1, (2 * device_cu_count() + rows - 1) / rows));
       router_dx_kernel<EP, VEC><<<(unsigned)(rows * split), 256, 0, s>>>(a, tiles, split);
       e = hipGetLastError();

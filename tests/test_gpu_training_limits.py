@@ -78,3 +78,29 @@ def test_combine_backward_of_many_tokens(T):
     assert torch.equal(dy[order], w.unsqueeze(1) * do)
     dw[where] = 0.0
     assert not dw.any()
+
+
+@pytest.mark.parametrize("T,E,H,dtype", [(2 ** 31 - 1, 1, 8, torch.float32), (2 ** 31 - 3, 1, 8, torch.float32),
+                                         (2 ** 26 + 33, 3, 64, torch.bfloat16)])
+def test_router_grad_of_many_tokens(T, E, H, dtype):
+    """dlogits are zero but for a few tokens, at the ends and in the middle of the ranges."""
+    banner("router limit", T, E, H, dtype)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(T)
+    where = torch.tensor([0, 1, 31, T // 64, T // 2, T - 300, T - 33, T - 5, T - 2, T - 1], device=DEV)
+    n = where.numel()
+    dz = torch.zeros((T, E), device=DEV)
+    dz[where] = torch.randn((n, E), generator=g, device=DEV)
+    x = torch.ones((T, H), dtype=dtype, device=DEV)
+    x[where] = torch.randn((n, H), generator=g, device=DEV).to(dtype)
+    w = torch.randn((E, H), generator=g, device=DEV).to(dtype)
+    bf16 = dtype == torch.bfloat16
+    dx, dw, db, _ = moe.moe_router_grad(dz, x, w, need_dx=bf16)
+    a, b = dz[where].double(), x[where].double()
+    assert ((dw.double() - a.t() @ b).abs() <= 3 * n * U * (a.abs().t() @ b.abs())).all()
+    assert ((db.double() - a.sum(0)).abs() <= n * U * a.abs().sum(0)).all()
+    if bf16:
+        want, size = a @ w.double(), a.abs() @ w.abs().double()
+        assert ((dx[where].double() - want).abs() <= (2.0 ** -17 + 2 * E * U) * size + 2.0 ** -8 * want.abs()).all()
+        dx[where] = 0.0
+        assert not dx.any()
