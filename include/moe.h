@@ -638,7 +638,8 @@ moe_status moe_combine_backward(const void* dout, const void* y_perm, const floa
  * in order (results do not depend on timing); its size depends on the device's
  * compute units. As in any such product, a row of x that is not finite makes dw_router
  * NaN even where its dlogits are 0: rows of masked tokens must hold numbers. An
- * infinite dlogits gives NaN in dw_router.
+ * infinite dlogits gives NaN in dw_router, and in bf16, where the other operand meets
+ * each term of dlogits by itself, an infinite x or w_router gives NaN or an infinity.
  * Limits: 1 <= E <= 256, H % 8 == 0 (bf16: H % 64 == 0), H <= 2^20.
  */
 moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_router, int T, int E,
