@@ -96,15 +96,6 @@ __device__ __forceinline__ void dma16(const void* gaddr, const bf16_t* lds) {
                : "memory");
 }
 
-// 4 bytes a lane: lane i fills bytes [4 i, 4 i + 4) past `lds`.
-__device__ __forceinline__ void dma4(const void* gaddr, const bf16_t* lds) {
-  const uint32_t m0 = lds_addr(lds);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off"
-               :
-               : "v"(gaddr), "s"(m0)
-               : "memory");
-}
-
 // The same loads with a wave-uniform 64-bit base in SGPRs and a 32-bit
 // per-lane byte offset (global address = base + offset): one VGPR per load
 // instead of two. dma16s moves 16 bytes per lane, dma4s 4 bytes (lane i
