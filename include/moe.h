@@ -492,10 +492,12 @@ moe_status moe_grouped_gemm_mx4(const uint8_t* aq, const uint32_t* as, const uin
  * the workspace (every call leaves them zero), then h codes [M_cap, 128 C(I)]
  * and, 256-byte aligned after them, their scales, then the split plan and the
  * fp32 partial sums of tiles split along K (summed in a fixed order, so results
- * are deterministic). Calls that share a workspace must not overlap. The
- * schedules and launches are those of moe_grouped_swiglu_ffn; without a
- * reduction launch where no expert can have more than 128 rows (M_cap <= 128;
- * with perm_src min(T, M_cap) <= 128).
+ * are deterministic). Calls that share a workspace must not overlap. Each of the
+ * two products takes a kernel of its own for few rows where M_cap <= 128 and its
+ * weight codes, an expert's once per 16 rows that it can have, are at most 128 MB;
+ * otherwise one launch with the schedules of moe_grouped_swiglu_ffn, on 8 waves for
+ * every load, and a reduction launch unless no expert can have more than 128 rows
+ * (M_cap <= 128; with perm_src min(T, M_cap) <= 128).
  */
 moe_status moe_grouped_swiglu_ffn_mx4(const uint8_t* xq, const uint32_t* xs,
                                       const int32_t* perm_src, int T, int k, const uint8_t* wgq,

@@ -1075,8 +1075,9 @@ def ffn_mx4_ws_bytes(E_local, H, I, M_cap):
 def moe_grouped_swiglu_ffn_mx4(x, w_gate, w_up, w_down, offsets, ws=None, y_perm=None, perm_src=None, k=1, experts=0):
     """MXFP4 expert FFN. x: Mx4Tensor [M_cap, H], or with perm_src [M_cap] (moe_permute)
     [T, H], of which row r of the input is x[perm_src[r] // k]. ``experts`` is there for
-    calls written like moe_grouped_swiglu_ffn_gather's: there is one kernel for all
-    loads, and nothing depends on it. Returns (y_perm [M_cap, H] bf16, ws)."""
+    calls written like moe_grouped_swiglu_ffn_gather's: here the kernels are chosen by
+    M_cap, E_local and the weights' size, and nothing depends on it. Returns (y_perm
+    [M_cap, H] bf16, ws)."""
     L = load_library()
     (T, H), xq, xs = _mx4_rows(x, "x")
     M_cap, src = (T, None) if perm_src is None else (perm_src.numel(), _dev(perm_src, "perm_src", torch.int32))

@@ -28,7 +28,9 @@ namespace moe {
 constexpr int kQRows = 16, kQChunks = 2;
 
 // A block's share: kQRows rows from row0 on of matrix b, kQChunks chunks from
-// chunk0 on. At most 2^31 of them (batch * rows * K <= 2^40, K >= 32).
+// chunk0 on. Fewer than 2^32 - 2^20 of them, so that a block's step past the last does
+// not wrap: K <= 512 is one group of chunks, rows <= 16 one of rows, and batch * rows * K
+// <= 2^40 with batch < 2^31 leaves at most 4.05e9 (17 rows of K = 32).
 struct QTile {
   size_t b;
   int row0, chunk0;
