@@ -939,12 +939,13 @@ class Mx4Tensor:
     operands accept. An operand keeps its codes and scales; what they hold may change,
     their sizes may not (a call refuses what was resized since)."""
 
-    __slots__ = ("_codes", "_scales", "_K", "_shape", "_ld", "_codes_n", "_scales_n")
+    __slots__ = ("_codes", "_scales", "_K", "_shape", "_ld", "_dense", "_codes_b", "_scales_b")
 
     def __init__(self, codes, scales, K):
         self._shape, self._ld = _mx4_layout(codes, scales, K)
         self._codes, self._scales, self._K = codes, scales, K
-        self._codes_n, self._scales_n = codes.numel(), scales.numel()
+        self._dense = self._ld == (K + 255) // 256 * 128
+        self._codes_b, self._scales_b = codes.nbytes, scales.nbytes
 
     codes = property(lambda self: self._codes)
     scales = property(lambda self: self._scales)
@@ -1002,12 +1003,11 @@ def _mx4(t, name, dims=0):
     codes, scales, shape, ld = t._codes, t._scales, t._shape, t._ld
     if dims and len(shape) != dims:
         raise TypeError(f"{name} must have {dims} dimensions")
-    # dense codes and scales of as many elements as at first are as they were checked
-    # then; all others (and padded rows) are looked at whole
-    if not (codes.is_contiguous() and scales.is_contiguous() and codes.numel() == t._codes_n
-            and scales.numel() == t._scales_n and codes.dtype is torch.uint8 and scales.dtype is torch.int32):
-        if _mx4_layout(codes, scales, t._K) != (shape, ld):
-            raise ValueError(f"{name}: codes must be of the size that the Mx4Tensor was made with")
+    # dense codes and scales of as many bytes as at first hold what was checked then; all
+    # others (and padded rows) are looked at whole
+    if not (codes.is_contiguous() and scales.is_contiguous() and codes.nbytes == t._codes_b
+            and scales.nbytes == t._scales_b) and _mx4_layout(codes, scales, t._K) != (shape, ld):
+        raise ValueError(f"{name}: codes must be of the size that the Mx4Tensor was made with")
     if not (codes.is_cuda and scales.is_cuda):
         raise ValueError(f"{name} must be on the GPU (libmoe has no CPU path)")
     return shape, ld, codes.data_ptr(), scales.data_ptr()
@@ -1015,8 +1015,8 @@ def _mx4(t, name, dims=0):
 
 def _mx4_rows(t, name):
     """The same of rows of activations [R, K]: only weights may have padded code rows."""
-    shape, ld, codes, scales = _mx4(t, name, 2)
-    if ld != t._codes.shape[1]:
+    shape, _, codes, scales = _mx4(t, name, 2)
+    if not t._dense:
         raise ValueError(f"{name} must have dense code rows")
     return shape, codes, scales
 
