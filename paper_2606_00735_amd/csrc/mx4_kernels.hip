@@ -184,12 +184,14 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint32_t* scales, i
 // schedules of the bf16 FFN (grouped_gemm.hpp).
 //
 // Measured, gate/up + down: decode (8 experts of 8 rows, H = 4096, I = 14336, 749 MB
-// of weights) 92 + 46 us, 5.4 TB/s, the memory's streaming rate; 128 experts of about
-// 60 rows (H = 2048, I = 768) 62 + 41 us, 3.1 TB/s, bound by the L1 misses a CU keeps
-// in flight, since 64 token rows a tile come along with 128 to 256 weight rows;
-// prefill (8192 rows, H = 4096, I = 14336) 628-673 + 290-312 us with their reductions'
-// 20 us, 2.9 PFLOP/s: MFMAs busy 44 % of gate/up and 60 % of down at 1.7 GHz, the rest
-// what stands around the K loop, as follows.
+// of weights) 92 + 47 us, 5.4 TB/s, the memory's streaming rate (95 L1 misses in flight
+// a CU); 128 experts of about 60 rows (H = 2048, I = 768) 62 + 41 us, 3.1 TB/s: the
+// pipelines' fills and the epilogues of K loops of 8 and of 3 chunks (56 and 40 misses
+// in flight); prefill (8192 rows, H = 4096, I = 14336) 620-665 + 280-303 us and their
+// reductions' 20 us, 3.0 PFLOP/s: MFMAs busy 39 % of the cycles of gate/up and 40 % of
+// down, the rest the LDS and issue of the K loop and what stands around it, as follows;
+// the cycles are the same at a clock of 2.2 GHz (547 + 267 us, launches with pauses
+// between them) and at the lower one that power leaves to launches in a row.
 // ---------------------------------------------------------------------------
 // 8 waves for every tile: the 256-row tile in quadrant phases on 4 waves that bf16
 // and MXFP8 take for large experts was no faster at 4 bits (FFN us, 4 / 8 waves, 8
@@ -256,6 +258,13 @@ __global__ __launch_bounds__(256) void split_reduce_mx4_kernel(GemmArgs a) {
 // I = 2048, 1 of 1 (15 MB) 21.0 / 17.1, 1 of 64 31.4 / 24.1, 1 of 128 43.4 / 40.1, 8 of 1
 // (117 MB) 52.6 / 45.7, 8 of 14 57.8 / 64.5, 32 of 4 (470 MB) 153 / 166; H = 4096, I =
 // 14336, 1 of 1 (59 MB) 32.2 / 33.0, 2 of 60 62.9 / 171, 8 of 8 (470 MB) 146 / 175.
+// The rule takes each product by itself, so that the halves of a call may differ (us, the
+// decode schedule for both / as chosen / this for both, in a graph): H = 2048, I = 768,
+// 96 rows on 70 of 128 experts 58 / 53 / 48, 128 rows on 86 67 / 59 / 55; H = 7168, I = 2048,
+// 32 experts, two of them with a row of 16 that they might have 29 / 23 / 21, and where
+// 32 and 128 rows might be there but 5 and 18 are, 41 / 41 / 36 and 84 / 85 / 88; H = 5120, I
+// = 8192, 16 experts, one row of 4 32 / 30 / 27, 15 of 64 128 / 129 / 147. It counts the
+// rows that may be there, not those that are, and so gives some away on a shard.
 // A step of two chunks instead of four: 17.3 for 16.9, 46.1 for 45.7. At most 80
 // registers, so that a CU holds three blocks: 64 experts of 1 row 41.8 for 44.0 with
 // two; with 64 registers (four blocks, some spilt) 56, with all of a step's loads issued

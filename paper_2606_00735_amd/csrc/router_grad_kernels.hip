@@ -84,10 +84,11 @@ __device__ __forceinline__ void split8_nearest(const float (&f)[8], bf16x8_t (&f
 // every dz value is cut into its terms once, by the wave that owns its expert, as
 // it is read (lanes across experts: a row of LDS is read without conflicts). Two
 // waves on a SIMD: one's MFMAs run while the other cuts.
-// Bound by the chip's power: 16384 tokens, H = 7168, E = 256 take 192-243 us (60
-// GFLOP, three times that on the MFMAs: 0.74-0.94 PFLOP/s), MFMAs busy 59 % at 1.42
-// GHz. Two terms lost bits (relative error 2.5e-6 for 2e-7); the 60 GFLOP alone take
-// 390 us at the rate of a large fp32 product.
+// 16384 tokens, H = 7168, E = 256 take 190-240 us (60 GFLOP, three times that on the
+// MFMAs: 0.75-0.95 PFLOP/s): 372 thousand cycles, MFMAs busy in 43 % of them, the rest
+// the reads and cuts of dz; at a clock of 2.3 GHz 169 us (launches with pauses between
+// them), in a row at what power leaves. Two terms lost bits (relative error 2.5e-6 for
+// 2e-7); the 60 GFLOP alone take 390 us at the rate of a large fp32 product.
 // Experts past E are computed from other rows' values and not stored. Blocks of one
 // token range follow each other by the number of ranges, so that (for 2, 4 or 8 of
 // them) an XCD works on one or a few ranges and reads their dz from its L2.
@@ -252,9 +253,9 @@ __global__ __launch_bounds__(256) void router_dw_reduce_kernel(const float* __re
 // direct loads, NS pieces in a ring. Fragments of W are read one 16-expert step
 // ahead of the MFMAs. Blocks that walk the same columns follow each other by the
 // number of column ranges, so that (for 2, 4 or 8 of them) an XCD's L2 holds one or
-// a few ranges of W. 16384 tokens, H = 7168, E = 256: 110-135 us (60 GFLOP, twice that
-// on the MFMAs, and 235 MB written), MFMAs busy 60 % at 1.71 GHz: power, then the
-// stores.
+// a few ranges of W. 16384 tokens, H = 7168, E = 256: 111-131 us (60 GFLOP, twice that
+// on the MFMAs, and 235 MB written): 210 thousand cycles, MFMAs busy in 49 % of them,
+// then the stores; 106 us at 2.2 GHz, in a row at what power leaves.
 // ---------------------------------------------------------------------------
 constexpr int kDxRows = 128;
 
