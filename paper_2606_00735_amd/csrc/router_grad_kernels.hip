@@ -4,7 +4,7 @@
 // dz is fp32, x and W bf16, and the MFMA takes bf16 pairs: dz is cut into bf16
 // terms, each multiplied with the exact other operand and summed in fp32. For dW,
 // fp32 like the sums, three terms hold all 24 bits of an element; for dx, rounded
-// to bf16 (2^-9 of its value), two rounded to nearest are enough: they are off by at
+// to bf16 (2^-8 of its value), two rounded to nearest are enough: they are off by at
 // most 2^-17 of an element, in either direction. (Cut off, as the three are, two would
 // lose up to 2^-15, always towards zero, which shows where dx is small beside its
 // terms: rows of dz sum to nearly nothing, and the rows of W may have much in common.)

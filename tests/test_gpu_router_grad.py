@@ -4,7 +4,7 @@ staged weights can go wrong, against float64.
 Tolerances (fixed before any GPU run), u = 2^-24:
 * dx: dz enters as two bf16 terms rounded to nearest, off by at most 2^-17 of an
   element; n products are summed in fp32, n u of their sizes (2 n u for the two
-  terms); one rounding to bf16, 2^-8 of the value with both sides of a boundary.
+  terms); one rounding to bf16, 2^-8 of the value.
 * dW: dz enters whole, in three bf16 terms whose products with a bf16 are exact in fp32,
   so a single product is off by the two additions of its parts, 4 u with room to spare
   (without the third term by up to 2^-15); T products in 2 T u more.
