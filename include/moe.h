@@ -58,6 +58,10 @@ typedef enum moe_status {
 
 typedef enum moe_dtype { MOE_F32 = 0, MOE_BF16 = 1 } moe_dtype;
 
+/* Scores of moe_route and activations of moe_linear. */
+typedef enum moe_score { MOE_SIGMOID = 0, MOE_SOFTMAX = 1 } moe_score;
+typedef enum moe_act { MOE_ACT_NONE = 0, MOE_ACT_RELU = 1, MOE_ACT_SILU = 2, MOE_ACT_GELU = 3 } moe_act;
+
 /* Short text for a status code (static storage, never NULL). */
 const char* moe_status_string(moe_status s);
 
@@ -647,6 +651,126 @@ moe_status moe_combine_backward(const void* dout, const void* y_perm, const floa
 moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_router, int T, int E,
                            int H, moe_dtype dt, void* dx, float* dw_router, float* dbias, void* ws,
                            size_t* ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Around the routed experts: routing by scores, groups and a bias for balance
+ * (in moe_gate_topk's place, on its logits), dense products with an epilogue
+ * (a shared expert, added to the routed ones' output), dropout of the layer's
+ * output, and their gradients.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * moe_route - experts and gate weights of a token from scores of its logits.
+ *
+ *   s_e = sigmoid(z_e), or exp(z_e) / sum_i exp(z_i)
+ *   c_e = s_e + bias_e: what experts are selected by; the weights do not see bias
+ *   Experts form n_group groups of E / n_group consecutive ones. A group's score is
+ *   the sum of its two largest c (of its one c, where it has one to select); the
+ *   topk_group groups of the largest scores are kept.
+ *   ids[t,:] = the k experts of kept groups with the largest c, in that order; equal
+ *              values go to the lower group and the lower expert id
+ *   w[t,j]   = scale * s_j, or with norm scale * s_j / sum of the selected s (a ratio
+ *              that selected scores have where they underflow, too)
+ * s and c are computed in 64 bits, w is rounded to fp32 once.
+ *
+ * An expert whose logit is -inf, or whose c is -inf or NaN, is not selected (a -inf
+ * takes part in a softmax with 0). A slot for which no expert is left, and every slot of a
+ * token that mask marks as not live (0), gets id -1 and weight 0: moe_expert_histogram_scan
+ * and moe_permute pass over it. A live row with a NaN logit (or, in a softmax, with +inf) has
+ * NaN weights; its ids are of its other experts.
+ *
+ * logits [T, E] fp32; bias [E] fp32 or NULL; mask [T] uint8 or NULL (all live)
+ * ids [T, k] int32, w [T, k] fp32: written completely
+ * Limits: 1 <= E <= 256, n_group divides E, 1 <= topk_group <= n_group,
+ * 1 <= k <= min(topk_group * E / n_group, 16), scale finite, T * E <= 2^40.
+ */
+moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask, int T, int E, int k,
+                     moe_score score, int n_group, int topk_group, int norm, double scale, int32_t* ids,
+                     float* w, hipStream_t stream);
+
+/*
+ * moe_route_backward - gradient of moe_route's weights to the logits.
+ *
+ * With r_j = s_j / (sum of the selected s), sums over the slots j of a token, and
+ * "slots of e" those with ids[t,j] == e (which carry no gradient of their own):
+ *   sigmoid:         dlogits[t,e] = sum over slots of e of scale dw_j s_j (1 - s_j)
+ *   sigmoid, norm:   ... of scale r_j (dw_j - sum_i r_i dw_i) (1 - s_j)
+ *   softmax:         s_e scale (sum over slots of e of dw_j - sum_i s_i dw_i)
+ *   softmax, norm:   sum over slots of e of scale r_j (dw_j - sum_i r_i dw_i)
+ * in fp32. Slots whose id is outside [0, E) add nothing. accumulate != 0 adds to what
+ * dlogits holds (moe_gate_backward's gradient of the losses, say).
+ *
+ * logits [T, E], dw [T, k] fp32; ids [T, k] int32; dlogits [T, E] fp32, written completely;
+ * it must not overlap logits. Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), scale finite,
+ * T * E <= 2^40.
+ */
+moe_status moe_route_backward(const float* logits, const int32_t* ids, const float* dw, int T, int E, int k,
+                              moe_score score, int norm, double scale, int accumulate, float* dlogits,
+                              hipStream_t stream);
+
+/*
+ * moe_linear - a dense product with an epilogue.
+ *
+ *   z = x w^T + bias                          (fp32 accumulation)
+ *   y = round_dt( act(z) * mul + residual )   (fp32, rounded once)
+ * act: none, max(z, 0), z / (1 + exp(-z)), or z times the normal distribution's integral
+ * up to z. A gated projection is act and mul, a down projection added to the routed
+ * experts' output is residual.
+ *
+ * x [M, K] dt; w [N, K] dt, rows ldw elements apart (0: K; otherwise as the expert
+ * weights' strides); bias [N] fp32, mul and residual [M, N] dt: each may be NULL
+ * y [M, N] dt; it may be mul or residual itself. z [M, N] dt or NULL: round_dt(z), what
+ *   moe_linear_backward needs of a layer with an activation; not y
+ * ws: partial sums of products of few tiles, split along K and joined in a fixed order
+ *   (results do not depend on timing). Its size depends on the device's compute units;
+ *   it need not hold anything; calls that share one must not overlap.
+ * Limits: N % 8 == 0, K % 8 == 0, 8 <= N, K <= 2^20, M <= 2^28, and M N, M K, N K <= 2^36
+ * (fp32: 2^34). M == 0 is a no-op.
+ */
+moe_status moe_linear(const void* x, const void* w, const float* bias, const void* mul, const void* residual,
+                      int M, int N, int K, int ldw, moe_act act, moe_dtype dt, void* y, void* z, void* ws,
+                      size_t* ws_bytes, hipStream_t stream);
+
+/*
+ * moe_linear_backward - the gradients of moe_linear.
+ *
+ *   dmul  = round_dt( dy * act(z) )
+ *   dz    = round_dt( dy * mul * act'(z) )      (dy itself without act and mul)
+ *   dbias = sum over rows of dz, before it is rounded
+ *   dx    = round_dt( dz w )                    (fp32 accumulation, of the rounded dz)
+ *   dw    = round_dw_dt( dz^T x )
+ * The residual's gradient is dy. act'(0) of max(z, 0) is 0.
+ *
+ * dy [M, N] dt; z [M, N] dt as moe_linear wrote it: required with an activation and
+ *   for dmul, otherwise not read; mul [M, N] dt or NULL; x, w, ldw as moe_linear
+ * dz [M, N] dt: required with an activation or mul (it may be dy itself), not written
+ *   without; dmul [M, N] dt or NULL (NULL without mul; not dz, dy or mul)
+ * dx [M, K] dt or NULL; dw [N, K] of dw_dt or NULL (fp32 data: fp32; bf16 data: either);
+ * dbias [N] fp32 or NULL
+ * ws and limits as moe_linear. M == 0 writes zeros to dw and dbias.
+ */
+moe_status moe_linear_backward(const void* dy, const void* x, const void* w, const void* z, const void* mul,
+                               int M, int N, int K, int ldw, moe_act act, moe_dtype dt, void* dz, void* dmul,
+                               void* dx, void* dw, moe_dtype dw_dt, float* dbias, void* ws, size_t* ws_bytes,
+                               hipStream_t stream);
+
+/*
+ * moe_dropout_add - dropout by a counter-based generator, and a residual.
+ *
+ *   out_i = round_dt( residual_i + (u_i < floor(2^32 p) ? 0 : x_i * fl32(1 / (1 - p))) )
+ * u_i is word i % 4 of Philox4x32 with 10 rounds at counter offset + i / 4 (64 bits, modulo
+ * 2^64; the counter's upper half is 0) under the 64-bit key seed. The mask is never stored:
+ * the gradient to x is the same call on the gradient of out, without a residual. A call on n
+ * elements uses ceil(n / 4) counters: the caller moves offset on between calls that are to
+ * differ.
+ *
+ * x, residual (or NULL), out [n] dt; out may be x or residual itself
+ * rng [2] uint64 (DEVICE): seed, offset; read when the call runs, so a captured call takes
+ *   what a replay finds there
+ * Limits: 0 <= p < 1, n <= 2^40. n == 0 is a no-op.
+ */
+moe_status moe_dropout_add(const void* x, const void* residual, long long n, double p, const uint64_t* rng,
+                           moe_dtype dt, void* out, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * Placement control path (Section 4.2, Algorithms 1 and 2): the per-GPU

@@ -21,16 +21,20 @@ from ._lib import (  # noqa: F401
     Mx4Tensor,
     MxTensor,
     balance_ws_bytes,
+    dropout_counters,
     ffn_hidden,
     ffn_mx4_ws_bytes,
     ffn_mx_ws_bytes,
     ffn_ws_bytes,
     gate_ws_bytes,
     hist_ws_bytes,
+    linear_backward_ws_bytes,
+    linear_ws_bytes,
     load_library,
     moe_balance_loss,
     moe_combine_backward,
     moe_drift_distance,
+    moe_dropout_add,
     moe_expert_histogram_scan,
     moe_fit_latency_model,
     moe_gate_backward,
@@ -45,6 +49,8 @@ from ._lib import (  # noqa: F401
     moe_grouped_swiglu_mx,
     moe_grouped_swiglu_mx4,
     moe_layer,
+    moe_linear,
+    moe_linear_backward,
     moe_load_sweep,
     moe_load_sweep_mx,
     moe_mx4_dequantize,
@@ -54,6 +60,8 @@ from ._lib import (  # noqa: F401
     moe_place_greedy,
     moe_place_incremental,
     moe_placement_cost,
+    moe_route,
+    moe_route_backward,
     moe_router_grad,
     moe_unpermute_combine,
     moe_window_push,

@@ -29,7 +29,8 @@ EXPORTED = ("moe_status_string", "moe_abi_version", "moe_gate_topk", "moe_expert
             "moe_grouped_swiglu_ffn_gather", "moe_grouped_swiglu_ffn_gather_of",
             "moe_grouped_swiglu_ffn_noalloc", "moe_ffn_scratch_bytes", "moe_mx4_quantize", "moe_mx4_dequantize",
             "moe_grouped_swiglu_mx4", "moe_grouped_gemm_mx4", "moe_grouped_swiglu_ffn_mx4", "moe_balance_loss",
-            "moe_gate_backward", "moe_combine_backward", "moe_router_grad")
+            "moe_gate_backward", "moe_combine_backward", "moe_router_grad", "moe_route", "moe_route_backward", "moe_linear",
+            "moe_linear_backward", "moe_dropout_add")
 
 
 class MoeError(RuntimeError):
@@ -124,6 +125,16 @@ def load_library(path: str = LIB_PATH):
     L.moe_combine_backward.argtypes = [_P, _P, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P]
     L.moe_router_grad.restype = _I
     L.moe_router_grad.argtypes = [_P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _PSZ, _P]
+    L.moe_route.restype = _I
+    L.moe_route.argtypes = [_P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _D, _P, _P, _P]
+    L.moe_route_backward.restype = _I
+    L.moe_route_backward.argtypes = [_P, _P, _P, _I, _I, _I, _I, _I, _D, _I, _P, _P]
+    L.moe_linear.restype = _I
+    L.moe_linear.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _PSZ, _P]
+    L.moe_linear_backward.restype = _I
+    L.moe_linear_backward.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P, _PSZ, _P]
+    L.moe_dropout_add.restype = _I
+    L.moe_dropout_add.argtypes = [_P, _P, ctypes.c_longlong, _D, _P, _I, _P, _P]
     if L.moe_abi_version() != 3:
         raise RuntimeError("libmoe ABI version mismatch")
     _lib = L
@@ -460,13 +471,16 @@ def moe_load_sweep(x, w_gate, w_up, w_down, Ms, warmup=3, iters=10, y_scratch=No
 # Whole layer: the five stream-ordered calls, no host synchronisation.
 # ---------------------------------------------------------------------------
 def moe_layer(x, w_router, bias, k, expert_map, w_gate, w_up, w_down, logits=False, bufs=None,
-              fuse_gather=False):
+              fuse_gather=False, route=None):
     """One GPU's share of the MoE layer; returns a dict of every output.
 
     ``bufs`` (optional dict) supplies preallocated outputs and workspaces so
     that repeated calls allocate nothing. ``fuse_gather`` (bf16): the FFN
     reads the routed rows of x itself (moe_grouped_swiglu_ffn_gather) and
     x_perm is not built (None in the result); every other output is the same.
+    ``route`` (a dict of moe_route's score, n_group, topk_group, norm, scale and mask)
+    selects by moe_route on the router's product; ``bias`` then counts for the selection
+    only.
     """
     b = {} if bufs is None else bufs
     T = x.shape[0]
@@ -475,8 +489,15 @@ def moe_layer(x, w_router, bias, k, expert_map, w_gate, w_up, w_down, logits=Fal
     if gws is None:
         need = gate_ws_bytes(T, x.shape[1], E, x.dtype)
         gws = torch.empty(need, dtype=torch.uint8, device=x.device) if need > 0 else None
-    ids, wts, lg = moe_gate_topk(x, w_router, bias, k, logits=logits, ids=b.get("ids"),
-                                 weights=b.get("weights"), ws=gws)
+    if route is None:
+        ids, wts, lg = moe_gate_topk(x, w_router, bias, k, logits=logits, ids=b.get("ids"),
+                                     weights=b.get("weights"), ws=gws)
+    else:
+        top, top_w, lg = moe_gate_topk(x, w_router, None, 1, logits=b.get("logits", True), ids=b.get("top"),
+                                       weights=b.get("top_w"), ws=gws)
+        ids, wts = moe_route(lg, k, bias=bias, ids=b.get("ids"), weights=b.get("weights"), **route)
+        if bufs is not None:
+            bufs.update(logits=lg, top=top, top_w=top_w)
     counts, offsets, hws = moe_expert_histogram_scan(ids, E, expert_map, ws=b.get("hist_ws"),
                                                      counts=b.get("counts"), offsets=b.get("offsets"))
     x_perm, perm_src, dest = moe_permute(x, ids, expert_map, hws, x_perm=b.get("x_perm"),
@@ -653,6 +674,211 @@ def moe_router_grad(dlogits, x, w_router, dx=None, dw=None, dbias=None, ws=None,
                            _dev(dbias, "dbias", torch.float32), _dev(ws, "ws", torch.uint8), ctypes.byref(n), _stream())
     _check("moe_router_grad", st)
     return dx, dw, dbias, ws
+
+
+# ---------------------------------------------------------------------------
+# Around the routed experts: scored routing, dense products, dropout
+# ---------------------------------------------------------------------------
+SCORES = {"sigmoid": 0, "softmax": 1}
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def _code(table, name, what):
+    try:
+        return table[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"{what} must be one of {', '.join(table)}, got {name!r}") from None
+
+
+def _on(t, name, dtype, dev, shape):
+    """Pointer of a contiguous tensor of the given type and shape on GPU `dev`, the current one."""
+    p = _dev(t, name, dtype)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the current GPU, cuda:{dev}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return p
+
+
+def _weight(w, name, dtype, dev):
+    """(pointer, row stride) of a weight matrix [N, K] whose rows may be padded."""
+    if not isinstance(w, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if w.get_device() != dev:
+        raise ValueError(f"{name} must be on the current GPU, cuda:{dev} (libmoe has no CPU path)")
+    if w.dtype != dtype or w.dim() != 2:
+        raise ValueError(f"{name} must be [N, K] of {dtype}")
+    sr, sk = w.stride()
+    if w.shape[0] == 1:
+        sr = w.shape[1]
+    if sk != 1 or sr < w.shape[1]:
+        raise ValueError(f"{name} must have unit element stride and rows at least {w.shape[1]} apart")
+    return w.data_ptr(), sr
+
+
+def _matrix(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {list(t.shape)}")
+    return t.shape
+
+
+def moe_route(logits, k, score="sigmoid", bias=None, mask=None, n_group=1, topk_group=1, norm=True, scale=1.0, ids=None,
+              weights=None):
+    """Experts and gate weights from scores of the logits [T, E]: sigmoid or softmax, a bias
+    [E] that counts for the selection only, the topk_group best of n_group groups, top-k,
+    weights normalised (norm) and scaled. mask [T] uint8: 0 for tokens that get id -1 and
+    weight 0. Returns (ids [T, k] int32, weights [T, k] fp32)."""
+    L = load_library()
+    T, E = _matrix(logits, "logits")
+    dev = torch.cuda.current_device()
+    code = _code(SCORES, score, "score")
+    if ids is None:
+        ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    if weights is None:
+        weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    st = L.moe_route(_on(logits, "logits", torch.float32, dev, (T, E)),
+                     None if bias is None else _on(bias, "bias", torch.float32, dev, (E,)),
+                     None if mask is None else _on(mask, "mask", torch.uint8, dev, (T,)), T, E, k, code, n_group,
+                     topk_group, 1 if norm else 0, scale, _on(ids, "ids", torch.int32, dev, (T, k)),
+                     _on(weights, "weights", torch.float32, dev, (T, k)), _stream())
+    _check("moe_route", st)
+    return ids, weights
+
+
+def moe_route_backward(logits, ids, dweights, score="sigmoid", norm=True, scale=1.0, dlogits=None, accumulate=False):
+    """Gradient [T, E] of moe_route's weights to its logits; accumulate=True adds it to dlogits."""
+    L = load_library()
+    T, E = _matrix(logits, "logits")
+    k = _matrix(ids, "ids")[1]
+    dev = torch.cuda.current_device()
+    code = _code(SCORES, score, "score")
+    if dlogits is None:
+        if accumulate:
+            raise ValueError("accumulate needs dlogits")
+        dlogits = torch.empty_like(logits)
+    st = L.moe_route_backward(_on(logits, "logits", torch.float32, dev, (T, E)), _on(ids, "ids", torch.int32, dev, (T, k)),
+                              _on(dweights, "dweights", torch.float32, dev, (T, k)), T, E, k, code, 1 if norm else 0, scale,
+                              1 if accumulate else 0, _on(dlogits, "dlogits", torch.float32, dev, (T, E)), _stream())
+    _check("moe_route_backward", st)
+    return dlogits
+
+
+def linear_ws_bytes(M, N, K, dtype):
+    """Bytes of moe_linear's workspace."""
+    n = ctypes.c_size_t(0)
+    dt = MOE_BF16 if dtype == torch.bfloat16 else MOE_F32
+    _check("moe_linear", load_library().moe_linear(None, None, None, None, None, M, N, K, 0, 0, dt, None, None, None,
+                                                   ctypes.byref(n), None))
+    return n.value
+
+
+def linear_backward_ws_bytes(M, N, K, dtype):
+    """Bytes of moe_linear_backward's workspace."""
+    n = ctypes.c_size_t(0)
+    dt = MOE_BF16 if dtype == torch.bfloat16 else MOE_F32
+    _check("moe_linear_backward", load_library().moe_linear_backward(
+        None, None, None, None, None, M, N, K, 0, 0, dt, None, None, None, None, dt, None, None, ctypes.byref(n), None))
+    return n.value
+
+
+def _workspace(ws, need, dev, device):
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    n = ws.numel()
+    if n == 0:  # a null pointer would ask for the size
+        raise ValueError("ws must not be empty")
+    return ws, _on(ws, "ws", torch.uint8, dev, ws.shape), ctypes.byref(ctypes.c_size_t(n))
+
+
+def moe_linear(x, w, bias=None, act="none", mul=None, residual=None, z=None, out=None, ws=None):
+    """act(x w^T + bias) * mul + residual [M, N] for x [M, K] and w [N, K] (rows may be padded).
+    act: "none", "relu", "silu" or "gelu". z (a tensor [M, N]) receives the product with the
+    bias, which moe_linear_backward needs of a layer with an activation. out may be mul or
+    residual. ws: linear_ws_bytes bytes, allocated if missing."""
+    L = load_library()
+    M, K = _matrix(x, "x")
+    N = _matrix(w, "w")[0]
+    dt, dtype = _dtype_code(x), x.dtype
+    dev = torch.cuda.current_device()
+    code = _code(ACTS, act, "act")
+    if w.shape[1] != K:
+        raise ValueError(f"w must be [N, {K}], got {list(w.shape)}")
+    xp = _on(x, "x", dtype, dev, (M, K))
+    wp, ldw = _weight(w, "w", dtype, dev)
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=x.device)
+    ws, wsp, wsn = _workspace(ws, linear_ws_bytes(M, N, K, dtype) if ws is None else 0, dev, x.device)
+    st = L.moe_linear(xp, wp, None if bias is None else _on(bias, "bias", torch.float32, dev, (N,)),
+                      None if mul is None else _on(mul, "mul", dtype, dev, (M, N)),
+                      None if residual is None else _on(residual, "residual", dtype, dev, (M, N)), M, N, K, ldw, code, dt,
+                      _on(out, "out", dtype, dev, (M, N)), None if z is None else _on(z, "z", dtype, dev, (M, N)), wsp,
+                      wsn, _stream())
+    _check("moe_linear", st)
+    return out
+
+
+def moe_linear_backward(dy, x, w, z=None, act="none", mul=None, need_dx=True, need_dw=True, need_dbias=True,
+                        dw_dtype=torch.float32, dx=None, dw=None, dbias=None, dz=None, dmul=None, ws=None):
+    """Gradients of moe_linear. Returns (dx [M, K], dw [N, K] of dw_dtype, dbias [N] fp32, dz
+    [M, N], dmul [M, N]): dx, dw, dbias None where not needed, dz dy itself and dmul None
+    without act and mul. z as moe_linear filled it, with an activation or a mul. ws:
+    linear_backward_ws_bytes bytes, allocated if missing."""
+    L = load_library()
+    M, N = _matrix(dy, "dy")
+    K = _matrix(x, "x")[1]
+    dt, dtype = _dtype_code(dy), dy.dtype
+    dev = torch.cuda.current_device()
+    code = _code(ACTS, act, "act")
+    if dw_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dw_dtype must be torch.float32 or torch.bfloat16")
+    if _matrix(w, "w") != (N, K):
+        raise ValueError(f"w must be {[N, K]}, got {list(w.shape)}")
+    dyp, xp = _on(dy, "dy", dtype, dev, (M, N)), _on(x, "x", dtype, dev, (M, K))
+    wp, ldw = _weight(w, "w", dtype, dev)
+
+    def out(t, shape, kind, name):
+        t = torch.empty(shape, dtype=kind, device=dy.device) if t is None else t
+        return t, _on(t, name, kind, dev, shape)
+
+    own = code != 0 or mul is not None
+    dxp = dwp = dbp = dzp = dmp = None
+    dx, dxp = out(dx, (M, K), dtype, "dx") if need_dx else (None, None)
+    dw, dwp = out(dw, (N, K), dw_dtype, "dw") if need_dw else (None, None)
+    dbias, dbp = out(dbias, (N,), torch.float32, "dbias") if need_dbias else (None, None)
+    dz, dzp = out(dz, (M, N), dtype, "dz") if own else (dy, None)
+    dmul, dmp = out(dmul, (M, N), dtype, "dmul") if mul is not None else (None, None)
+    ws, wsp, wsn = _workspace(ws, linear_backward_ws_bytes(M, N, K, dtype) if ws is None else 0, dev, dy.device)
+    st = L.moe_linear_backward(dyp, xp, wp, None if z is None else _on(z, "z", dtype, dev, (M, N)),
+                               None if mul is None else _on(mul, "mul", dtype, dev, (M, N)), M, N, K, ldw, code, dt, dzp,
+                               dmp, dxp, dwp, MOE_BF16 if dw_dtype == torch.bfloat16 else MOE_F32, dbp, wsp, wsn,
+                               _stream())
+    _check("moe_linear_backward", st)
+    return dx, dw, dbias, dz, dmul
+
+
+def moe_dropout_add(x, p, rng, residual=None, out=None):
+    """Dropout of x with probability p, its mask from Philox4x32 keyed by rng (int64 [2] on the
+    GPU: seed, offset), plus residual. The gradient to x is the same call on the gradient,
+    without a residual. A call uses dropout_counters(x.numel()) counters from offset on."""
+    L = load_library()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch tensor")
+    dt, dtype, shape = _dtype_code(x), x.dtype, x.shape
+    dev = torch.cuda.current_device()
+    xp = _on(x, "x", dtype, dev, shape)
+    if out is None:
+        out = torch.empty_like(x)
+    st = L.moe_dropout_add(xp, None if residual is None else _on(residual, "residual", dtype, dev, shape), x.numel(), p,
+                           _on(rng, "rng", torch.int64, dev, (2,)), dt, _on(out, "out", dtype, dev, shape), _stream())
+    _check("moe_dropout_add", st)
+    return out
+
+
+def dropout_counters(n):
+    """Counters that a moe_dropout_add of n elements uses."""
+    return (n + 3) // 4
 
 
 # ---------------------------------------------------------------------------

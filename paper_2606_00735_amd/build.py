@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmoe.so")
 
 SOURCES = ["route_kernels.hip", "ffn_kernels.hip", "mx_kernels.hip", "mx4_kernels.hip", "train_kernels.hip",
-           "router_grad_kernels.hip", "placement_kernels.hip", "moe_abi.cpp"]
+           "router_grad_kernels.hip", "scored_route_kernels.hip", "linear_kernels.hip", "dropout_kernels.hip",
+           "placement_kernels.hip", "moe_abi.cpp"]
 HEADERS = ["common.hpp", "grouped_gemm.hpp", "launch.hpp", "mx.hpp"]
 
 

@@ -103,6 +103,40 @@ size_t router_grad_ws_bytes(int T, int E, int H, bool bf16);
 hipError_t launch_router_grad(const float* dz, const void* x, const void* w, int T, int E, int H, bool bf16, void* dx,
                               float* dw, float* db, void* ws, hipStream_t s);
 
+// Scored, group-limited routing (scored_route_kernels.hip). T > 0.
+hipError_t launch_route(const float* z, const float* bias, const uint8_t* mask, int T, int E, int k, bool softmax,
+                        int groups, int kept, bool norm, double scale, int32_t* ids, float* w, hipStream_t s);
+hipError_t launch_route_backward(const float* z, const int32_t* ids, const float* dw, int T, int E, int k,
+                                 bool softmax, bool norm, float scale, bool accumulate, float* dz, hipStream_t s);
+
+// Dense products with an epilogue, and their gradients (linear_kernels.hip). Activation
+// codes are moe_act's.
+enum Act : int { kActNone, kActRelu, kActSilu, kActGelu };
+struct LinearCall {
+  const void *x, *w;
+  const float* bias;
+  const void *mul, *residual;
+  int M, N, K, ldw, act;
+  bool bf16;
+  void *y, *z;
+};
+size_t linear_ws_bytes(int M, int N, int K, bool bf16);
+hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s);
+struct LinearBackwardCall {
+  const void *dy, *x, *w, *z, *mul;
+  int M, N, K, ldw, act;
+  bool bf16, dw_bf16;
+  void *dz, *dmul, *dx, *dw;
+  float* dbias;
+};
+size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16);
+hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStream_t s);
+
+// Dropout with a residual (dropout_kernels.hip): rng holds the seed and the first
+// counter. n > 0.
+hipError_t launch_dropout(const void* x, const void* residual, const uint64_t* rng, long long n, uint32_t threshold,
+                          float scale, bool bf16, void* out, hipStream_t s);
+
 // The result of the check that block b of a launch runs on XCD b % 8, for a
 // launch on stream s, or nullptr (ffn_kernels.hip).
 const int32_t* xcd_state(hipStream_t s);

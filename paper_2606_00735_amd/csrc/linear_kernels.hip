@@ -1,0 +1,607 @@
+// Dense products with an epilogue, and their gradients (gfx950):
+//   y  = act(x w^T + bias) * mul + residual
+//   dz = dy * mul * act'(z), dx = dz w, dw = dz^T x, dbias = sum of dz's rows
+//
+// All three products are C[rows, cols] = sum over k of A(row, k) B(col, k), k the
+// reduction: x and w have it along their rows; w in dx and both operands of dw have it
+// as their row index ("transposed" below). A transposed operand is copied to LDS as it
+// lies in memory and its fragments are read with the transposing read, so that no
+// operand is ever laid out anew. Sums are fp32 in the MFMA; a result is rounded once.
+#include <algorithm>
+#include <climits>
+#include <type_traits>
+
+#include "common.hpp"
+#include "grouped_gemm.hpp"
+#include "launch.hpp"
+
+namespace moe {
+
+namespace {
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------
+// Activations, fp32.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float sigmoid32(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * 1.4426950408889634f));
+}
+// the normal distribution's integral: by erfc, whose small values keep their digits
+__device__ __forceinline__ float normal_below(float z) { return 0.5f * erfcf(-0.70710678f * z); }
+
+__device__ __forceinline__ float act_value(float z, int act) {
+  switch (act) {
+    case kActRelu: return z < 0.0f ? 0.0f : z;
+    case kActSilu: return z * sigmoid32(z);
+    case kActGelu: return z * normal_below(z);
+    default: return z;
+  }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+  switch (act) {
+    case kActRelu: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    case kActSilu: {
+      const float q = sigmoid32(z);
+      return q * (1.0f + z * (1.0f - q));
+    }
+    case kActGelu: return normal_below(z) + z * 0.3989422804f * __builtin_amdgcn_exp2f(z * z * -0.7213475204f);
+    default: return 1.0f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Operands and epilogue of one product.
+// ---------------------------------------------------------------------------
+struct LinArgs {
+  const void* A;
+  const void* B;
+  int lda, ldb;          // elements between rows as they lie in memory
+  int rows, cols, red;   // C [rows, cols], dense; length of the reduction
+  int S;                 // ranges of the reduction; S > 1: sums go to part [S][rows][cols]
+  float* part;
+  // epilogue
+  const float* bias;     // [cols]
+  const void* mul;       // [rows, cols]
+  const void* res;
+  void* z;               // [rows, cols]: the sum with the bias, or null
+  void* out;             // of the operands' type, or
+  float* out32;          // fp32: the plain sum
+  int act;
+};
+
+__device__ __forceinline__ void unpack8(uint4 v, float (&f)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    f[2 * q] = __uint_as_float(w[q] << 16);
+    f[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                    pack_bf16x2(f[6], f[7]));
+}
+
+// Eight consecutive columns of a row, from their sums to memory. mul and res may be out:
+// they are read before it is written.
+__device__ __forceinline__ void finish8(const LinArgs& a, size_t row, int col, float (&v)[8]) {
+  const size_t at = row * (size_t)a.cols + (size_t)col;
+  if (a.out32 != nullptr) {
+    *reinterpret_cast<float4*>(a.out32 + at) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(a.out32 + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    return;
+  }
+  if (a.bias != nullptr) {
+    const float4 b0 = *reinterpret_cast<const float4*>(a.bias + col);
+    const float4 b1 = *reinterpret_cast<const float4*>(a.bias + col + 4);
+    v[0] += b0.x, v[1] += b0.y, v[2] += b0.z, v[3] += b0.w;
+    v[4] += b1.x, v[5] += b1.y, v[6] += b1.z, v[7] += b1.w;
+  }
+  if (a.z != nullptr) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.z) + at) = pack8(v);
+  if (a.act != kActNone) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = act_value(v[q], a.act);
+  }
+  float f[8];
+  if (a.mul != nullptr) {
+    unpack8(*reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.mul) + at), f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= f[q];
+  }
+  if (a.res != nullptr) {
+    unpack8(*reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.res) + at), f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] += f[q];
+  }
+  *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.out) + at) = pack8(v);
+}
+
+// ---------------------------------------------------------------------------
+// A panel: R rows (of C, or columns) by a chunk of 64 of the reduction, in LDS.
+// Plain: R rows of 128 bytes, swizzled as in the grouped GEMMs (swz_chunk). Transposed:
+// 64 rows (of the reduction) of 2 R bytes, whose 16-byte pieces are swizzled so that the
+// four rows of a transposing read lie in different banks. R = 64 or 128.
+// ---------------------------------------------------------------------------
+constexpr int kChunk = 64;
+
+template <int R>
+__device__ __forceinline__ int tr_piece(int row, int piece) {
+  return R == 128 ? piece ^ ((row & 3) << 2) : piece ^ (((row >> 1) & 1) << 2);
+}
+
+template <int R, bool TR, int W>
+struct Panel {
+  static_assert(R == 64 || R == 128, "panel rows");
+  static constexpr int BYTES = R * kChunk * 2;
+  static constexpr int LOADS = BYTES / (1024 * W);
+  static constexpr int RB = TR ? 2 * R : 128, PP = RB / 16, RPI = 1024 / RB;
+  static_assert(BYTES % (1024 * W) == 0, "loads of a wave");
+  const char* base;
+  size_t step;  // bytes between chunks
+  uint32_t off[LOADS];
+
+  // the panel's first row (column) and how many there are from it on; a load past the
+  // last one reads the last, whose results are not stored
+  __device__ __forceinline__ void init(const void* p, int ld, int first, int left, int wave, int lane) {
+    base = static_cast<const char*>(p) + (TR ? (size_t)first * 2 : (size_t)first * (size_t)ld * 2);
+    step = TR ? (size_t)ld * (kChunk * 2) : (size_t)(kChunk * 2);
+#pragma unroll
+    for (int t = 0; t < LOADS; ++t) {
+      const int r = (t * W + wave) * RPI + lane / PP;
+      if (TR)
+        off[t] = (uint32_t)r * (uint32_t)(ld * 2) + (uint32_t)(min(tr_piece<R>(r, lane % PP) * 8, left - 8) * 2);
+      else
+        off[t] = (uint32_t)min(r, left - 1) * (uint32_t)(ld * 2) + (uint32_t)(swz_chunk<kChunk>(r, lane % PP) * 16);
+    }
+  }
+  // load t of chunk kc; not live: the operand's first bytes, which are there in any case
+  __device__ __forceinline__ void load(int t, int kc, bool live, uint32_t lds, int wave) const {
+    const uint32_t msk = live ? 0xffffffffu : 0u;
+    dma16a(uniform_ptr(base + (live ? (size_t)kc * step : 0)), off[t] & msk, lds + (uint32_t)((t * W + wave) * 1024));
+  }
+  // the last, partial chunk (n of 64): through registers, zeros past the end
+  __device__ __forceinline__ void load_tail(int kc, int n, char* lds, int wave, int lane) const {
+    const char* p = base + (size_t)kc * step;
+#pragma unroll
+    for (int t = 0; t < LOADS; ++t) {
+      const int r = (t * W + wave) * RPI + lane / PP;
+      const bool in = TR ? r < n : swz_chunk<kChunk>(r, lane % PP) * 8 < n;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (in) v = *reinterpret_cast<const uint4*>(p + off[t]);
+      *reinterpret_cast<uint4*>(lds + (t * W + wave) * 1024 + lane * 16) = v;
+    }
+  }
+  // fragment of k-step s for rows [r0, r0 + 32): lane (r = lane % 32, h = lane / 32)
+  // holds k = 16 s + 8 h + (0..7) of row r0 + r
+  static __device__ __forceinline__ bf16x8_t frag(const char* lds, int r0, int s, int lane) {
+    if (!TR) return lds_frag<kChunk>(reinterpret_cast<const bf16_t*>(lds), r0 + (lane & 31), 2 * s + (lane >> 5));
+    // a transposing read takes 16 lanes x 8 bytes as 4 rows x 16 columns and hands lane
+    // i column i
+    const int row = 16 * s + 8 * (lane >> 5) + ((lane & 15) >> 2);
+    const int colb = r0 * 2 + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    typedef __attribute__((address_space(3))) s16x4_t* lds4;
+    const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
+    const uint32_t p0 = (uint32_t)(row * RB + tr_piece<R>(row, colb >> 4) * 16 + (colb & 15));
+    // (row + 4) & 3 and ((row + 4) >> 1) & 1 are those of row: the same piece, 4 rows on
+    const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at + p0));
+    const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at + p0 + 4 * RB));
+    struct {
+      s16x4_t lo, hi;
+    } v = {a, b};
+    return __builtin_bit_cast(bf16x8_t, v);
+  }
+};
+
+// A wave's MI x NI blocks of 32 x 32 sums, whose lanes hold 4 consecutive columns of a
+// row per register group, through its own piece of LDS to whole rows of 8 columns a
+// lane. Rows and columns past C's are not stored.
+template <int MI, int NI>
+__device__ __forceinline__ void finish_tile(const LinArgs& a, const f32x16_t (&acc)[MI][NI], char* lds, int row0,
+                                            int col0, int split, int lane) {
+  constexpr int RB = NI * 128, PP = RB / 16;
+  static_assert(PP == 8 || PP == 16, "row pieces");
+  auto key = [](int r) { return PP == 16 ? (r & 15) : ((r >> 1) & 7); };
+  const int r32 = lane & 31, hi = lane >> 5;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    if (row0 + i * 32 < a.rows) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(lds + r32 * RB + (((j * 8 + 2 * g + hi) ^ key(r32)) * 16)) =
+              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int it = 0; it < PP / 4; ++it) {
+        const int r = (it * 64 + lane) / (PP / 2), p = (it * 64 + lane) % (PP / 2);
+        const float4 u = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p) ^ key(r)) * 16));
+        const float4 w = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p + 1) ^ key(r)) * 16));
+        const int row = row0 + i * 32 + r, col = col0 + p * 8;
+        if (row < a.rows && col < a.cols) {
+          float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+          if (a.S > 1) {
+            float* q = a.part + ((size_t)split * a.rows + row) * (size_t)a.cols + col;
+            *reinterpret_cast<float4*>(q) = u;
+            *reinterpret_cast<float4*>(q + 4) = w;
+          } else {
+            finish8(a, (size_t)row, col, v);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// Tile of a block: tiles of bands of 8 row tiles, so that what runs together shares
+// operands; consecutive tiles to one XCD (block b runs on XCD b % 8).
+struct TileAt {
+  int mt, nt, split;
+};
+__device__ __forceinline__ TileAt tile_at(unsigned b, unsigned total, int mts, int nts) {
+  const unsigned x = b % 8u, i = b / 8u, q = total / 8u, r = total % 8u;
+  const unsigned t = x * q + (x < r ? x : r) + i;
+  const unsigned tiles = (unsigned)mts * (unsigned)nts;
+  const unsigned split = t / tiles, u = t % tiles;
+  const unsigned band = u / (8u * (unsigned)nts), in = u % (8u * (unsigned)nts);
+  const unsigned h = min(8u, (unsigned)mts - band * 8u);
+  return {(int)(band * 8u + in % h), (int)(in / h), (int)split};
+}
+
+// ---------------------------------------------------------------------------
+// BM x BN tile, WM_ x WN_ waves, NS chunks in LDS by direct loads (pipeline_xk).
+// ---------------------------------------------------------------------------
+template <int BM, int BN, int WR, int WC, int NS, bool TA, bool TB>
+__global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
+  constexpr int W = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+  using PA = Panel<BM, TA, W>;
+  using PB = Panel<BN, TB, W>;
+  constexpr int STAGE = PA::BYTES + PB::BYTES;
+  constexpr int LDS = STAGE * NS > W * 32 * WN * 4 ? STAGE * NS : W * 32 * WN * 4;
+  __shared__ __align__(16) bf16_t smem[LDS / 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WC, wn = wave % WC;
+  const int mts = (a.rows - 1) / BM + 1, nts = (a.cols - 1) / BN + 1;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, mts, nts);
+  const int row0 = uniform_int(at.mt * BM), col0 = uniform_int(at.nt * BN);
+  const int chunks = a.red / kChunk;
+  const int k0 = uniform_int((int)((long long)at.split * chunks / a.S));
+  const int k1 = uniform_int((int)((long long)(at.split + 1) * chunks / a.S));
+  PA pa;
+  PB pb;
+  pa.init(a.A, a.lda, row0, a.rows - row0, wave, lane);
+  pb.init(a.B, a.ldb, col0, a.cols - col0, wave, lane);
+  f32x16_t acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x16_t{};
+  constexpr int KS = kChunk / 16, LOADS = PA::LOADS + PB::LOADS;
+  auto issue = [&](int kc, bool live, bf16_t* st, int part) {
+    const uint32_t lds = lds_addr(st);
+    auto mine = [&](int t) { return part < 0 || (NS > 2 ? t * KS / LOADS : 0) == part; };
+#pragma unroll
+    for (int t = 0; t < PA::LOADS; ++t)
+      if (mine(t)) pa.load(t, k0 + kc, live, lds, wave);
+#pragma unroll
+    for (int t = 0; t < PB::LOADS; ++t)
+      if (mine(PA::LOADS + t)) pb.load(t, k0 + kc, live, lds + PA::BYTES, wave);
+  };
+  bf16x8_t fa[2][MI], fb[2][NI];
+  auto read = [&](const bf16_t* st, int s, int buf) {
+    const char* p = reinterpret_cast<const char*>(st);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[buf][i] = PA::frag(p, wm * WM + i * 32, s, lane);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) fb[buf][j] = PB::frag(p + PA::BYTES, wn * WN + j * 32, s, lane);
+  };
+  auto mma = [&](int s) {
+    const int buf = s & 1;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[buf][j], fa[buf][i], acc[i][j], 0, 0, 0);
+  };
+  pipeline_xk<NS, LOADS, KS>(k1 - k0, smem, STAGE / 2, issue, read, mma, [] {});
+  const int n = a.red - chunks * kChunk;
+  if (n > 0 && at.split == a.S - 1) {
+    char* p = reinterpret_cast<char*>(smem);
+    pa.load_tail(chunks, n, p, wave, lane);
+    pb.load_tail(chunks, n, p + PA::BYTES, wave, lane);
+    __syncthreads();
+    for (int s = 0; s * 16 < n; ++s) {
+      read(smem, s, 0);
+      mma(0);
+    }
+    __syncthreads();
+  }
+  finish_tile<MI, NI>(a, acc, reinterpret_cast<char*>(smem) + wave * (32 * WN * 4), row0 + wm * WM, col0 + wn * WN,
+                      at.split, lane);
+}
+
+// Joins the S partial sums of every output, in their order.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
+  const size_t n8 = (size_t)a.rows * (size_t)(a.cols / 8), plane = (size_t)a.rows * (size_t)a.cols;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
+    const float4 u = sum_splits(a.part + i * 8, plane, a.S), w = sum_splits(a.part + i * 8 + 4, plane, a.S);
+    float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+    const size_t row = i / (size_t)(a.cols / 8);
+    finish8(a, row, (int)(i % (size_t)(a.cols / 8)) * 8, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// fp32 (the tiny layer, a parity configuration): a 64 x 64 tile, 4 x 4 outputs a
+// thread, plain sums.
+// ---------------------------------------------------------------------------
+template <bool TA, bool TB>
+__global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
+  __shared__ float la[16][65], lb[16][65];
+  const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+  const int nts = (a.cols - 1) / 64 + 1;
+  const int row0 = (int)(blockIdx.x / (unsigned)nts) * 64, col0 = (int)(blockIdx.x % (unsigned)nts) * 64;
+  const float *A = static_cast<const float*>(a.A), *B = static_cast<const float*>(a.B);
+  float acc[4][4] = {};
+  for (int k0 = 0; k0 < a.red; k0 += 16) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int i = q * 256 + tid;
+      const int ra = TA ? i % 64 : i / 16, ka = TA ? i / 64 : i % 16;
+      const int rb = TB ? i % 64 : i / 16, kb = TB ? i / 64 : i % 16;
+      la[ka][ra] = row0 + ra < a.rows && k0 + ka < a.red
+                       ? A[TA ? (size_t)(k0 + ka) * a.lda + row0 + ra : (size_t)(row0 + ra) * a.lda + k0 + ka]
+                       : 0.0f;
+      lb[kb][rb] = col0 + rb < a.cols && k0 + kb < a.red
+                       ? B[TB ? (size_t)(k0 + kb) * a.ldb + col0 + rb : (size_t)(col0 + rb) * a.ldb + k0 + kb]
+                       : 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(la[k][ty * 4 + i], lb[k][tx + 16 * j], acc[i][j]);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = row0 + ty * 4 + i, col = col0 + tx + 16 * j;
+      if (row >= a.rows || col >= a.cols) continue;
+      const size_t at = (size_t)row * a.cols + col;
+      float v = acc[i][j];
+      if (a.bias != nullptr) v += a.bias[col];
+      if (a.z != nullptr) static_cast<float*>(a.z)[at] = v;
+      v = act_value(v, a.act);
+      if (a.mul != nullptr) v *= static_cast<const float*>(a.mul)[at];
+      if (a.res != nullptr) v += static_cast<const float*>(a.res)[at];
+      (a.out32 != nullptr ? a.out32 : static_cast<float*>(a.out))[at] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// dz = dy * mul * act'(z), dmul = dy * act(z), and partial sums of dz's columns (of the
+// fp32 values, before dz is rounded). A block: 256 columns of a range of rows, 8 columns
+// a lane, 8 rows at a time.
+// ---------------------------------------------------------------------------
+struct ActBackwardArgs {
+  const void *dy, *z, *mul;
+  void *dz, *dmul;  // or null
+  float* db;        // [P][cols], or null
+  int rows, cols, P, act;
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void act_backward_kernel(ActBackwardArgs a) {
+  __shared__ float sums[8][256];
+  const int tid = threadIdx.x, c8 = tid % 32, ry = tid / 32;
+  const int cb = (int)(blockIdx.x / (unsigned)a.P), p = (int)(blockIdx.x % (unsigned)a.P);
+  const int col = cb * 256 + c8 * 8;
+  const int r0 = (int)((long long)p * a.rows / a.P), r1 = (int)((long long)(p + 1) * a.rows / a.P);
+  float db[8] = {};
+  auto load = [&](const void* q, size_t at, float (&f)[8]) {
+    if (BF16) {
+      unpack8(*reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(q) + at), f);
+    } else {
+      const float4 u = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at);
+      const float4 w = *reinterpret_cast<const float4*>(static_cast<const float*>(q) + at + 4);
+      f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w, f[4] = w.x, f[5] = w.y, f[6] = w.z, f[7] = w.w;
+    }
+  };
+  auto store = [&](void* q, size_t at, const float (&f)[8]) {
+    if (BF16) {
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(q) + at) = pack8(f);
+    } else {
+      *reinterpret_cast<float4*>(static_cast<float*>(q) + at) = make_float4(f[0], f[1], f[2], f[3]);
+      *reinterpret_cast<float4*>(static_cast<float*>(q) + at + 4) = make_float4(f[4], f[5], f[6], f[7]);
+    }
+  };
+  if (col < a.cols) {
+    for (int r = r0 + ry; r < r1; r += 8) {
+      const size_t at = (size_t)r * a.cols + col;
+      float d[8], z[8], m[8];
+      load(a.dy, at, d);
+      if (a.z != nullptr) load(a.z, at, z);
+      if (a.mul != nullptr) load(a.mul, at, m);
+      if (a.dmul != nullptr) {
+        float g[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) g[q] = d[q] * act_value(z[q], a.act);
+        store(a.dmul, at, g);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (a.mul != nullptr) d[q] *= m[q];
+        if (a.act != kActNone) d[q] *= act_slope(z[q], a.act);
+        db[q] += d[q];
+      }
+      if (a.dz != nullptr) store(a.dz, at, d);
+    }
+  }
+  if (a.db == nullptr) return;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) sums[ry][c8 * 8 + q] = db[q];
+  __syncthreads();
+  if (cb * 256 + tid < a.cols) {
+    float s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += sums[q][tid];
+    a.db[(size_t)p * a.cols + cb * 256 + tid] = s;
+  }
+}
+
+__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, int cols, int P,
+                                                        float* __restrict__ db) {
+  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+  if (c >= cols) return;
+  float s = 0.0f;
+  for (int p = 0; p < P; ++p) s += part[(size_t)p * cols + c];
+  db[c] = s;
+}
+
+__global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// Which kernel a product takes.
+// ---------------------------------------------------------------------------
+struct LinPlan {
+  int tile;  // rows and columns of a tile
+  int S;
+};
+
+constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
+
+LinPlan linear_plan(int rows, int cols, int red) {
+  const long long cus = device_cu_count();
+  auto tiles = [&](int t) { return ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1); };
+  LinPlan p{tiles(128) >= cus ? 128 : 64, 1};
+  const long long n = tiles(p.tile);
+  const int chunks = red / kChunk;
+  if (n < cus && chunks >= 8) {
+    long long S = std::min({(2 * cus) / n, (long long)chunks / 4, 16LL});
+    const size_t plane = (size_t)rows * (size_t)cols * 4;
+    S = std::min(S, (long long)(kLinPartBytes / plane));
+    p.S = (int)std::max(1LL, S);
+  }
+  return p;
+}
+
+size_t product_ws(int rows, int cols, int red, bool bf16) {
+  if (!bf16 || rows == 0) return 0;
+  const LinPlan p = linear_plan(rows, cols, red);
+  return p.S > 1 ? (size_t)p.S * (size_t)rows * (size_t)cols * 4 : 0;
+}
+
+template <bool TA, bool TB>
+hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
+  if (!bf16) {
+    const long long tiles = ((a.rows - 1LL) / 64 + 1) * ((a.cols - 1LL) / 64 + 1);
+    linear_f32_kernel<TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const LinPlan p = linear_plan(a.rows, a.cols, a.red);
+  a.S = p.S;
+  a.part = static_cast<float*>(ws);
+  const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
+  if (p.tile == 128)
+    linear_tile_kernel<128, 128, 2, 4, 4, TA, TB><<<(unsigned)tiles, 512, 0, s>>>(a);
+  else
+    linear_tile_kernel<64, 64, 2, 2, 4, TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.S == 1) return e;
+  const size_t n8 = (size_t)a.rows * (size_t)(a.cols / 8);
+  linear_join_kernel<<<(unsigned)std::min<size_t>((n8 + 255) / 256, 8 * (size_t)device_cu_count()), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// Row ranges of the bias' sums: enough blocks for the chip, at least 32 rows each.
+int bias_ranges(int rows, int cols) {
+  const int cb = (cols - 1) / 256 + 1;
+  return std::max(1, std::min((4 * device_cu_count() + cb - 1) / cb, (rows + 31) / 32));
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// Never 0: a call without a workspace asks for its size.
+constexpr size_t kLinearWsLeast = 256;
+
+size_t linear_ws_bytes(int M, int N, int K, bool bf16) { return std::max(kLinearWsLeast, product_ws(M, N, K, bf16)); }
+
+hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
+  LinArgs a{};
+  a.A = c.x, a.B = c.w, a.lda = c.K, a.ldb = c.ldw;
+  a.rows = c.M, a.cols = c.N, a.red = c.K;
+  a.bias = c.bias, a.mul = c.mul, a.res = c.residual, a.z = c.z, a.out = c.y, a.act = c.act;
+  return launch_product<false, false>(a, c.bf16, ws, s);
+}
+
+size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16) {
+  if (M == 0) return kLinearWsLeast;
+  return align256((size_t)bias_ranges(M, N) * (size_t)N * 4) +
+         std::max(product_ws(M, K, N, bf16), product_ws(N, K, M, bf16));
+}
+
+hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (c.M == 0) {
+    auto zero = [&](void* p, size_t words) {
+      if (p == nullptr || e != hipSuccess) return;
+      fill_zero_kernel<<<(unsigned)std::min<size_t>((words + 255) / 256, 2048), 256, 0, s>>>(static_cast<uint32_t*>(p),
+                                                                                             words);
+      e = hipGetLastError();
+    };
+    zero(c.dw, (size_t)c.N * c.K / (c.dw_bf16 ? 2 : 1));
+    zero(c.dbias, c.N);
+    return e;
+  }
+  const bool own = c.act != kActNone || c.mul != nullptr;  // dz is not dy
+  const int P = bias_ranges(c.M, c.N);
+  if (own || c.dbias != nullptr) {
+    ActBackwardArgs b{};
+    b.dy = c.dy, b.mul = c.mul, b.dmul = c.dmul, b.act = c.act;
+    b.z = c.act != kActNone || c.dmul != nullptr ? c.z : nullptr;
+    b.dz = own ? c.dz : nullptr;
+    b.rows = c.M, b.cols = c.N, b.P = P;
+    b.db = c.dbias == nullptr ? nullptr : P > 1 ? static_cast<float*>(ws) : c.dbias;
+    const unsigned grid = (unsigned)(((c.N - 1) / 256 + 1) * P);
+    if (c.bf16)
+      act_backward_kernel<true><<<grid, 256, 0, s>>>(b);
+    else
+      act_backward_kernel<false><<<grid, 256, 0, s>>>(b);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (c.dbias != nullptr && P > 1) {
+      bias_join_kernel<<<(unsigned)((c.N + 255) / 256), 256, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  const void* dz = own ? c.dz : c.dy;
+  void* part = static_cast<char*>(ws) + align256((size_t)P * (size_t)c.N * 4);
+  if (c.dx != nullptr) {
+    LinArgs a{};
+    a.A = dz, a.B = c.w, a.lda = c.N, a.ldb = c.ldw;
+    a.rows = c.M, a.cols = c.K, a.red = c.N, a.out = c.dx;
+    if ((e = launch_product<false, true>(a, c.bf16, part, s)) != hipSuccess) return e;
+  }
+  if (c.dw != nullptr) {
+    LinArgs a{};
+    a.A = dz, a.B = c.x, a.lda = c.N, a.ldb = c.K;
+    a.rows = c.N, a.cols = c.K, a.red = c.M;
+    if (c.dw_bf16)
+      a.out = c.dw;
+    else
+      a.out32 = static_cast<float*>(c.dw);
+    if ((e = launch_product<true, true>(a, c.bf16, part, s)) != hipSuccess) return e;
+  }
+  return e;
+}
+
+}  // namespace moe

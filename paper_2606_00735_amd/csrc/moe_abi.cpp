@@ -694,6 +694,126 @@ moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_ro
                                             stream));
 }
 
+// ---------------------------------------------------------------------------
+// Around the routed experts
+// ---------------------------------------------------------------------------
+static_assert((int)MOE_ACT_NONE == moe::kActNone && (int)MOE_ACT_RELU == moe::kActRelu &&
+                  (int)MOE_ACT_SILU == moe::kActSilu && (int)MOE_ACT_GELU == moe::kActGelu,
+              "activation codes");
+
+moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask, int T, int E, int k,
+                     moe_score score, int n_group, int topk_group, int norm, double scale, int32_t* ids, float* w,
+                     hipStream_t stream) {
+  const moe_status st = check_tk(T, k, E);
+  if (st != MOE_OK) return st;
+  if (score != MOE_SIGMOID && score != MOE_SOFTMAX) return MOE_ERR_INVALID_ARG;
+  if (n_group < 1 || n_group > E || E % n_group != 0 || topk_group < 1 || topk_group > n_group ||
+      k > topk_group * (E / n_group) || !std::isfinite(scale))
+    return MOE_ERR_INVALID_ARG;
+  if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  if (!logits || !ids || !w || !aligned16(logits) || !aligned4(bias) || !aligned4(ids) || !aligned4(w))
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_route(logits, bias, mask, T, E, k, score == MOE_SOFTMAX, n_group, topk_group, norm != 0,
+                                      scale, ids, w, stream));
+}
+
+moe_status moe_route_backward(const float* logits, const int32_t* ids, const float* dw, int T, int E, int k,
+                              moe_score score, int norm, double scale, int accumulate, float* dlogits,
+                              hipStream_t stream) {
+  const moe_status st = check_tk(T, k, E);
+  if (st != MOE_OK) return st;
+  if ((score != MOE_SIGMOID && score != MOE_SOFTMAX) || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
+  if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  if (!logits || !ids || !dw || !dlogits || !aligned16(logits) || !aligned16(dlogits) || !aligned4(ids) ||
+      !aligned4(dw) || dlogits == logits)
+    return MOE_ERR_INVALID_ARG;
+  return hip_status(moe::launch_route_backward(logits, ids, dw, T, E, k, score == MOE_SOFTMAX, norm != 0, (float)scale,
+                                               accumulate != 0, dlogits, stream));
+}
+
+// Sizes of a dense product; *ld: the row stride of w.
+static moe_status linear_shape_ok(int M, int N, int K, int ldw, moe_act act, moe_dtype dt, int* ld) {
+  if (!valid_dtype(dt) || M < 0 || N < 8 || K < 8 || N % 8 != 0 || K % 8 != 0) return MOE_ERR_INVALID_ARG;
+  if (act != MOE_ACT_NONE && act != MOE_ACT_RELU && act != MOE_ACT_SILU && act != MOE_ACT_GELU)
+    return MOE_ERR_INVALID_ARG;
+  // the limits keep row indices of a tile in 31 bits and a launch's threads below 2^32
+  const long long most = 1LL << (dt == MOE_BF16 ? 36 : 34);
+  if (N > (1 << 20) || K > (1 << 20) || M > (1 << 28) || (long long)M * N > most || (long long)M * K > most ||
+      (long long)N * K > most)
+    return MOE_ERR_UNSUPPORTED;
+  return resolve_ld(ldw, K, dt, ld);
+}
+
+moe_status moe_linear(const void* x, const void* w, const float* bias, const void* mul, const void* residual, int M,
+                      int N, int K, int ldw, moe_act act, moe_dtype dt, void* y, void* z, void* ws, size_t* ws_bytes,
+                      hipStream_t stream) {
+  int ld = 0;
+  const moe_status st = linear_shape_ok(M, N, K, ldw, act, dt, &ld);
+  if (st != MOE_OK) return st;
+  if (ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
+  const size_t need = moe::linear_ws_bytes(M, N, K, dt == MOE_BF16);
+  if (ws == nullptr) {
+    *ws_bytes = need;
+    return MOE_OK;
+  }
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (M == 0) return MOE_OK;
+  if (!x || !w || !y || y == x || y == w || (z && (z == y || z == x || z == w || z == mul || z == residual)))
+    return MOE_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(mul) || !aligned16(residual) || !aligned16(y) ||
+      !aligned16(z) || !aligned16(ws))
+    return MOE_ERR_INVALID_ARG;
+  moe::LinearCall c{x, w, bias, mul, residual, M, N, K, ld, (int)act, dt == MOE_BF16, y, z};
+  return hip_status(moe::launch_linear(c, ws, stream));
+}
+
+moe_status moe_linear_backward(const void* dy, const void* x, const void* w, const void* z, const void* mul, int M,
+                               int N, int K, int ldw, moe_act act, moe_dtype dt, void* dz, void* dmul, void* dx,
+                               void* dw, moe_dtype dw_dt, float* dbias, void* ws, size_t* ws_bytes,
+                               hipStream_t stream) {
+  int ld = 0;
+  const moe_status st = linear_shape_ok(M, N, K, ldw, act, dt, &ld);
+  if (st != MOE_OK) return st;
+  if (ws_bytes == nullptr || !valid_dtype(dw_dt) || (dt == MOE_F32 && dw_dt != MOE_F32)) return MOE_ERR_INVALID_ARG;
+  const size_t need = moe::linear_backward_ws_bytes(M, N, K, dt == MOE_BF16);
+  if (ws == nullptr) {
+    *ws_bytes = need;
+    return MOE_OK;
+  }
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(z) || !aligned16(mul) || !aligned16(dz) ||
+      !aligned16(dmul) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias) || !aligned16(ws))
+    return MOE_ERR_INVALID_ARG;
+  if (M > 0) {
+    const bool own = act != MOE_ACT_NONE || mul != nullptr;
+    if (!dy || (dx && !w) || (dw && !x) || (own && !dz) || (dmul && !mul) ||
+        ((act != MOE_ACT_NONE || dmul) && !z))
+      return MOE_ERR_INVALID_ARG;
+    if ((dmul && (dmul == dz || dmul == dy || dmul == mul || dmul == z)) || (own && (dz == z || dz == mul)))
+      return MOE_ERR_INVALID_ARG;
+    for (const void* in : {dy, x, w, (const void*)(own ? dz : nullptr)})
+      if (in && (dx == in || dw == in)) return MOE_ERR_INVALID_ARG;
+  }
+  moe::LinearBackwardCall c{dy, x, w, z, mul, M, N, K, ld, (int)act, dt == MOE_BF16, dw_dt == MOE_BF16, dz, dmul, dx,
+                            dw, dbias};
+  return hip_status(moe::launch_linear_backward(c, ws, stream));
+}
+
+moe_status moe_dropout_add(const void* x, const void* residual, long long n, double p, const uint64_t* rng,
+                           moe_dtype dt, void* out, hipStream_t stream) {
+  if (n < 0 || !valid_dtype(dt) || !(p >= 0.0 && p < 1.0)) return MOE_ERR_INVALID_ARG;
+  if (n > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
+  if (n == 0) return MOE_OK;
+  if (!x || !rng || !out || !aligned16(x) || !aligned16(residual) || !aligned16(out) ||
+      (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
+    return MOE_ERR_INVALID_ARG;
+  // p < 1, so the threshold is below 2^32
+  return hip_status(moe::launch_dropout(x, residual, rng, n, (uint32_t)std::floor(p * 4294967296.0),
+                                        (float)(1.0 / (1.0 - p)), dt == MOE_BF16, out, stream));
+}
+
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
