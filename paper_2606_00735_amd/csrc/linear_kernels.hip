@@ -322,6 +322,248 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
                       at.split, lane);
 }
 
+// ---------------------------------------------------------------------------
+// The 256 x 256 tile: 4 waves (2 x 2), each 128 x 128 as four quadrants (A half, B half)
+// of 64 x 64, in phases as the grouped GEMMs' 256-row tile (big_tile): a chunk is four
+// 16 KB slots (A0, A1, B0, B1: the halves that every wave's quadrants read), two chunks
+// deep; a phase runs one quadrant's 16 MFMAs from registers, reads the fragments of the
+// slot that the next phase needs and refills the slot read in the phase before, for the
+// chunk after next:
+//
+//   even chunk  A0 B0 | A0 B1 | A1 B1 | A1 B0     odd chunk  A0 B1 | A0 B0 | A1 B0 | A1 B1
+//   reads       B1      A1      A0'     B1'                  B0      A1      A0'     B0'
+//
+// Either operand may be transposed; its slot is then 64 rows of the reduction by 128 rows
+// of C, its fragments two transposing reads each.
+// ---------------------------------------------------------------------------
+constexpr int kSlotBytes = 128 * kChunk * 2;
+
+template <bool TR>
+struct BigOperand {
+  static constexpr int RB = TR ? 256 : 128, PP = RB / 16, RPI = 1024 / RB;
+  const char* base;
+  size_t step;
+  uint32_t off[2][4];  // of load t of half h
+  uint32_t fof[TR ? 2 : 4];
+
+  // slot row (TR: column) q of half h is the tile's row 128 (q / 64) + 64 h + q % 64
+  __device__ __forceinline__ void init(const void* p, int ld, int first, int left, int wsel, int wave, int lane) {
+    base = static_cast<const char*>(p) + (TR ? (size_t)first * 2 : (size_t)first * (size_t)ld * 2);
+    step = TR ? (size_t)ld * (kChunk * 2) : (size_t)(kChunk * 2);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int r = (t * 4 + wave) * RPI + lane / PP;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (TR) {
+          const int piece = tr_piece<128>(r, lane % PP);
+          off[h][t] = (uint32_t)r * (uint32_t)(ld * 2) +
+                      (uint32_t)(min((piece >> 3) * 128 + h * 64 + (piece & 7) * 8, left - 8) * 2);
+        } else {
+          off[h][t] = (uint32_t)min((r >> 6) * 128 + h * 64 + (r & 63), left - 1) * (uint32_t)(ld * 2) +
+                      (uint32_t)(swz_chunk<kChunk>(r, lane % PP) * 16);
+        }
+      }
+    }
+    const int hi = lane >> 5, r32 = lane & 31;
+    if (TR) {
+      const int row = 8 * hi + ((lane & 15) >> 2);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int colb = (wsel * 64 + i * 32) * 2 + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+        fof[i] = (uint32_t)(row * RB + tr_piece<128>(row, colb >> 4) * 16 + (colb & 15));
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        fof[q] = (uint32_t)((wsel * 64 + r32) * RB + swz_chunk<kChunk>(r32, 2 * q + hi) * 16);
+    }
+  }
+  // fragment of block i (32 rows of the wave's 64) at k-step q of the slot at byte `slot`
+  __device__ __forceinline__ bf16x8_t frag(uint32_t lds, int slot, int i, int q) const {
+    if constexpr (TR) {
+      typedef __attribute__((address_space(3))) s16x4_t* lds4;
+      const uint32_t at = lds + fof[i] + (uint32_t)(slot + q * 16 * RB);
+      const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at));
+      const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at + 4 * RB));
+      struct {
+        s16x4_t lo, hi;
+      } v = {a, b};
+      return __builtin_bit_cast(bf16x8_t, v);
+    } else {
+      typedef __attribute__((address_space(3))) u32x4_t* lds16;
+      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<lds16>(lds + fof[q] + (uint32_t)(slot + i * 32 * RB)));
+    }
+  }
+  // the partial chunk kc (n of 64) into the slots at `slot` of half h, zeros past its end
+  __device__ __forceinline__ void load_tail(int kc, int n, char* lds, int h, int wave, int lane) const {
+    const char* p = base + (size_t)kc * step;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int r = (t * 4 + wave) * RPI + lane / PP;
+      const bool in = TR ? r < n : swz_chunk<kChunk>(r, lane % PP) * 8 < n;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (in) v = *reinterpret_cast<const uint4*>(p + off[h][t]);
+      *reinterpret_cast<uint4*>(lds + (t * 4 + wave) * 1024 + lane * 16) = v;
+    }
+  }
+};
+
+template <bool TA, bool TB>
+__global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
+  __shared__ __align__(16) bf16_t smem[8 * kSlotBytes / 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int mts = (a.rows - 1) / 256 + 1, nts = (a.cols - 1) / 256 + 1;
+  const TileAt at = tile_at(blockIdx.x, gridDim.x, mts, nts);
+  const int row0 = uniform_int(at.mt * 256), col0 = uniform_int(at.nt * 256);
+  const int chunks = a.red / kChunk;
+  const int kc0 = uniform_int((int)((long long)at.split * chunks / a.S));
+  const int nK = uniform_int((int)((long long)(at.split + 1) * chunks / a.S)) - kc0;
+  BigOperand<TA> A;
+  BigOperand<TB> B;
+  A.init(a.A, a.lda, row0, a.rows - row0, wm, wave, lane);
+  B.init(a.B, a.ldb, col0, a.cols - col0, wn, wave, lane);
+  const uint32_t lds = lds_addr(smem), lds0 = lds + wave * 1024;
+  bf16x8_t fr[4][2][4];  // [slot: A0, A1, B0, B1][block][k-step]
+  f32x16_t acc[2][2][2][2];  // [A half][B half][row block][column block]
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[h][b][i][j] = f32x16_t{};
+  // load t of slot w of chunk kc; past the last chunk a placeholder load of one line
+  auto issue = [&](int w, int kc, int t) __attribute__((always_inline)) {
+    const int msk = (kc - nK) >> 31;
+    const size_t kcl = (size_t)(kc0 + (kc & msk));
+    const void* p = uniform_ptr(w < 2 ? A.base + kcl * A.step : B.base + kcl * B.step);
+    dma16o(p, (w < 2 ? A.off[w & 1][t] : B.off[w & 1][t]) & (uint32_t)msk, lds0, ((kc & 1) * 4 + w) * kSlotBytes + t * 4096);
+  };
+  auto issue_slot = [&](int w, int kc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) issue(w, kc, t);
+  };
+  auto readf = [&](int w, int kc, int i, int q) __attribute__((always_inline)) {
+    const int slot = ((kc & 1) * 4 + w) * kSlotBytes;
+    fr[w][i][q] = w < 2 ? A.frag(lds, slot, i, q) : B.frag(lds, slot, i, q);
+  };
+  auto mma = [&](int ha, int hb, int i, int j, int q) __attribute__((always_inline)) {
+    acc[ha][hb][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[2 + hb][j][q], fr[ha][i][q], acc[ha][hb][i][j], 0, 0, 0);
+  };
+  // One phase: the MFMAs of quadrant (ha, hb); reads slot rw of chunk rc, refills slot iw
+  // with chunk ic (its last read was the phase before).
+  auto phase = [&](int ha, int hb, int rw, int rc, int iw, int ic) __attribute__((always_inline)) {
+    wait_lgkmcnt0();      // the fragments read in the last phase are here
+    wait_vmcnt<6 * 4>();  // this wave's loads of slot rw landed
+    lds_barrier();        // everyone's; and everyone has read slot iw
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      mma(ha, hb, 0, 0, t);
+      mma(ha, hb, 0, 1, t);
+      issue(iw, ic, t);
+      if (t < 2) {
+        readf(rw, rc, 0, 2 * t);
+        readf(rw, rc, 1, 2 * t);
+      }
+      mma(ha, hb, 1, 0, t);
+      mma(ha, hb, 1, 1, t);
+      if (t < 2) {
+        readf(rw, rc, 0, 2 * t + 1);
+        readf(rw, rc, 1, 2 * t + 1);
+        // an MFMA, a fragment, ...
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (rw < 2 ? TA : TB)
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          else
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (nK > 0) {
+    // slots in the order they are read, nine of them
+    issue_slot(0, 0);
+    issue_slot(2, 0);
+    issue_slot(3, 0);
+    issue_slot(1, 0);
+    issue_slot(0, 1);
+    issue_slot(3, 1);
+    issue_slot(2, 1);
+    issue_slot(1, 1);
+    wait_vmcnt<6 * 4>();  // A0, B0 of chunk 0
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        readf(0, 0, i, q);
+        readf(2, 0, i, q);
+      }
+    wait_lgkmcnt0();
+    lds_barrier();  // every wave has read A0 of chunk 0
+    issue_slot(0, 2);
+    auto even = [&](int c) __attribute__((always_inline)) {
+      phase(0, 0, 3, c, 2, c + 2);
+      phase(0, 1, 1, c, 3, c + 2);
+      phase(1, 1, 0, c + 1, 1, c + 2);
+      phase(1, 0, 3, c + 1, 0, c + 3);
+    };
+    int c = 0;
+    for (; c + 1 < nK; c += 2) {
+      even(c);
+      phase(0, 1, 2, c + 1, 3, c + 3);
+      phase(0, 0, 1, c + 1, 2, c + 3);
+      phase(1, 0, 0, c + 2, 1, c + 3);
+      phase(1, 1, 2, c + 2, 0, c + 4);
+    }
+    if (c < nK) even(c);
+    wait_lgkmcnt0();
+    wait_vmcnt<0>();
+    lds_barrier();  // no load is in flight and every wave is done with the slots
+  }
+  const int n = a.red - chunks * kChunk;
+  if (n > 0 && at.split == a.S - 1) {
+    char* p = reinterpret_cast<char*>(smem);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      A.load_tail(chunks, n, p + h * kSlotBytes, h, wave, lane);
+      B.load_tail(chunks, n, p + (2 + h) * kSlotBytes, h, wave, lane);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q * 16 < n) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) readf(w, 0, i, q);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) mma(h, b, i, j, q);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      finish_tile<2, 2>(a, acc[h][b], reinterpret_cast<char*>(smem) + wave * 8192, row0 + wm * 128 + h * 64,
+                        col0 + wn * 128 + b * 64, at.split, lane);
+}
+
 // Joins the S partial sums of every output, in their order.
 __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
   const size_t n8 = (size_t)a.rows * (size_t)(a.cols / 8), plane = (size_t)a.rows * (size_t)a.cols;
@@ -481,7 +723,8 @@ constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 LinPlan linear_plan(int rows, int cols, int red) {
   const long long cus = device_cu_count();
   auto tiles = [&](int t) { return ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1); };
-  LinPlan p{tiles(128) >= cus ? 128 : 64, 1};
+  LinPlan p{tiles(256) >= cus * 3 / 4 ? 256 : tiles(128) >= cus ? 128 : 64, 1};
+  if (p.tile == 256) return p;
   const long long n = tiles(p.tile);
   const int chunks = red / kChunk;
   if (n < cus && chunks >= 8) {
@@ -510,7 +753,9 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   a.S = p.S;
   a.part = static_cast<float*>(ws);
   const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
-  if (p.tile == 128)
+  if (p.tile == 256)
+    linear_big_kernel<TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+  else if (p.tile == 128)
     linear_tile_kernel<128, 128, 2, 4, 4, TA, TB><<<(unsigned)tiles, 512, 0, s>>>(a);
   else
     linear_tile_kernel<64, 64, 2, 2, 4, TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);

@@ -100,6 +100,23 @@ def test_integer_gradients_are_exact(M, N, K, dtype):
     assert torch.equal(dx, (want @ w.double()).to(dtype)) and torch.equal(dw, (want.t() @ x.double()).to(dtype))
 
 
+# large and ragged in two dimensions, the third one of few chunks: none, one, two, three, with
+# and without a partial one
+LARGE = [(3601, 3592, n) for n in (40, 64, 72, 128, 200, 320)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE + [(M, K, N) for M, N, K in LARGE] + [(K + d, N, M + 7) for d, (M, N, K) in enumerate(LARGE)])
+def test_large_integer_products_are_exact(M, N, K):
+    banner("linear large ints", M, N, K)
+    g = gen(M + N + K)
+    x, w, dy, r = ints(g, M, K), ints(g, N, K), ints(g, M, N), ints(g, M, N)
+    y = moe.moe_linear(x, w, residual=r)
+    assert torch.equal(y, (x.double() @ w.double().t() + r.double()).to(BF))
+    dx, dw, db, _, _ = moe.moe_linear_backward(dy, x, w)
+    assert torch.equal(dx, (dy.double() @ w.double()).to(BF))
+    assert torch.equal(dw, (dy.double().t() @ x.double()).float()) and torch.equal(db, dy.double().sum(0).float())
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
 @pytest.mark.parametrize("dtype", [BF, torch.float32])
 @pytest.mark.parametrize("M,N,K", [(1, 256, 2048), (65, 264, 1000), (300, 136, 520)])
