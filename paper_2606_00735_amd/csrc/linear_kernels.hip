@@ -27,8 +27,25 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float sigmoid32(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * 1.4426950408889634f));
 }
-// the normal distribution's integral: by erfc, whose small values keep their digits
-__device__ __forceinline__ float normal_below(float z) { return 0.5f * erfcf(-0.70710678f * z); }
+// exp(-z^2 / 2)
+__device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(z * z * -0.7213475204f); }
+// The normal distribution's integral up to z. Its small side is exp(-z^2 / 2) R(|z|), R
+// smooth: a polynomial of degree 8 in t = 1 / (1 + 0.3 |z|), fitted for the least largest
+// relative error over [0, 14], 1.5e-7, 4.8e-7 in fp32 (a call of erfcf cost an epilogue of
+// 16384 x 2048 values 50 us).
+__device__ __forceinline__ float normal_below(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.0f));
+  float p = 0.03567765653133392f;
+  p = fmaf(p, t, -0.15721559524536133f);
+  p = fmaf(p, t, 0.20637577772140503f);
+  p = fmaf(p, t, -0.05370469018816948f);
+  p = fmaf(p, t, 0.1285729855298996f);
+  p = fmaf(p, t, 0.09990999847650528f);
+  p = fmaf(p, t, 0.12075452506542206f);
+  p = fmaf(p, t, 0.11962926387786865f);
+  const float q = p * t * bell(z);
+  return z >= 0.0f ? 1.0f - q : q;
+}
 
 __device__ __forceinline__ float act_value(float z, int act) {
   switch (act) {
@@ -45,7 +62,7 @@ __device__ __forceinline__ float act_slope(float z, int act) {
       const float q = sigmoid32(z);
       return q * (1.0f + z * (1.0f - q));
     }
-    case kActGelu: return normal_below(z) + z * 0.3989422804f * __builtin_amdgcn_exp2f(z * z * -0.7213475204f);
+    case kActGelu: return fmaf(z * 0.3989422804f, bell(z), normal_below(z));
     default: return 1.0f;
   }
 }
@@ -83,10 +100,19 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
                     pack_bf16x2(f[6], f[7]));
 }
 
-// Eight consecutive columns of a row, from their sums to memory. mul and res may be out:
-// they are read before it is written.
-__device__ __forceinline__ void finish8(const LinArgs& a, size_t row, int col, float (&v)[8]) {
-  const size_t at = row * (size_t)a.cols + (size_t)col;
+// mul's and res' values of eight consecutive columns of a row.
+struct Beside {
+  uint4 mul, res;
+};
+__device__ __forceinline__ Beside load_beside(const LinArgs& a, size_t at) {
+  Beside b{};
+  if (a.mul != nullptr) b.mul = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.mul) + at);
+  if (a.res != nullptr) b.res = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.res) + at);
+  return b;
+}
+
+// Eight consecutive columns of a row, from their sums to memory.
+__device__ __forceinline__ void finish8(const LinArgs& a, size_t at, int col, float (&v)[8], const Beside& o) {
   if (a.out32 != nullptr) {
     *reinterpret_cast<float4*>(a.out32 + at) = make_float4(v[0], v[1], v[2], v[3]);
     *reinterpret_cast<float4*>(a.out32 + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -105,12 +131,12 @@ __device__ __forceinline__ void finish8(const LinArgs& a, size_t row, int col, f
   }
   float f[8];
   if (a.mul != nullptr) {
-    unpack8(*reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.mul) + at), f);
+    unpack8(o.mul, f);
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] *= f[q];
   }
   if (a.res != nullptr) {
-    unpack8(*reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.res) + at), f);
+    unpack8(o.res, f);
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] += f[q];
   }
@@ -193,45 +219,55 @@ struct Panel {
   }
 };
 
-// A wave's MI x NI blocks of 32 x 32 sums, whose lanes hold 4 consecutive columns of a
-// row per register group, through its own piece of LDS to whole rows of 8 columns a
-// lane. Rows and columns past C's are not stored.
-template <int MI, int NI>
-__device__ __forceinline__ void finish_tile(const LinArgs& a, const f32x16_t (&acc)[MI][NI], char* lds, int row0,
-                                            int col0, int split, int lane) {
-  constexpr int RB = NI * 128, PP = RB / 16;
+// N stripes of a wave's sums, 32 rows x 32 NI columns each, whose lanes hold groups of 4
+// consecutive columns of a row, through the wave's own piece of LDS to whole rows of 8
+// columns a lane. sums(n, put) puts stripe n's groups: put(row, group of columns, values);
+// the stripe's first row and column are r0(n) and c0(n). mul and res are loaded a stripe ahead: each element is read by
+// the lane that writes it, so out may be one of them. Rows and columns past C's are not
+// stored.
+template <int N, int NI, class Sums, class Row, class Col>
+__device__ __forceinline__ void finish_stripes(const LinArgs& a, char* lds, int split, int lane, Sums&& sums, Row&& r0,
+                                               Col&& c0) {
+  constexpr int RB = NI * 128, PP = RB / 16, IT = PP / 4;
   static_assert(PP == 8 || PP == 16, "row pieces");
   auto key = [](int r) { return PP == 16 ? (r & 15) : ((r >> 1) & 7); };
-  const int r32 = lane & 31, hi = lane >> 5;
+  asm volatile("" : "+v"(lane));  // what depends on it is computed here, not kept through the K loop
+  const int lr = lane / (PP / 2), lc = lane % (PP / 2) * 8;
+  const bool beside = a.S == 1 && (a.mul != nullptr || a.res != nullptr);
+  Beside o[2][IT] = {};
+  auto row_of = [&](int n, int it) { return r0(n) + it * (128 / PP) + lr; };
+  auto in = [&](int n, int it) { return row_of(n, it) < a.rows && c0(n) + lc < a.cols; };
+  auto prefetch = [&](int n) {
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    if (row0 + i * 32 < a.rows) {
+    for (int it = 0; it < IT; ++it)
+      if (in(n, it)) o[n & 1][it] = load_beside(a, (size_t)row_of(n, it) * (size_t)a.cols + (size_t)(c0(n) + lc));
+  };
+  if (beside) prefetch(0);
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+  for (int n = 0; n < N; ++n) {
+    if (beside && n + 1 < N) prefetch(n + 1);
+    sums(n, [&](int r, int p, f32x4_t v) __attribute__((always_inline)) {
+      *reinterpret_cast<f32x4_t*>(lds + r * RB + ((p ^ key(r)) * 16)) = v;
+    });
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<float4*>(lds + r32 * RB + (((j * 8 + 2 * g + hi) ^ key(r32)) * 16)) =
-              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int it = 0; it < PP / 4; ++it) {
-        const int r = (it * 64 + lane) / (PP / 2), p = (it * 64 + lane) % (PP / 2);
-        const float4 u = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p) ^ key(r)) * 16));
-        const float4 w = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p + 1) ^ key(r)) * 16));
-        const int row = row0 + i * 32 + r, col = col0 + p * 8;
-        if (row < a.rows && col < a.cols) {
-          float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-          if (a.S > 1) {
-            float* q = a.part + ((size_t)split * a.rows + row) * (size_t)a.cols + col;
-            *reinterpret_cast<float4*>(q) = u;
-            *reinterpret_cast<float4*>(q + 4) = w;
-          } else {
-            finish8(a, (size_t)row, col, v);
-          }
+    for (int it = 0; it < IT; ++it) {
+      const int r = it * (128 / PP) + lr, p = lane % (PP / 2);
+      const float4 u = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p) ^ key(r)) * 16));
+      const float4 w = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p + 1) ^ key(r)) * 16));
+      if (in(n, it)) {
+        const size_t at = (size_t)row_of(n, it) * (size_t)a.cols + (size_t)(c0(n) + lc);
+        float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+        if (a.S > 1) {
+          float* q = a.part + (size_t)split * (size_t)a.rows * (size_t)a.cols + at;
+          *reinterpret_cast<float4*>(q) = u;
+          *reinterpret_cast<float4*>(q + 4) = w;
+        } else {
+          finish8(a, at, c0(n) + lc, v, o[n & 1][it]);
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -318,8 +354,18 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
     }
     __syncthreads();
   }
-  finish_tile<MI, NI>(a, acc, reinterpret_cast<char*>(smem) + wave * (32 * WN * 4), row0 + wm * WM, col0 + wn * WN,
-                      at.split, lane);
+  finish_stripes<MI, NI>(
+      a, reinterpret_cast<char*>(smem) + wave * (32 * WN * 4), at.split, lane,
+      [&](int n, auto&& put) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            put(lane & 31, j * 8 + 2 * g + (lane >> 5),
+                f32x4_t{acc[n][j][4 * g], acc[n][j][4 * g + 1], acc[n][j][4 * g + 2], acc[n][j][4 * g + 3]});
+      },
+      [&](int n) { return row0 + wm * WM + n * 32; },
+      [&](int) { return col0 + wn * WN; });
 }
 
 // ---------------------------------------------------------------------------
@@ -342,14 +388,16 @@ template <bool TR>
 struct BigOperand {
   static constexpr int RB = TR ? 256 : 128, PP = RB / 16, RPI = 1024 / RB;
   const char* base;
-  size_t step;
+  uint64_t step;       // bytes between chunks
   uint32_t off[2][4];  // of load t of half h
-  uint32_t fof[TR ? 2 : 4];
+  uint64_t next;       // address of the chunk that is loaded next,
+  uint32_t records;    // 0 past the last one
+  uint32_t fof[TR ? 4 : 2];
 
   // slot row (TR: column) q of half h is the tile's row 128 (q / 64) + 64 h + q % 64
   __device__ __forceinline__ void init(const void* p, int ld, int first, int left, int wsel, int wave, int lane) {
     base = static_cast<const char*>(p) + (TR ? (size_t)first * 2 : (size_t)first * (size_t)ld * 2);
-    step = TR ? (size_t)ld * (kChunk * 2) : (size_t)(kChunk * 2);
+    step = TR ? (uint64_t)ld * (kChunk * 2) : (uint64_t)(kChunk * 2);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int r = (t * 4 + wave) * RPI + lane / PP;
@@ -365,25 +413,49 @@ struct BigOperand {
         }
       }
     }
-    const int hi = lane >> 5, r32 = lane & 31;
+    // lane (r = lane % 16, g = lane / 16) holds k = 32 s + 8 g + (0..7) of row r
+    const int g = lane >> 4, r = lane & 15;
     if (TR) {
-      const int row = 8 * hi + ((lane & 15) >> 2);
+      const int row = 8 * g + (r >> 2);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int colb = (wsel * 64 + i * 32) * 2 + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+      for (int i = 0; i < 4; ++i) {
+        const int colb = (wsel * 64 + i * 16) * 2 + 8 * (lane & 3);
         fof[i] = (uint32_t)(row * RB + tr_piece<128>(row, colb >> 4) * 16 + (colb & 15));
       }
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        fof[q] = (uint32_t)((wsel * 64 + r32) * RB + swz_chunk<kChunk>(r32, 2 * q + hi) * 16);
+      for (int s = 0; s < 2; ++s)
+        fof[s] = (uint32_t)((wsel * 64 + r) * RB + swz_chunk<kChunk>(r, 4 * s + g) * 16);
     }
   }
-  // fragment of block i (32 rows of the wave's 64) at k-step q of the slot at byte `slot`
-  __device__ __forceinline__ bf16x8_t frag(uint32_t lds, int slot, int i, int q) const {
+  // Chunk kc is next; live: -1, or 0 past the last one. Offsets are in the operand by
+  // construction; without records a load brings zeros and reads nothing.
+  __device__ __forceinline__ void start(int kc, int live) {
+    next = reinterpret_cast<uint64_t>(uniform_ptr(base + (uint64_t)kc * step));
+    records = (uint32_t)live;
+  }
+  __device__ __forceinline__ void advance(int live) {
+    next += step;
+    records = (uint32_t)live;
+  }
+  // Load t of half h to LDS byte address lds + at. M0 needs one wait state; a descriptor
+  // that vector instructions have written (FIRST: as start leaves it) five, which the
+  // compiler, not seeing the load, would not keep.
+  template <bool FIRST = false>
+  __device__ __forceinline__ void load(int h, int t, uint32_t lds, int at) const {
+    const u32x4_t srd = {(uint32_t)next, (uint32_t)(next >> 32), records, 0x00020000u};
+    if (FIRST) asm volatile("s_nop 4" ::"s"(srd) : "memory");
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                 :
+                 : "v"(off[h][t]), "s"(srd), "s"(lds), "is"(at)
+                 : "memory", "scc");
+  }
+  // fragment of block i (16 rows of the wave's 64) at k-step s (32 of the chunk's 64) of
+  // the slot at byte `slot`
+  __device__ __forceinline__ bf16x8_t frag(uint32_t lds, int slot, int i, int s) const {
     if constexpr (TR) {
       typedef __attribute__((address_space(3))) s16x4_t* lds4;
-      const uint32_t at = lds + fof[i] + (uint32_t)(slot + q * 16 * RB);
+      const uint32_t at = lds + fof[i] + (uint32_t)(slot + s * 32 * RB);
       const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at));
       const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at + 4 * RB));
       struct {
@@ -392,7 +464,8 @@ struct BigOperand {
       return __builtin_bit_cast(bf16x8_t, v);
     } else {
       typedef __attribute__((address_space(3))) u32x4_t* lds16;
-      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<lds16>(lds + fof[q] + (uint32_t)(slot + i * 32 * RB)));
+      // rows 16 apart swizzle alike
+      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<lds16>(lds + fof[s] + (uint32_t)(slot + i * 16 * RB)));
     }
   }
   // the partial chunk kc (n of 64) into the slots at `slot` of half h, zeros past its end
@@ -425,103 +498,119 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   A.init(a.A, a.lda, row0, a.rows - row0, wm, wave, lane);
   B.init(a.B, a.ldb, col0, a.cols - col0, wn, wave, lane);
   const uint32_t lds = lds_addr(smem), lds0 = lds + wave * 1024;
-  bf16x8_t fr[4][2][4];  // [slot: A0, A1, B0, B1][block][k-step]
-  f32x16_t acc[2][2][2][2];  // [A half][B half][row block][column block]
+  bf16x8_t fr[4][4][2];  // [slot: A0, A1, B0, B1][block][k-step]
+  f32x4_t acc[2][2][4][4];  // [A half][B half][row block][column block]
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[h][b][i][j] = f32x16_t{};
-  // load t of slot w of chunk kc; past the last chunk a placeholder load of one line
-  auto issue = [&](int w, int kc, int t) __attribute__((always_inline)) {
-    const int msk = (kc - nK) >> 31;
-    const size_t kcl = (size_t)(kc0 + (kc & msk));
-    const void* p = uniform_ptr(w < 2 ? A.base + kcl * A.step : B.base + kcl * B.step);
-    dma16o(p, (w < 2 ? A.off[w & 1][t] : B.off[w & 1][t]) & (uint32_t)msk, lds0, ((kc & 1) * 4 + w) * kSlotBytes + t * 4096);
+        for (int j = 0; j < 4; ++j) acc[h][b][i][j] = f32x4_t{};
+  // load t of slot w of the chunk (of parity par) that its operand is at
+  auto issue = [&](int w, int par, int t) __attribute__((always_inline)) {
+    if (w < 2)
+      A.load(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
+    else
+      B.load(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
   };
-  auto issue_slot = [&](int w, int kc) __attribute__((always_inline)) {
+  auto issue_slot = [&](int w, int par) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) issue(w, kc, t);
+    for (int t = 0; t < 4; ++t) {
+      if (w < 2)
+        A.template load<true>(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
+      else
+        B.template load<true>(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
+    }
   };
-  auto readf = [&](int w, int kc, int i, int q) __attribute__((always_inline)) {
-    const int slot = ((kc & 1) * 4 + w) * kSlotBytes;
+  auto readf = [&](int w, int par, int i, int q) __attribute__((always_inline)) {
+    const int slot = (par * 4 + w) * kSlotBytes;
     fr[w][i][q] = w < 2 ? A.frag(lds, slot, i, q) : B.frag(lds, slot, i, q);
   };
+  // As inline assembly, in place in the accumulation registers: as a builtin the compiler
+  // gives result and addend of these small blocks different registers and moves them about.
+  // It does not see that this is an MFMA: its sums are read by other instructions only
+  // after the wait that follows the last one (settle).
   auto mma = [&](int ha, int hb, int i, int j, int q) __attribute__((always_inline)) {
-    acc[ha][hb][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[2 + hb][j][q], fr[ha][i][q], acc[ha][hb][i][j], 0, 0, 0);
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
+                 : "+a"(acc[ha][hb][i][j])
+                 : "v"(fr[2 + hb][j][q]), "v"(fr[ha][i][q]));
   };
-  // One phase: the MFMAs of quadrant (ha, hb); reads slot rw of chunk rc, refills slot iw
-  // with chunk ic (its last read was the phase before).
-  auto phase = [&](int ha, int hb, int rw, int rc, int iw, int ic) __attribute__((always_inline)) {
+  // One phase: the MFMAs of quadrant (ha, hb); reads slot rw (of parity rp), refills slot iw
+  // (of parity ip; its last read was the phase before). step(): what moves a descriptor on.
+  // In exactly this order: two MFMAs, a fragment or a load, two MFMAs, ...
+  auto phase = [&](int ha, int hb, int rw, int rp, int iw, int ip, auto&& step) __attribute__((always_inline)) {
     wait_lgkmcnt0();      // the fragments read in the last phase are here
     wait_vmcnt<6 * 4>();  // this wave's loads of slot rw landed
     lds_barrier();        // everyone's; and everyone has read slot iw
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int s = t >> 1, i = 2 * (t & 1) + (e >> 1), j = 2 * (e & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        mma(ha, hb, i, j, s);
+        mma(ha, hb, i, j + 1, s);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t < 2) readf(rw, rp, e, t);
+        if (e == 0 && t == 0) step();
+        if (e == 1) issue(iw, ip, t);
+      }
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      mma(ha, hb, 0, 0, t);
-      mma(ha, hb, 0, 1, t);
-      issue(iw, ic, t);
-      if (t < 2) {
-        readf(rw, rc, 0, 2 * t);
-        readf(rw, rc, 1, 2 * t);
-      }
-      mma(ha, hb, 1, 0, t);
-      mma(ha, hb, 1, 1, t);
-      if (t < 2) {
-        readf(rw, rc, 0, 2 * t + 1);
-        readf(rw, rc, 1, 2 * t + 1);
-        // an MFMA, a fragment, ...
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          if (rw < 2 ? TA : TB)
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-          else
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
   };
+  auto keep = [] {};
+  // -1 if there is a chunk c, else 0: in scalar registers, where a comparison would be
+  // widened in vector registers
+  auto live = [&](int c) __attribute__((always_inline)) {
+    int v;
+    asm("s_cmp_lt_i32 %1, %2\n\ts_cselect_b32 %0, -1, 0" : "=s"(v) : "s"(c), "s"(nK) : "scc");
+    return v;
+  };
+  // wait states between an MFMA and other readers of its result (at most 11 of 4 passes)
+  auto settle = [&]() __attribute__((always_inline)) { asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); };
   if (nK > 0) {
+    A.start(kc0, -1);
+    B.start(kc0, -1);
     // slots in the order they are read, nine of them
     issue_slot(0, 0);
     issue_slot(2, 0);
     issue_slot(3, 0);
     issue_slot(1, 0);
+    A.advance(live(1));
+    B.advance(live(1));
     issue_slot(0, 1);
     issue_slot(3, 1);
     issue_slot(2, 1);
     issue_slot(1, 1);
+    A.advance(live(2));
     wait_vmcnt<6 * 4>();  // A0, B0 of chunk 0
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < 2; ++q) {
         readf(0, 0, i, q);
         readf(2, 0, i, q);
       }
     wait_lgkmcnt0();
     lds_barrier();  // every wave has read A0 of chunk 0
-    issue_slot(0, 2);
+    issue_slot(0, 0);
+    // a chunk's four phases: its last one loads A0 of the chunk after the one that the
+    // others load
     auto even = [&](int c) __attribute__((always_inline)) {
-      phase(0, 0, 3, c, 2, c + 2);
-      phase(0, 1, 1, c, 3, c + 2);
-      phase(1, 1, 0, c + 1, 1, c + 2);
-      phase(1, 0, 3, c + 1, 0, c + 3);
+      phase(0, 0, 3, 0, 2, 0, [&]() __attribute__((always_inline)) { B.advance(live(c + 2)); });
+      phase(0, 1, 1, 0, 3, 0, keep);
+      phase(1, 1, 0, 1, 1, 0, keep);
+      phase(1, 0, 3, 1, 0, 1, [&]() __attribute__((always_inline)) { A.advance(live(c + 3)); });
     };
     int c = 0;
     for (; c + 1 < nK; c += 2) {
       even(c);
-      phase(0, 1, 2, c + 1, 3, c + 3);
-      phase(0, 0, 1, c + 1, 2, c + 3);
-      phase(1, 0, 0, c + 2, 1, c + 3);
-      phase(1, 1, 2, c + 2, 0, c + 4);
+      phase(0, 1, 2, 1, 3, 1, [&]() __attribute__((always_inline)) { B.advance(live(c + 3)); });
+      phase(0, 0, 1, 1, 2, 1, keep);
+      phase(1, 0, 0, 0, 1, 1, keep);
+      phase(1, 1, 2, 0, 0, 0, [&]() __attribute__((always_inline)) { A.advance(live(c + 4)); });
     }
     if (c < nK) even(c);
     wait_lgkmcnt0();
@@ -538,30 +627,36 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
     }
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (q * 16 < n) {
+    for (int q = 0; q < 2; ++q) {
+      if (q * 32 < n) {
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) readf(w, 0, i, q);
+          for (int i = 0; i < 4; ++i) readf(w, 0, i, q);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) mma(h, b, i, j, q);
+              for (int j = 0; j < 4; ++j) mma(h, b, i, j, q);
       }
     }
     __syncthreads();
   }
+  settle();
+  // stripe n: B half n / 4, A half n / 2 % 2, row blocks 2 (n % 2) and the next
+  finish_stripes<8, 2>(
+      a, reinterpret_cast<char*>(smem) + wave * 8192, at.split, lane,
+      [&](int n, auto&& put) __attribute__((always_inline)) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      finish_tile<2, 2>(a, acc[h][b], reinterpret_cast<char*>(smem) + wave * 8192, row0 + wm * 128 + h * 64,
-                        col0 + wn * 128 + b * 64, at.split, lane);
+          for (int j = 0; j < 4; ++j)
+            put(16 * i + (lane & 15), 4 * j + (lane >> 4), acc[(n >> 1) & 1][n >> 2][2 * (n & 1) + i][j]);
+      },
+      [&](int n) { return row0 + wm * 128 + (n & 3) * 32; }, [&](int n) { return col0 + wn * 128 + (n >> 2) * 64; });
 }
 
 // Joins the S partial sums of every output, in their order.
@@ -570,8 +665,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
     const float4 u = sum_splits(a.part + i * 8, plane, a.S), w = sum_splits(a.part + i * 8 + 4, plane, a.S);
     float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-    const size_t row = i / (size_t)(a.cols / 8);
-    finish8(a, row, (int)(i % (size_t)(a.cols / 8)) * 8, v);
+    finish8(a, i * 8, (int)(i % (size_t)(a.cols / 8)) * 8, v, load_beside(a, i * 8));
   }
 }
 
