@@ -47,23 +47,32 @@ __device__ __forceinline__ float normal_below(float z) {
   return z >= 0.0f ? 1.0f - q : q;
 }
 
-__device__ __forceinline__ float act_value(float z, int act) {
-  switch (act) {
-    case kActRelu: return z < 0.0f ? 0.0f : z;
-    case kActSilu: return z * sigmoid32(z);
-    case kActGelu: return z * normal_below(z);
-    default: return z;
-  }
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+  if (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
+  if (ACT == kActSilu) return z * sigmoid32(z);
+  if (ACT == kActGelu) return z * normal_below(z);
+  return z;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+  if (ACT == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+  if (ACT == kActSilu) {
+    const float q = sigmoid32(z);
+    return q * (1.0f + z * (1.0f - q));
+  }
+  if (ACT == kActGelu) return fmaf(z * 0.3989422804f, bell(z), normal_below(z));
+  return 1.0f;
+}
+// f(std::integral_constant<int, act>): kernels have the activation as a parameter, since a
+// choice at every value costs more than the value (20 us a 256 x 256 tile).
+template <class F>
+auto with_act(int act, F&& f) {
   switch (act) {
-    case kActRelu: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-    case kActSilu: {
-      const float q = sigmoid32(z);
-      return q * (1.0f + z * (1.0f - q));
-    }
-    case kActGelu: return fmaf(z * 0.3989422804f, bell(z), normal_below(z));
-    default: return 1.0f;
+    case kActRelu: return f(std::integral_constant<int, kActRelu>{});
+    case kActSilu: return f(std::integral_constant<int, kActSilu>{});
+    case kActGelu: return f(std::integral_constant<int, kActGelu>{});
+    default: return f(std::integral_constant<int, kActNone>{});
   }
 }
 
@@ -84,7 +93,6 @@ struct LinArgs {
   void* z;               // [rows, cols]: the sum with the bias, or null
   void* out;             // of the operands' type, or
   float* out32;          // fp32: the plain sum
-  int act;
 };
 
 __device__ __forceinline__ void unpack8(uint4 v, float (&f)[8]) {
@@ -112,23 +120,26 @@ __device__ __forceinline__ Beside load_beside(const LinArgs& a, size_t at) {
 }
 
 // Eight consecutive columns of a row, from their sums to memory.
-__device__ __forceinline__ void finish8(const LinArgs& a, size_t at, int col, float (&v)[8], const Beside& o) {
+struct Bias8 {
+  float4 lo, hi;
+};
+__device__ __forceinline__ Bias8 load_bias(const LinArgs& a, int col) {
+  return {*reinterpret_cast<const float4*>(a.bias + col), *reinterpret_cast<const float4*>(a.bias + col + 4)};
+}
+template <int ACT>
+__device__ __forceinline__ void finish8(const LinArgs& a, size_t at, float (&v)[8], const Beside& o, const Bias8& b) {
   if (a.out32 != nullptr) {
     *reinterpret_cast<float4*>(a.out32 + at) = make_float4(v[0], v[1], v[2], v[3]);
     *reinterpret_cast<float4*>(a.out32 + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
     return;
   }
   if (a.bias != nullptr) {
-    const float4 b0 = *reinterpret_cast<const float4*>(a.bias + col);
-    const float4 b1 = *reinterpret_cast<const float4*>(a.bias + col + 4);
-    v[0] += b0.x, v[1] += b0.y, v[2] += b0.z, v[3] += b0.w;
-    v[4] += b1.x, v[5] += b1.y, v[6] += b1.z, v[7] += b1.w;
+    v[0] += b.lo.x, v[1] += b.lo.y, v[2] += b.lo.z, v[3] += b.lo.w;
+    v[4] += b.hi.x, v[5] += b.hi.y, v[6] += b.hi.z, v[7] += b.hi.w;
   }
   if (a.z != nullptr) *reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.z) + at) = pack8(v);
-  if (a.act != kActNone) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = act_value(v[q], a.act);
-  }
+  for (int q = 0; q < 8; ++q) v[q] = act_value<ACT>(v[q]);
   float f[8];
   if (a.mul != nullptr) {
     unpack8(o.mul, f);
@@ -222,10 +233,11 @@ struct Panel {
 // N stripes of a wave's sums, 32 rows x 32 NI columns each, whose lanes hold groups of 4
 // consecutive columns of a row, through the wave's own piece of LDS to whole rows of 8
 // columns a lane. sums(n, put) puts stripe n's groups: put(row, group of columns, values);
-// the stripe's first row and column are r0(n) and c0(n). mul and res are loaded a stripe ahead: each element is read by
-// the lane that writes it, so out may be one of them. Rows and columns past C's are not
+// the stripe's first row and column are r0(n) and c0(n). mul and res are loaded four stripes ahead (one ahead, their latencies
+// took 20 us a 256 x 256 tile); each element is read by the lane that writes it, so out may
+// be one of them. Rows and columns past C's are not
 // stored.
-template <int N, int NI, class Sums, class Row, class Col>
+template <int ACT, int N, int NI, class Sums, class Row, class Col>
 __device__ __forceinline__ void finish_stripes(const LinArgs& a, char* lds, int split, int lane, Sums&& sums, Row&& r0,
                                                Col&& c0) {
   constexpr int RB = NI * 128, PP = RB / 16, IT = PP / 4;
@@ -233,40 +245,59 @@ __device__ __forceinline__ void finish_stripes(const LinArgs& a, char* lds, int 
   auto key = [](int r) { return PP == 16 ? (r & 15) : ((r >> 1) & 7); };
   asm volatile("" : "+v"(lane));  // what depends on it is computed here, not kept through the K loop
   const int lr = lane / (PP / 2), lc = lane % (PP / 2) * 8;
+  const bool biased = a.S == 1 && a.bias != nullptr;
   const bool beside = a.S == 1 && (a.mul != nullptr || a.res != nullptr);
-  Beside o[2][IT] = {};
+  constexpr int AHEAD = N < 4 ? N : 4;
+  Beside o[AHEAD][IT] = {};
+  Bias8 b[AHEAD] = {};
   auto row_of = [&](int n, int it) { return r0(n) + it * (128 / PP) + lr; };
   auto in = [&](int n, int it) { return row_of(n, it) < a.rows && c0(n) + lc < a.cols; };
   auto prefetch = [&](int n) {
+    if (biased && c0(n) + lc < a.cols) b[n % AHEAD] = load_bias(a, c0(n) + lc);
+    if (beside) {
 #pragma unroll
-    for (int it = 0; it < IT; ++it)
-      if (in(n, it)) o[n & 1][it] = load_beside(a, (size_t)row_of(n, it) * (size_t)a.cols + (size_t)(c0(n) + lc));
+      for (int it = 0; it < IT; ++it)
+        if (in(n, it)) o[n % AHEAD][it] = load_beside(a, (size_t)row_of(n, it) * (size_t)a.cols + (size_t)(c0(n) + lc));
+    }
   };
-  if (beside) prefetch(0);
+  auto put = [&](int n) {
+    char* buf = lds + (n & 1) * (32 * RB);
+    sums(n, [&](int r, int p, f32x4_t v) __attribute__((always_inline)) {
+      *reinterpret_cast<f32x4_t*>(buf + r * RB + ((p ^ key(r)) * 16)) = v;
+    });
+  };
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) prefetch(n);
+  put(0);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    if (beside && n + 1 < N) prefetch(n + 1);
-    sums(n, [&](int r, int p, f32x4_t v) __attribute__((always_inline)) {
-      *reinterpret_cast<f32x4_t*>(lds + r * RB + ((p ^ key(r)) * 16)) = v;
-    });
-    __builtin_amdgcn_sched_barrier(0);
+    // the next stripe goes to LDS while this one's reads return
+    const char* buf = lds + (n & 1) * (32 * RB);
+    float4 u[IT], w[IT];
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
       const int r = it * (128 / PP) + lr, p = lane % (PP / 2);
-      const float4 u = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p) ^ key(r)) * 16));
-      const float4 w = *reinterpret_cast<const float4*>(lds + r * RB + (((2 * p + 1) ^ key(r)) * 16));
+      u[it] = *reinterpret_cast<const float4*>(buf + r * RB + (((2 * p) ^ key(r)) * 16));
+      w[it] = *reinterpret_cast<const float4*>(buf + r * RB + (((2 * p + 1) ^ key(r)) * 16));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (n + 1 < N) put(n + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
       if (in(n, it)) {
         const size_t at = (size_t)row_of(n, it) * (size_t)a.cols + (size_t)(c0(n) + lc);
-        float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+        float v[8] = {u[it].x, u[it].y, u[it].z, u[it].w, w[it].x, w[it].y, w[it].z, w[it].w};
         if (a.S > 1) {
           float* q = a.part + (size_t)split * (size_t)a.rows * (size_t)a.cols + at;
-          *reinterpret_cast<float4*>(q) = u;
-          *reinterpret_cast<float4*>(q + 4) = w;
+          *reinterpret_cast<float4*>(q) = u[it];
+          *reinterpret_cast<float4*>(q + 4) = w[it];
         } else {
-          finish8(a, at, c0(n) + lc, v, o[n & 1][it]);
+          finish8<ACT>(a, at, v, o[n % AHEAD][it], b[n % AHEAD]);
         }
       }
     }
+    if (n + AHEAD < N) prefetch(n + AHEAD);
     __builtin_amdgcn_sched_barrier(0);
   }
 }
@@ -289,13 +320,14 @@ __device__ __forceinline__ TileAt tile_at(unsigned b, unsigned total, int mts, i
 // ---------------------------------------------------------------------------
 // BM x BN tile, WM_ x WN_ waves, NS chunks in LDS by direct loads (pipeline_xk).
 // ---------------------------------------------------------------------------
-template <int BM, int BN, int WR, int WC, int NS, bool TA, bool TB>
+template <int BM, int BN, int WR, int WC, int NS, bool TA, bool TB, int ACT>
 __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
   constexpr int W = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
   using PA = Panel<BM, TA, W>;
   using PB = Panel<BN, TB, W>;
   constexpr int STAGE = PA::BYTES + PB::BYTES;
-  constexpr int LDS = STAGE * NS > W * 32 * WN * 4 ? STAGE * NS : W * 32 * WN * 4;
+  constexpr int OUT = (MI > 1 ? 2 : 1) * 32 * WN * 4;  // of a wave (finish_stripes)
+  constexpr int LDS = STAGE * NS > W * OUT ? STAGE * NS : W * OUT;
   __shared__ __align__(16) bf16_t smem[LDS / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WC, wn = wave % WC;
@@ -354,8 +386,8 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
     }
     __syncthreads();
   }
-  finish_stripes<MI, NI>(
-      a, reinterpret_cast<char*>(smem) + wave * (32 * WN * 4), at.split, lane,
+  finish_stripes<ACT, MI, NI>(
+      a, reinterpret_cast<char*>(smem) + wave * OUT, at.split, lane,
       [&](int n, auto&& put) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
@@ -392,10 +424,11 @@ struct BigOperand {
   uint32_t off[2][4];  // of load t of half h
   uint64_t next;       // address of the chunk that is loaded next,
   uint32_t records;    // 0 past the last one
-  uint32_t fof[TR ? 4 : 2];
+  uint32_t fof[2][TR ? 4 : 2];  // fragments in slots of even and odd chunks: 64 KB apart, more than an instruction's offset holds
 
   // slot row (TR: column) q of half h is the tile's row 128 (q / 64) + 64 h + q % 64
-  __device__ __forceinline__ void init(const void* p, int ld, int first, int left, int wsel, int wave, int lane) {
+  __device__ __forceinline__ void init(const void* p, int ld, int first, int left, int wsel, int wave, int lane,
+                                       uint32_t lds) {
     base = static_cast<const char*>(p) + (TR ? (size_t)first * 2 : (size_t)first * (size_t)ld * 2);
     step = TR ? (uint64_t)ld * (kChunk * 2) : (uint64_t)(kChunk * 2);
 #pragma unroll
@@ -420,12 +453,17 @@ struct BigOperand {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int colb = (wsel * 64 + i * 16) * 2 + 8 * (lane & 3);
-        fof[i] = (uint32_t)(row * RB + tr_piece<128>(row, colb >> 4) * 16 + (colb & 15));
+        fof[0][i] = lds + (uint32_t)(row * RB + tr_piece<128>(row, colb >> 4) * 16 + (colb & 15));
+        fof[1][i] = fof[0][i] + 4 * kSlotBytes;
+        asm("" : "+v"(fof[1][i]));  // a register of its own, not an addition at each read
       }
     } else {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        fof[s] = (uint32_t)((wsel * 64 + r) * RB + swz_chunk<kChunk>(r, 4 * s + g) * 16);
+      for (int s = 0; s < 2; ++s) {
+        fof[0][s] = lds + (uint32_t)((wsel * 64 + r) * RB + swz_chunk<kChunk>(r, 4 * s + g) * 16);
+        fof[1][s] = fof[0][s] + 4 * kSlotBytes;
+        asm("" : "+v"(fof[1][s]));
+      }
     }
   }
   // Chunk kc is next; live: -1, or 0 past the last one. Offsets are in the operand by
@@ -438,24 +476,28 @@ struct BigOperand {
     next += step;
     records = (uint32_t)live;
   }
-  // Load t of half h to LDS byte address lds + at. M0 needs one wait state; a descriptor
-  // that vector instructions have written (FIRST: as start leaves it) five, which the
-  // compiler, not seeing the load, would not keep.
-  template <bool FIRST = false>
-  __device__ __forceinline__ void load(int h, int t, uint32_t lds, int at) const {
+  // Load t of half h to the LDS byte address that M0 holds (aim_m0). Between that write of
+  // M0 and the load there must be another instruction.
+  __device__ __forceinline__ void load(int h, int t) const {
     const u32x4_t srd = {(uint32_t)next, (uint32_t)(next >> 32), records, 0x00020000u};
-    if (FIRST) asm volatile("s_nop 4" ::"s"(srd) : "memory");
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+    asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off[h][t]), "s"(srd) : "memory");
+  }
+  // The same, with the wait states that M0 (one) and a descriptor that vector instructions
+  // have written (five: as start leaves it) need and the compiler, not seeing the load,
+  // would not keep.
+  __device__ __forceinline__ void load_first(int h, int t, uint32_t lds, int at) const {
+    const u32x4_t srd = {(uint32_t)next, (uint32_t)(next >> 32), records, 0x00020000u};
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                  :
                  : "v"(off[h][t]), "s"(srd), "s"(lds), "is"(at)
                  : "memory", "scc");
   }
   // fragment of block i (16 rows of the wave's 64) at k-step s (32 of the chunk's 64) of
-  // the slot at byte `slot`
-  __device__ __forceinline__ bf16x8_t frag(uint32_t lds, int slot, int i, int s) const {
+  // slot w of a chunk of parity par
+  __device__ __forceinline__ bf16x8_t frag(int w, int par, int i, int s) const {
     if constexpr (TR) {
       typedef __attribute__((address_space(3))) s16x4_t* lds4;
-      const uint32_t at = lds + fof[i] + (uint32_t)(slot + s * 32 * RB);
+      const uint32_t at = fof[par][i] + (uint32_t)(w * kSlotBytes + s * 32 * RB);
       const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at));
       const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds4>(at + 4 * RB));
       struct {
@@ -465,7 +507,7 @@ struct BigOperand {
     } else {
       typedef __attribute__((address_space(3))) u32x4_t* lds16;
       // rows 16 apart swizzle alike
-      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<lds16>(lds + fof[s] + (uint32_t)(slot + i * 16 * RB)));
+      return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<lds16>(fof[par][s] + (uint32_t)(w * kSlotBytes + i * 16 * RB)));
     }
   }
   // the partial chunk kc (n of 64) into the slots at `slot` of half h, zeros past its end
@@ -482,7 +524,7 @@ struct BigOperand {
   }
 };
 
-template <bool TA, bool TB>
+template <bool TA, bool TB, int ACT>
 __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   __shared__ __align__(16) bf16_t smem[8 * kSlotBytes / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -495,9 +537,9 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   const int nK = uniform_int((int)((long long)(at.split + 1) * chunks / a.S)) - kc0;
   BigOperand<TA> A;
   BigOperand<TB> B;
-  A.init(a.A, a.lda, row0, a.rows - row0, wm, wave, lane);
-  B.init(a.B, a.ldb, col0, a.cols - col0, wn, wave, lane);
   const uint32_t lds = lds_addr(smem), lds0 = lds + wave * 1024;
+  A.init(a.A, a.lda, row0, a.rows - row0, wm, wave, lane, lds);
+  B.init(a.B, a.ldb, col0, a.cols - col0, wn, wave, lane, lds);
   bf16x8_t fr[4][4][2];  // [slot: A0, A1, B0, B1][block][k-step]
   f32x4_t acc[2][2][4][4];  // [A half][B half][row block][column block]
 #pragma unroll
@@ -510,23 +552,21 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
         for (int j = 0; j < 4; ++j) acc[h][b][i][j] = f32x4_t{};
   // load t of slot w of the chunk (of parity par) that its operand is at
   auto issue = [&](int w, int par, int t) __attribute__((always_inline)) {
-    if (w < 2)
-      A.load(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
-    else
-      B.load(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
+    w < 2 ? A.load(w & 1, t) : B.load(w & 1, t);
+  };
+  // M0: the LDS address of that load; nothing else in the loop uses it
+  auto aim = [&](int w, int par, int t) __attribute__((always_inline)) {
+    asm volatile("s_add_u32 m0, %0, %1" ::"s"(lds0), "is"((par * 4 + w) * kSlotBytes + t * 4096) : "memory", "scc");
   };
   auto issue_slot = [&](int w, int par) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      if (w < 2)
-        A.template load<true>(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
-      else
-        B.template load<true>(w & 1, t, lds0, (par * 4 + w) * kSlotBytes + t * 4096);
+      const int at = (par * 4 + w) * kSlotBytes + t * 4096;
+      w < 2 ? A.load_first(w & 1, t, lds0, at) : B.load_first(w & 1, t, lds0, at);
     }
   };
   auto readf = [&](int w, int par, int i, int q) __attribute__((always_inline)) {
-    const int slot = (par * 4 + w) * kSlotBytes;
-    fr[w][i][q] = w < 2 ? A.frag(lds, slot, i, q) : B.frag(lds, slot, i, q);
+    fr[w][i][q] = w < 2 ? A.frag(w, par, i, q) : B.frag(w, par, i, q);
   };
   // As inline assembly, in place in the accumulation registers: as a builtin the compiler
   // gives result and addend of these small blocks different registers and moves them about.
@@ -539,24 +579,23 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   };
   // One phase: the MFMAs of quadrant (ha, hb); reads slot rw (of parity rp), refills slot iw
   // (of parity ip; its last read was the phase before). step(): what moves a descriptor on.
-  // In exactly this order: two MFMAs, a fragment or a load, two MFMAs, ...
+  // In exactly this order: an MFMA takes 16 cycles of the matrix pipe and 4 of the wave's
+  // issue, so the gap after it holds two or three other instructions; more would leave the
+  // pipe idle.
   auto phase = [&](int ha, int hb, int rw, int rp, int iw, int ip, auto&& step) __attribute__((always_inline)) {
     wait_lgkmcnt0();      // the fragments read in the last phase are here
     wait_vmcnt<6 * 4>();  // this wave's loads of slot rw landed
     lds_barrier();        // everyone's; and everyone has read slot iw
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int s = t >> 1, i = 2 * (t & 1) + (e >> 1), j = 2 * (e & 1);
-        __builtin_amdgcn_sched_barrier(0);
-        mma(ha, hb, i, j, s);
-        mma(ha, hb, i, j + 1, s);
-        __builtin_amdgcn_sched_barrier(0);
-        if (t < 2) readf(rw, rp, e, t);
-        if (e == 0 && t == 0) step();
-        if (e == 1) issue(iw, ip, t);
-      }
+    for (int g = 0; g < 32; ++g) {
+      __builtin_amdgcn_sched_barrier(0);
+      mma(ha, hb, (g >> 2) & 3, g & 3, g >> 4);
+      __builtin_amdgcn_sched_barrier(0);
+      if (g < 16 && g % 2 == 1) readf(rw, rp, (g >> 1) & 3, g >> 3);
+      if (g == 0) step();
+      if (g % 8 == 2) aim(iw, ip, g >> 3);
+      if (g % 8 == 4) issue(iw, ip, g >> 3);
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
   auto keep = [] {};
@@ -647,8 +686,8 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   }
   settle();
   // stripe n: B half n / 4, A half n / 2 % 2, row blocks 2 (n % 2) and the next
-  finish_stripes<8, 2>(
-      a, reinterpret_cast<char*>(smem) + wave * 8192, at.split, lane,
+  finish_stripes<ACT, 8, 2>(
+      a, reinterpret_cast<char*>(smem) + wave * 16384, at.split, lane,
       [&](int n, auto&& put) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -660,12 +699,15 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
 }
 
 // Joins the S partial sums of every output, in their order.
+template <int ACT>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
   const size_t n8 = (size_t)a.rows * (size_t)(a.cols / 8), plane = (size_t)a.rows * (size_t)a.cols;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
     const float4 u = sum_splits(a.part + i * 8, plane, a.S), w = sum_splits(a.part + i * 8 + 4, plane, a.S);
     float v[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-    finish8(a, i * 8, (int)(i % (size_t)(a.cols / 8)) * 8, v, load_beside(a, i * 8));
+    Bias8 b{};
+    if (a.bias != nullptr) b = load_bias(a, (int)(i % (size_t)(a.cols / 8)) * 8);
+    finish8<ACT>(a, i * 8, v, load_beside(a, i * 8), b);
   }
 }
 
@@ -673,7 +715,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
 // fp32 (the tiny layer, a parity configuration): a 64 x 64 tile, 4 x 4 outputs a
 // thread, plain sums.
 // ---------------------------------------------------------------------------
-template <bool TA, bool TB>
+template <bool TA, bool TB, int ACT>
 __global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
   __shared__ float la[16][65], lb[16][65];
   const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
@@ -713,7 +755,7 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
       float v = acc[i][j];
       if (a.bias != nullptr) v += a.bias[col];
       if (a.z != nullptr) static_cast<float*>(a.z)[at] = v;
-      v = act_value(v, a.act);
+      v = act_value<ACT>(v);
       if (a.mul != nullptr) v *= static_cast<const float*>(a.mul)[at];
       if (a.res != nullptr) v += static_cast<const float*>(a.res)[at];
       (a.out32 != nullptr ? a.out32 : static_cast<float*>(a.out))[at] = v;
@@ -729,10 +771,10 @@ struct ActBackwardArgs {
   const void *dy, *z, *mul;
   void *dz, *dmul;  // or null
   float* db;        // [P][cols], or null
-  int rows, cols, P, act;
+  int rows, cols, P;
 };
 
-template <bool BF16>
+template <bool BF16, int ACT>
 __global__ __launch_bounds__(256) void act_backward_kernel(ActBackwardArgs a) {
   __shared__ float sums[8][256];
   const int tid = threadIdx.x, c8 = tid % 32, ry = tid / 32;
@@ -767,13 +809,13 @@ __global__ __launch_bounds__(256) void act_backward_kernel(ActBackwardArgs a) {
       if (a.dmul != nullptr) {
         float g[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) g[q] = d[q] * act_value(z[q], a.act);
+        for (int q = 0; q < 8; ++q) g[q] = d[q] * act_value<ACT>(z[q]);
         store(a.dmul, at, g);
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         if (a.mul != nullptr) d[q] *= m[q];
-        if (a.act != kActNone) d[q] *= act_slope(z[q], a.act);
+        if (ACT != kActNone) d[q] *= act_slope<ACT>(z[q]);
         db[q] += d[q];
       }
       if (a.dz != nullptr) store(a.dz, at, d);
@@ -836,11 +878,11 @@ size_t product_ws(int rows, int cols, int red, bool bf16) {
   return p.S > 1 ? (size_t)p.S * (size_t)rows * (size_t)cols * 4 : 0;
 }
 
-template <bool TA, bool TB>
+template <bool TA, bool TB, int ACT>
 hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   if (!bf16) {
     const long long tiles = ((a.rows - 1LL) / 64 + 1) * ((a.cols - 1LL) / 64 + 1);
-    linear_f32_kernel<TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+    linear_f32_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
     return hipGetLastError();
   }
   const LinPlan p = linear_plan(a.rows, a.cols, a.red);
@@ -848,15 +890,15 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   a.part = static_cast<float*>(ws);
   const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
   if (p.tile == 256)
-    linear_big_kernel<TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+    linear_big_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
   else if (p.tile == 128)
-    linear_tile_kernel<128, 128, 2, 4, 4, TA, TB><<<(unsigned)tiles, 512, 0, s>>>(a);
+    linear_tile_kernel<128, 128, 2, 4, 4, TA, TB, ACT><<<(unsigned)tiles, 512, 0, s>>>(a);
   else
-    linear_tile_kernel<64, 64, 2, 2, 4, TA, TB><<<(unsigned)tiles, 256, 0, s>>>(a);
+    linear_tile_kernel<64, 64, 2, 2, 4, TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.S == 1) return e;
   const size_t n8 = (size_t)a.rows * (size_t)(a.cols / 8);
-  linear_join_kernel<<<(unsigned)std::min<size_t>((n8 + 255) / 256, 8 * (size_t)device_cu_count()), 256, 0, s>>>(a);
+  linear_join_kernel<ACT><<<(unsigned)std::min<size_t>((n8 + 255) / 256, 8 * (size_t)device_cu_count()), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -879,8 +921,8 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
   LinArgs a{};
   a.A = c.x, a.B = c.w, a.lda = c.K, a.ldb = c.ldw;
   a.rows = c.M, a.cols = c.N, a.red = c.K;
-  a.bias = c.bias, a.mul = c.mul, a.res = c.residual, a.z = c.z, a.out = c.y, a.act = c.act;
-  return launch_product<false, false>(a, c.bf16, ws, s);
+  a.bias = c.bias, a.mul = c.mul, a.res = c.residual, a.z = c.z, a.out = c.y;
+  return with_act(c.act, [&](auto act) { return launch_product<false, false, decltype(act)::value>(a, c.bf16, ws, s); });
 }
 
 size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16) {
@@ -906,17 +948,20 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
   const int P = bias_ranges(c.M, c.N);
   if (own || c.dbias != nullptr) {
     ActBackwardArgs b{};
-    b.dy = c.dy, b.mul = c.mul, b.dmul = c.dmul, b.act = c.act;
+    b.dy = c.dy, b.mul = c.mul, b.dmul = c.dmul;
     b.z = c.act != kActNone || c.dmul != nullptr ? c.z : nullptr;
     b.dz = own ? c.dz : nullptr;
     b.rows = c.M, b.cols = c.N, b.P = P;
     b.db = c.dbias == nullptr ? nullptr : P > 1 ? static_cast<float*>(ws) : c.dbias;
     const unsigned grid = (unsigned)(((c.N - 1) / 256 + 1) * P);
-    if (c.bf16)
-      act_backward_kernel<true><<<grid, 256, 0, s>>>(b);
-    else
-      act_backward_kernel<false><<<grid, 256, 0, s>>>(b);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = with_act(c.act, [&](auto act) {
+      if (c.bf16)
+        act_backward_kernel<true, decltype(act)::value><<<grid, 256, 0, s>>>(b);
+      else
+        act_backward_kernel<false, decltype(act)::value><<<grid, 256, 0, s>>>(b);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
     if (c.dbias != nullptr && P > 1) {
       bias_join_kernel<<<(unsigned)((c.N + 255) / 256), 256, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
       if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -928,7 +973,7 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     LinArgs a{};
     a.A = dz, a.B = c.w, a.lda = c.N, a.ldb = c.ldw;
     a.rows = c.M, a.cols = c.K, a.red = c.N, a.out = c.dx;
-    if ((e = launch_product<false, true>(a, c.bf16, part, s)) != hipSuccess) return e;
+    if ((e = launch_product<false, true, kActNone>(a, c.bf16, part, s)) != hipSuccess) return e;
   }
   if (c.dw != nullptr) {
     LinArgs a{};
@@ -938,7 +983,7 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
       a.out = c.dw;
     else
       a.out32 = static_cast<float*>(c.dw);
-    if ((e = launch_product<true, true>(a, c.bf16, part, s)) != hipSuccess) return e;
+    if ((e = launch_product<true, true, kActNone>(a, c.bf16, part, s)) != hipSuccess) return e;
   }
   return e;
 }
