@@ -9,6 +9,7 @@ raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -691,13 +692,27 @@ def _code(table, name, what):
 
 
 def _on(t, name, dtype, dev, shape):
-    """Pointer of a contiguous tensor of the given type and shape on GPU `dev`, the current one."""
-    p = _dev(t, name, dtype)
+    """Pointer of a contiguous tensor of the given type and shape on GPU `dev`, the current one.
+    What is right is told from a few attributes; what is wrong, in _dev and below."""
+    try:
+        if t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype)
     if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current GPU, cuda:{dev}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    return p
+    raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+@functools.lru_cache(maxsize=256)
+def _size_ref(n):
+    """A workspace's size as the calls take it; with a workspace they only read it."""
+    return ctypes.byref(ctypes.c_size_t(n))
 
 
 def _weight(w, name, dtype, dev):
@@ -742,7 +757,7 @@ def moe_route(logits, k, score="sigmoid", bias=None, mask=None, n_group=1, topk_
                      None if bias is None else _on(bias, "bias", torch.float32, dev, (E,)),
                      None if mask is None else _on(mask, "mask", torch.uint8, dev, (T,)), T, E, k, code, n_group,
                      topk_group, 1 if norm else 0, scale, _on(ids, "ids", torch.int32, dev, (T, k)),
-                     _on(weights, "weights", torch.float32, dev, (T, k)), _stream())
+                     _on(weights, "weights", torch.float32, dev, (T, k)), _raw_stream(dev))
     _check("moe_route", st)
     return ids, weights
 
@@ -760,7 +775,7 @@ def moe_route_backward(logits, ids, dweights, score="sigmoid", norm=True, scale=
         dlogits = torch.empty_like(logits)
     st = L.moe_route_backward(_on(logits, "logits", torch.float32, dev, (T, E)), _on(ids, "ids", torch.int32, dev, (T, k)),
                               _on(dweights, "dweights", torch.float32, dev, (T, k)), T, E, k, code, 1 if norm else 0, scale,
-                              1 if accumulate else 0, _on(dlogits, "dlogits", torch.float32, dev, (T, E)), _stream())
+                              1 if accumulate else 0, _on(dlogits, "dlogits", torch.float32, dev, (T, E)), _raw_stream(dev))
     _check("moe_route_backward", st)
     return dlogits
 
@@ -789,7 +804,7 @@ def _workspace(ws, need, dev, device):
     n = ws.numel()
     if n == 0:  # a null pointer would ask for the size
         raise ValueError("ws must not be empty")
-    return ws, _on(ws, "ws", torch.uint8, dev, ws.shape), ctypes.byref(ctypes.c_size_t(n))
+    return ws, _on(ws, "ws", torch.uint8, dev, ws.shape), _size_ref(n)
 
 
 def moe_linear(x, w, bias=None, act="none", mul=None, residual=None, z=None, out=None, ws=None):
@@ -814,7 +829,7 @@ def moe_linear(x, w, bias=None, act="none", mul=None, residual=None, z=None, out
                       None if mul is None else _on(mul, "mul", dtype, dev, (M, N)),
                       None if residual is None else _on(residual, "residual", dtype, dev, (M, N)), M, N, K, ldw, code, dt,
                       _on(out, "out", dtype, dev, (M, N)), None if z is None else _on(z, "z", dtype, dev, (M, N)), wsp,
-                      wsn, _stream())
+                      wsn, _raw_stream(dev))
     _check("moe_linear", st)
     return out
 
@@ -853,7 +868,7 @@ def moe_linear_backward(dy, x, w, z=None, act="none", mul=None, need_dx=True, ne
     st = L.moe_linear_backward(dyp, xp, wp, None if z is None else _on(z, "z", dtype, dev, (M, N)),
                                None if mul is None else _on(mul, "mul", dtype, dev, (M, N)), M, N, K, ldw, code, dt, dzp,
                                dmp, dxp, dwp, MOE_BF16 if dw_dtype == torch.bfloat16 else MOE_F32, dbp, wsp, wsn,
-                               _stream())
+                               _raw_stream(dev))
     _check("moe_linear_backward", st)
     return dx, dw, dbias, dz, dmul
 
@@ -871,7 +886,7 @@ def moe_dropout_add(x, p, rng, residual=None, out=None):
     if out is None:
         out = torch.empty_like(x)
     st = L.moe_dropout_add(xp, None if residual is None else _on(residual, "residual", dtype, dev, shape), x.numel(), p,
-                           _on(rng, "rng", torch.int64, dev, (2,)), dt, _on(out, "out", dtype, dev, shape), _stream())
+                           _on(rng, "rng", torch.int64, dev, (2,)), dt, _on(out, "out", dtype, dev, shape), _raw_stream(dev))
     _check("moe_dropout_add", st)
     return out
 

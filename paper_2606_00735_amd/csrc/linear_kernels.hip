@@ -698,6 +698,69 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
       [&](int n) { return row0 + wm * 128 + (n & 3) * 32; }, [&](int n) { return col0 + wn * 128 + (n >> 2) * 64; });
 }
 
+// ---------------------------------------------------------------------------
+// Few rows (of x): 16 MB of them by 16 columns a block. The weights are read once, from
+// memory to the 16 x 16 x 32 MFMA's registers, the reduction dealt to the W waves k-step
+// by k-step, so that together they read whole lines; their sums are joined in LDS. With
+// one row it is a chain of three latencies (operands, join, stores) around the weights'
+// bytes. All loads of G k-steps are in flight together.
+// ---------------------------------------------------------------------------
+template <int MB, int W, int G, int ACT>
+__global__ __launch_bounds__(W* kWave) void linear_few_kernel(LinArgs a) {
+  __shared__ __align__(16) float part[W][MB][16][16];  // [wave][..][row][column]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int col0 = (int)blockIdx.x * 16;
+  // what the epilogue needs, by the lanes that run it
+  const int er = tid >> 1, ec = col0 + (tid & 1) * 8;
+  const bool mine = tid < MB * 32 && er < a.rows && ec < a.cols;
+  const size_t at = (size_t)er * (size_t)a.cols + (size_t)ec;
+  Beside o{};
+  Bias8 b{};
+  if (mine) {
+    o = load_beside(a, at);
+    if (a.bias != nullptr) b = load_bias(a, ec);
+  }
+  const bf16_t* w = static_cast<const bf16_t*>(a.B) + (size_t)min(col0 + r, a.cols - 1) * (size_t)a.ldb;
+  const bf16_t* x[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) x[m] = static_cast<const bf16_t*>(a.A) + (size_t)min(m * 16 + r, a.rows - 1) * (size_t)a.lda;
+  f32x4_t acc[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) acc[m] = f32x4_t{};
+  // k-steps of 32; the lane's 8 elements of one are there or not (K % 8 == 0)
+  const int steps = (a.red + 31) / 32;
+  for (int s0 = wave; s0 < steps; s0 += W * G) {
+    uint4 fw[G], fx[G][MB];
+#pragma unroll
+    for (int q = 0; q < G; ++q) {
+      const int k = (s0 + q * W) * 32 + 8 * g;
+      const bool in = k < a.red;
+      fw[q] = in ? *reinterpret_cast<const uint4*>(w + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) fx[q][m] = in ? *reinterpret_cast<const uint4*>(x[m] + k) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < G; ++q)
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fw[q]), as_bf16x8(fx[q][m]), acc[m], 0, 0, 0);
+  }
+  // the lane holds columns 4 g .. 4 g + 3 of row r
+#pragma unroll
+  for (int m = 0; m < MB; ++m) *reinterpret_cast<f32x4_t*>(&part[wave][m][r][4 * g]) = acc[m];
+  __syncthreads();
+  if (!mine) return;
+  float v[8] = {};
+#pragma unroll
+  for (int q = 0; q < W; ++q) {
+    const float* p = &part[q][0][er][(tid & 1) * 8];
+    const float4 u = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+    v[0] += u.x, v[1] += u.y, v[2] += u.z, v[3] += u.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+  }
+  finish8<ACT>(a, at, v, o, b);
+}
+
 // Joins the S partial sums of every output, in their order.
 template <int ACT>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs a) {
@@ -850,13 +913,16 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t* p, size_t n) {
 // Which kernel a product takes.
 // ---------------------------------------------------------------------------
 struct LinPlan {
-  int tile;  // rows and columns of a tile
+  int tile;  // rows and columns of a tile; 0: few rows
   int S;
 };
+constexpr int kFewRows = 32;
 
 constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 
-LinPlan linear_plan(int rows, int cols, int red) {
+// few: the kernel of few rows can run (no operand is transposed)
+LinPlan linear_plan(int rows, int cols, int red, bool few) {
+  if (few && rows <= kFewRows) return {0, 1};
   const long long cus = device_cu_count();
   auto tiles = [&](int t) { return ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1); };
   LinPlan p{tiles(256) >= cus * 3 / 4 ? 256 : tiles(128) >= cus ? 128 : 64, 1};
@@ -872,9 +938,9 @@ LinPlan linear_plan(int rows, int cols, int red) {
   return p;
 }
 
-size_t product_ws(int rows, int cols, int red, bool bf16) {
+size_t product_ws(int rows, int cols, int red, bool few, bool bf16) {
   if (!bf16 || rows == 0) return 0;
-  const LinPlan p = linear_plan(rows, cols, red);
+  const LinPlan p = linear_plan(rows, cols, red, few);
   return p.S > 1 ? (size_t)p.S * (size_t)rows * (size_t)cols * 4 : 0;
 }
 
@@ -885,9 +951,19 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
     linear_f32_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
     return hipGetLastError();
   }
-  const LinPlan p = linear_plan(a.rows, a.cols, a.red);
+  const LinPlan p = linear_plan(a.rows, a.cols, a.red, !TA && !TB);
   a.S = p.S;
   a.part = static_cast<float*>(ws);
+  if constexpr (!TA && !TB) {
+    if (p.tile == 0) {
+      const unsigned blocks = (unsigned)((a.cols + 15) / 16);
+      if (a.rows <= 16)
+        linear_few_kernel<1, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
+      else
+        linear_few_kernel<2, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
+      return hipGetLastError();
+    }
+  }
   const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
   if (p.tile == 256)
     linear_big_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
@@ -915,7 +991,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // Never 0: a call without a workspace asks for its size.
 constexpr size_t kLinearWsLeast = 256;
 
-size_t linear_ws_bytes(int M, int N, int K, bool bf16) { return std::max(kLinearWsLeast, product_ws(M, N, K, bf16)); }
+size_t linear_ws_bytes(int M, int N, int K, bool bf16) { return std::max(kLinearWsLeast, product_ws(M, N, K, true, bf16)); }
 
 hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
   LinArgs a{};
@@ -928,7 +1004,7 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
 size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16) {
   if (M == 0) return kLinearWsLeast;
   return align256((size_t)bias_ranges(M, N) * (size_t)N * 4) +
-         std::max(product_ws(M, K, N, bf16), product_ws(N, K, M, bf16));
+         std::max(product_ws(M, K, N, false, bf16), product_ws(N, K, M, false, bf16));
 }
 
 hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStream_t s) {
