@@ -184,6 +184,317 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 }
 
 // ---------------------------------------------------------------------------
+// Sixteen lanes a token, lane l the experts l V .. l V + V - 1, where groups are whole
+// lanes (1, 2, 4, 8 or 16 of them) or there is one group.
+//
+// The selection runs on 32-bit keys: c in fp32 (an exponential and a reciprocal of 1 ulp),
+// mapped to integers in the same order, the lowest 4 bits replaced by the position in the
+// lane, so that a round is a maximum over the lane's keys and four DPP maxima. What fp32
+// cannot decide is seen from the gaps: the k + 1 best have to be further apart, and the
+// last group kept from the first one left out, than twice what their keys can be off
+// (`wide`); a wave with a token where they are not (about one in fifty of a batch of
+// normal logits) and one with a NaN, an infinite score or a slot without an expert selects
+// again in 64 bits. 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64
+// bits, a wave each.
+// ---------------------------------------------------------------------------
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float x) {
+  return __uint_as_float(dpp_u32<CTRL>(__float_as_uint(x)));
+}
+// over 16 lanes; every lane gets the result
+template <class T, class Op>
+__device__ __forceinline__ T row_reduce(T x, Op op) {
+  auto at = [&](auto step) {
+    constexpr int C = decltype(step)::value;
+    if constexpr (std::is_same<T, float>::value)
+      return dpp_f<C>(x);
+    else
+      return dpp_u32<C>(x);
+  };
+  x = op(x, at(std::integral_constant<int, 0xB1>{}));   // quad_perm 1,0,3,2
+  x = op(x, at(std::integral_constant<int, 0x4E>{}));   // quad_perm 2,3,0,1
+  x = op(x, at(std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  x = op(x, at(std::integral_constant<int, 0x140>{}));  // row_mirror
+  return x;
+}
+__device__ __forceinline__ float row_max(float x) {
+  return row_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float row_min(float x) {
+  return row_reduce(x, [](float a, float b) { return fminf(a, b); });
+}
+__device__ __forceinline__ float row_sum(float x) {
+  return row_reduce(x, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ double row_sum64(double x) {
+#pragma unroll
+  for (int m = 1; m < 16; m <<= 1) x += shfl_xor_f64(x, m);
+  return x;
+}
+
+// fp32 in the order of unsigned integers; 0 is below every number
+__device__ __forceinline__ uint32_t order_key(float c) {
+  const uint32_t u = __float_as_uint(c);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  const uint32_t u = k & ~15u;
+  return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
+}
+
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+
+struct RouteArgs {
+  const float* z;
+  const float* bias;
+  const uint8_t* mask;
+  int T, E, k;
+  int groups, kept;  // groups 1: no grouping
+  int norm;
+  double scale;
+  int32_t* ids;
+  float* w;
+};
+
+// The selection of a token in 64 bits: this lane's slot (lane l: slot l) in id and its
+// logit in zsel; bad: the row has a NaN or an infinite score. All 64 lanes call it, tokens of their own every 16. Keys
+// are in LDS, a lane's own at keys[256 v], and every loop is rolled: rarely run, it is to
+// take neither registers nor code from what surrounds it.
+template <int V, bool SOFT>
+__device__ __forceinline__ void select64(const RouteArgs& a, const float* row, int l, bool live, double* keys, int& id,
+                                         float& zsel, bool& bad) {
+  const double ninf = -INFINITY;
+  const int E = a.E;
+  auto logit = [&](int v) { return l * V + v < E ? row[l * V + v] : -INFINITY; };
+  float m = -INFINITY;
+  bad = false;
+#pragma unroll 1
+  for (int v = 0; v < V; ++v) {
+    const float z = logit(v);
+    const bool out = z != z || (SOFT && z == INFINITY);
+    bad |= out;
+    if (!out) m = fmaxf(m, z);
+  }
+  m = row_max(m);
+  bad = row_max(bad ? 1.0f : 0.0f) != 0.0f;
+  auto rises = [](float z) { return z > -INFINITY && z < INFINITY; };
+  double sum = 0.0;
+  if (SOFT) {
+#pragma unroll 1
+    for (int v = 0; v < V; ++v) {
+      const float z = logit(v);
+      sum += rises(z) ? exp((double)z - (double)m) : 0.0;
+    }
+    sum = row_sum64(sum);
+  }
+  auto score = [&](float z) {
+    if (SOFT) return rises(z) ? exp((double)z - (double)m) / sum : 0.0;
+    return 1.0 / (1.0 + exp(-(double)z));
+  };
+  double x = ninf, y = ninf;  // the two largest of the lane, then of the group
+#pragma unroll 1
+  for (int v = 0; v < V; ++v) {
+    const int e = l * V + v;
+    const float z = logit(v);
+    const double c = score(z) + (a.bias != nullptr && e < E ? (double)a.bias[e] : 0.0);
+    const double key = z > -INFINITY && !(SOFT && z == INFINITY) && c > ninf ? c : ninf;
+    keys[256 * v] = key;
+    y = fmax(y, fmin(x, key));
+    x = fmax(x, key);
+  }
+  bool on = true;
+  if (a.groups > 1) {
+    const int LG = 16 / a.groups;
+#pragma unroll 1
+    for (int q = 1; q < LG; q <<= 1) {
+      const double ox = shfl_xor_f64(x, q), oy = shfl_xor_f64(y, q);
+      y = fmax(fmin(x, ox), fmax(y, oy));
+      x = fmax(x, ox);
+    }
+    const double mine = y > ninf ? x + y : x;
+    int before = 0;  // lanes of groups that come before this one
+#pragma unroll 1
+    for (int q = 1; q < 16; ++q) {
+      const double other = shfl_xor_f64(mine, q);
+      before += other > mine || (other == mine && (l ^ q) / LG < l / LG);
+    }
+    on = before < a.kept * LG;
+  }
+  id = -1;
+  zsel = -INFINITY;
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {
+    double bv = ninf;
+    int bi = INT32_MAX;
+#pragma unroll 1
+    for (int v = 0; v < V; ++v) {
+      const double key = on ? keys[256 * v] : ninf;
+      if (key > bv) bv = key, bi = l * V + v;
+    }
+#pragma unroll 1
+    for (int q = 1; q < 16; q <<= 1) {
+      const double ov = shfl_xor_f64(bv, q);
+      const int oi = __shfl_xor(bi, q, kWave);
+      if (ov > bv || (ov == bv && oi < bi)) bv = ov, bi = oi;
+    }
+    if (bv > ninf) {
+      if (bi / V == l) keys[256 * (bi % V)] = ninf;
+      if (l == j && live) id = bi, zsel = row[bi];
+    }
+  }
+}
+
+template <int V, bool SOFT>
+__global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
+  __shared__ double keys64[V * 256];  // of select64
+  const int lane = threadIdx.x & 63, l = lane & 15;
+  const long long t = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const size_t r = (size_t)(t < a.T ? t : a.T - 1);  // lanes past the last token repeat it and store nothing
+  const int E = a.E, e0 = l * V;
+  const float* row = a.z + r * (size_t)E;
+  float z[V];
+  if (V % 4 == 0 && E % 4 == 0) {
+#pragma unroll
+    for (int v = 0; v < V / 4; ++v) {
+      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (e0 + 4 * v < E) q = *reinterpret_cast<const float4*>(row + e0 + 4 * v);
+      z[4 * v % V] = q.x, z[(4 * v + 1) % V] = q.y, z[(4 * v + 2) % V] = q.z, z[(4 * v + 3) % V] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] = e0 + v < E ? row[e0 + v] : -INFINITY;
+  }
+  const bool live = a.mask == nullptr || a.mask[r] != 0;
+  const bool biased = a.bias != nullptr;
+  // range of the row's finite logits; ok: no NaN, no +inf
+  float hi = -INFINITY, lo = INFINITY;
+  bool ok = true;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    ok &= z[v] < INFINITY;
+    hi = fmaxf(hi, z[v]);
+    lo = fminf(lo, z[v] > -INFINITY ? z[v] : INFINITY);
+  }
+  hi = row_max(hi), lo = row_min(lo);
+  // What a score can be off, relative to it. sigmoid: the argument of the exponential (its
+  // product with log2 e, 1.5 2^-24 of it), 1 ulp each of exponential and reciprocal, a sum.
+  // softmax: a difference in the argument, too, and a sum of up to 20 steps.
+  const float span = fminf(SOFT ? hi - lo : fmaxf(fabsf(hi), fabsf(lo)), 128.0f);
+  const float rel = SOFT ? 0x1p-19f + span * 0x1p-22f : 0x1p-21f + span * 0x1p-23f;
+  uint32_t key[V];
+  float inv = 1.0f, top = 1.0f;  // 1 / sum, the largest score
+  if (SOFT) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum += z[v] > -INFINITY ? exp_fast(z[v] - hi) : 0.0f;
+    sum = row_sum(sum);
+    inv = __builtin_amdgcn_rcpf(sum);
+    top = inv;
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float c = SOFT ? exp_fast(z[v] - hi) * inv : __builtin_amdgcn_rcpf(1.0f + exp_fast(-z[v]));
+    if (biased) c += e0 + v < E ? a.bias[e0 + v] : 0.0f;
+    key[v] = z[v] > -INFINITY && c > -INFINITY ? (order_key(c) & ~15u) | (uint32_t)(15 - v) : 0u;
+  }
+  // twice what two keys' values, at most x and at most y in size, can differ by from
+  // their exact ones: the 4 bits, the sum with the bias, the scores
+  auto wide = [&](float gap, float x, float y) {
+    const float size = fmaxf(fabsf(x), fabsf(y));
+    return gap > 2.0f * (size * 0x1.1p-19f + rel * (biased ? top : size)) + 0x1p-120f;
+  };
+  if (a.groups > 1) {
+    uint32_t x = 0, y = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      y = max(y, min(x, key[v]));
+      x = max(x, key[v]);
+    }
+    const int LG = 16 / a.groups;
+    auto join = [&](uint32_t ox, uint32_t oy) {
+      y = max(min(x, ox), max(y, oy));
+      x = max(x, ox);
+    };
+    if (LG >= 2) join(dpp_u32<0xB1>(x), dpp_u32<0xB1>(y));
+    if (LG >= 4) join(dpp_u32<0x4E>(x), dpp_u32<0x4E>(y));
+    if (LG >= 8) join(dpp_u32<0x141>(x), dpp_u32<0x141>(y));
+    const float vx = x ? key_value(x) : -INFINITY, vy = y ? key_value(y) : 0.0f;
+    const float score = vx + vy, size = x ? fabsf(vx) + fabsf(vy) : 0.0f;
+    int before = 0;  // lanes of groups with a larger score
+    auto see = [&](float os) { before += os > score; };
+    see(dpp_f<0x121>(score)), see(dpp_f<0x122>(score)), see(dpp_f<0x123>(score)), see(dpp_f<0x124>(score));
+    see(dpp_f<0x125>(score)), see(dpp_f<0x126>(score)), see(dpp_f<0x127>(score)), see(dpp_f<0x128>(score));
+    see(dpp_f<0x129>(score)), see(dpp_f<0x12A>(score)), see(dpp_f<0x12B>(score)), see(dpp_f<0x12C>(score));
+    see(dpp_f<0x12D>(score)), see(dpp_f<0x12E>(score)), see(dpp_f<0x12F>(score));
+    const bool on = before < a.kept * LG;
+    // equal scores at the border leave more than the groups to keep
+    ok &= __popc((uint32_t)(__ballot(on) >> (lane & 48)) & 0xffffu) == a.kept * LG;
+    const float in = row_min(on ? score : INFINITY), out = row_max(on ? -INFINITY : score);
+    const float all = row_max(size);
+    // each score has the errors of two values; their sum's rounding is within the 0x1.1
+    ok &= wide((in - out) * 0.5f, all, biased ? top : all);
+    if (!on) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = 0;
+    }
+  }
+  int id = -1;
+  float last = 0.0f;
+#pragma unroll 1
+  for (int j = 0; j <= a.k; ++j) {
+    uint32_t mine = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine = max(mine, key[v]);
+    const uint32_t best = row_reduce(mine, [](uint32_t p, uint32_t q) { return max(p, q); });
+    const float value = key_value(best);
+    if (best == 0) {
+      ok &= j == a.k;  // a slot without an expert
+      break;
+    }
+    if (j > 0) ok &= wide(last - value, last, value);
+    last = value;
+    if (j == a.k) break;
+    const uint32_t holders = (uint32_t)(__ballot(mine == best) >> (lane & 48)) & 0xffffu;
+    ok &= (holders & (holders - 1)) == 0;  // equal keys of several lanes leave together
+    const int at = (__ffs(holders) - 1) * V + 15 - (int)(best & 15u);
+    if (l == j) id = at;
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
+  }
+  float zs = id >= 0 ? row[id] : -INFINITY;
+  bool bad = false;
+  if (__any(live && !ok)) {
+    int id64;
+    float zs64;
+    select64<V, SOFT>(a, row, l, live, keys64 + threadIdx.x, id64, zs64, bad);
+    if (!ok) id = id64, zs = zs64;
+  }
+  if (!live) id = -1;
+  // Weights in fp32, by one formula whatever path has selected: a few roundings each (36
+  // at most, and those of arguments).
+  const bool slot = l < a.k && id >= 0;
+  float x;
+  if (a.norm) {
+    const float m = row_max(slot ? zs : -INFINITY);
+    x = slot ? relative_score<SOFT, float>(zs, m) : 0.0f;
+    const float sum = row_sum(x);
+    x = slot ? x / sum * (float)a.scale : 0.0f;
+  } else {
+    x = SOFT ? expf(zs - hi) * inv : relative_score<false, float>(zs, 0.0f);
+    x = slot ? x * (float)a.scale : 0.0f;
+  }
+  if (bad && live) x = NAN;
+  if (l < a.k && t < a.T) {
+    a.ids[r * a.k + l] = id;
+    a.w[r * a.k + l] = x;
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Gradient to the logits. A wave a token: lane j < k holds slot j, lane l the
 // columns l + 64 v. With d_j the gradient of slot j's weight and r_j = s_j / sum of the
 // selected scores:
@@ -250,7 +561,7 @@ __global__ __launch_bounds__(kTokens* kWave) void route_backward_kernel(const fl
       r = sum != 0.0f ? r / sum : 0.0f;  // no slot has an expert, or they are -inf
       x -= sum_slots(slot ? r * x : 0.0f);
     } else {
-      r = slot ? 1.0f / (1.0f + expf(-zs)) : 0.0f;
+      r = slot ? relative_score<false, float>(zs, 0.0f) : 0.0f;
     }
     const float rest = SOFT ? 1.0f : 1.0f / (1.0f + expf(zs));
     val = slot ? scale * r * x * rest : 0.0f;
@@ -279,12 +590,46 @@ __global__ __launch_bounds__(kTokens* kWave) void route_backward_kernel(const fl
 // Tokens of a launch: its threads stay below 2^32.
 constexpr int kLaunchTokens = 1 << 24;
 
+// Experts of a lane in route_rows_kernel, or 0 where it does not apply: without groups any
+// count, with groups one that makes them 1, 2, 4 or 8 whole lanes.
+static int lane_experts(int E, int groups) {
+  for (int V : {1, 2, 4, 8, 10, 12, 16})
+    if (groups == 1 ? 16 * V >= E : 16 * V == E && 16 % groups == 0) return V;
+  return 0;
+}
+
 hipError_t launch_route(const float* z, const float* bias, const uint8_t* mask, int T, int E, int k, bool softmax,
                         int groups, int kept, bool norm, double scale, int32_t* ids, float* w, hipStream_t s) {
   if (kept >= groups) groups = kept = 1;  // every group is kept
   for (int t0 = 0; t0 < T;) {
     const int n = std::min(T - t0, kLaunchTokens);
     const dim3 grid((unsigned)((n - 1) / kTokens + 1)), block(kTokens * kWave);
+    const int V = lane_experts(E, groups);
+    if (V > 0) {
+      const RouteArgs a{z + (size_t)t0 * E, bias, mask ? mask + t0 : nullptr, n, E, k, groups, kept, norm ? 1 : 0, scale,
+                        ids + (size_t)t0 * k, w + (size_t)t0 * k};
+      const unsigned blocks = (unsigned)((n - 1) / 16 + 1);
+      auto rows = [&](auto vv) {
+        constexpr int W = decltype(vv)::value;
+        if (softmax)
+          route_rows_kernel<W, true><<<blocks, 256, 0, s>>>(a);
+        else
+          route_rows_kernel<W, false><<<blocks, 256, 0, s>>>(a);
+      };
+      switch (V) {
+        case 1: rows(std::integral_constant<int, 1>{}); break;
+        case 2: rows(std::integral_constant<int, 2>{}); break;
+        case 4: rows(std::integral_constant<int, 4>{}); break;
+        case 8: rows(std::integral_constant<int, 8>{}); break;
+        case 10: rows(std::integral_constant<int, 10>{}); break;
+        case 12: rows(std::integral_constant<int, 12>{}); break;
+        default: rows(std::integral_constant<int, 16>{}); break;
+      }
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      t0 += n;
+      continue;
+    }
     auto go = [&](auto kernel) {
       kernel<<<grid, block, 0, s>>>(z + (size_t)t0 * E, bias, mask ? mask + t0 : nullptr, n, E, k, groups, kept,
                                     norm ? 1 : 0, scale, ids + (size_t)t0 * k, w + (size_t)t0 * k);
