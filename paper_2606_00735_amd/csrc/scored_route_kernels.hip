@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "common.hpp"
 #include "launch.hpp"
@@ -189,13 +190,18 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 //
 // The selection runs on 32-bit keys: c in fp32 (an exponential and a reciprocal of 1 ulp),
 // mapped to integers in the same order, the lowest 4 bits replaced by the position in the
-// lane, so that a round is a maximum over the lane's keys and four DPP maxima. What fp32
-// cannot decide is seen from the gaps: the k + 1 best have to be further apart, and the
-// last group kept from the first one left out, than twice what their keys can be off
-// (`wide`); a wave with a token where they are not (about one in fifty of a batch of
-// normal logits) and one with a NaN, an infinite score or a slot without an expert selects
-// again in 64 bits. 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64
-// bits, a wave each.
+// lane. A lane sorts its keys once; a round is then a maximum of the lanes' first ones (four
+// DPP steps), and the lane that had it moves its keys up.
+//
+// What fp32 cannot decide is seen from the gaps (`wide`: more than twice what a key can be
+// off). Rounds go on until the next key is certainly below the k-th best, so that the k
+// best are among the candidates; where a gap between candidates is not wide, their c's are
+// computed in 64 bits, two a lane, and ordered by rank. So are the groups' scores where the
+// border of the kept ones is not certain. Only a token with more than 32 candidates, three
+// c's of a lane alike at that border, a NaN or an infinite score selects again from all its
+// experts in 64 bits.
+// 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64 bits, a wave each;
+// 37 us without the sort and with all uncertain rows done again.
 // ---------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
@@ -236,6 +242,12 @@ __device__ __forceinline__ double row_sum64(double x) {
   return x;
 }
 
+// f(std::integral_constant<int, q>) for every q of the sequence
+template <class F, int... Q>
+__device__ __forceinline__ void for_each_int(F&& f, std::integer_sequence<int, Q...>) {
+  (f(std::integral_constant<int, Q>{}), ...);
+}
+
 // fp32 in the order of unsigned integers; 0 is below every number
 __device__ __forceinline__ uint32_t order_key(float c) {
   const uint32_t u = __float_as_uint(c);
@@ -259,6 +271,31 @@ struct RouteArgs {
   int32_t* ids;
   float* w;
 };
+
+// Sorts V keys of a lane, the largest first (odd-even merges, the size rounded up to a
+// power of two with zeros that the compiler drops).
+template <int V>
+__device__ __forceinline__ void sort_keys(uint32_t (&key)[V]) {
+  constexpr int P = V <= 1 ? 1 : V <= 2 ? 2 : V <= 4 ? 4 : V <= 8 ? 8 : 16;
+  uint32_t x[P];
+#pragma unroll
+  for (int v = 0; v < P; ++v) x[v] = v < V ? key[v % V] : 0u;
+#pragma unroll
+  for (int p = 1; p < P; p *= 2)
+#pragma unroll
+    for (int d = p; d >= 1; d /= 2)
+#pragma unroll
+      for (int j = d % p; j + d < P; j += 2 * d)
+#pragma unroll
+        for (int i = 0; i < d; ++i)
+          if (i + j + d < P && (i + j) / (2 * p) == (i + j + d) / (2 * p)) {
+            const uint32_t a = x[i + j], b = x[i + j + d];
+            x[i + j] = max(a, b);
+            x[i + j + d] = min(a, b);
+          }
+#pragma unroll
+  for (int v = 0; v < V; ++v) key[v] = x[v];
+}
 
 // The selection of a token in 64 bits: this lane's slot (lane l: slot l) in id and its
 // logit in zsel; bad: the row has a NaN or an infinite score. All 64 lanes call it, tokens of their own every 16. Keys
@@ -370,6 +407,20 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
   }
   const bool live = a.mask == nullptr || a.mask[r] != 0;
   const bool biased = a.bias != nullptr;
+  float bias[V];
+  if (biased) {
+    if (V % 4 == 0 && E % 4 == 0 && (reinterpret_cast<uintptr_t>(a.bias) & 15u) == 0) {
+#pragma unroll
+      for (int v = 0; v < V / 4; ++v) {
+        float4 q = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (e0 + 4 * v < E) q = *reinterpret_cast<const float4*>(a.bias + e0 + 4 * v);
+        bias[4 * v % V] = q.x, bias[(4 * v + 1) % V] = q.y, bias[(4 * v + 2) % V] = q.z, bias[(4 * v + 3) % V] = q.w;
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) bias[v] = e0 + v < E ? a.bias[e0 + v] : 0.0f;
+    }
+  }
   // range of the row's finite logits; ok: no NaN, no +inf
   float hi = -INFINITY, lo = INFINITY;
   bool ok = true;
@@ -380,6 +431,7 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     lo = fminf(lo, z[v] > -INFINITY ? z[v] : INFINITY);
   }
   hi = row_max(hi), lo = row_min(lo);
+  ok = ((uint32_t)(__ballot(ok) >> (lane & 48)) & 0xffffu) == 0xffffu;  // of the row, as all that is and-ed to it below
   // What a score can be off, relative to it. sigmoid: the argument of the exponential (its
   // product with log2 e, 1.5 2^-24 of it), 1 ulp each of exponential and reciprocal, a sum.
   // softmax: a difference in the argument, too, and a sum of up to 20 steps.
@@ -398,7 +450,7 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float c = SOFT ? exp_fast(z[v] - hi) * inv : __builtin_amdgcn_rcpf(1.0f + exp_fast(-z[v]));
-    if (biased) c += e0 + v < E ? a.bias[e0 + v] : 0.0f;
+    if (biased) c += bias[v];
     key[v] = z[v] > -INFINITY && c > -INFINITY ? (order_key(c) & ~15u) | (uint32_t)(15 - v) : 0u;
   }
   // twice what two keys' values, at most x and at most y in size, can differ by from
@@ -407,13 +459,29 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     const float size = fmaxf(fabsf(x), fabsf(y));
     return gap > 2.0f * (size * 0x1.1p-19f + rel * (biased ? top : size)) + 0x1p-120f;
   };
-  if (a.groups > 1) {
-    uint32_t x = 0, y = 0;
-#pragma unroll
+  sort_keys<V>(key);
+  // c of an expert in 64 bits. A softmax's sum counts beside a bias only.
+  double total = 1.0;
+  bool have_total = false;
+  auto exact = [&](int e) {
+    const double zd = (double)row[e];
+    const double sc = SOFT ? exp(zd - (double)hi) / total : 1.0 / (1.0 + exp(-zd));
+    return biased ? sc + (double)a.bias[e] : sc;
+  };
+  auto sum_scores = [&] {
+    if (!SOFT || have_total) return;
+    have_total = true;
+    total = 0.0;
+#pragma unroll 1
     for (int v = 0; v < V; ++v) {
-      y = max(y, min(x, key[v]));
-      x = max(x, key[v]);
+      const float zv = e0 + v < E ? row[e0 + v] : -INFINITY;
+      total += zv > -INFINITY ? exp((double)zv - (double)hi) : 0.0;
     }
+    total = row_sum64(total);
+  };
+  auto expert_of = [&](uint32_t k) { return e0 + 15 - (int)(k & 15u); };
+  if (a.groups > 1) {
+    uint32_t x = key[0], y = V > 1 ? key[1 % V] : 0u;  // the two largest of the group
     const int LG = 16 / a.groups;
     auto join = [&](uint32_t ox, uint32_t oy) {
       y = max(min(x, ox), max(y, oy));
@@ -430,41 +498,116 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     see(dpp_f<0x125>(score)), see(dpp_f<0x126>(score)), see(dpp_f<0x127>(score)), see(dpp_f<0x128>(score));
     see(dpp_f<0x129>(score)), see(dpp_f<0x12A>(score)), see(dpp_f<0x12B>(score)), see(dpp_f<0x12C>(score));
     see(dpp_f<0x12D>(score)), see(dpp_f<0x12E>(score)), see(dpp_f<0x12F>(score));
-    const bool on = before < a.kept * LG;
-    // equal scores at the border leave more than the groups to keep
-    ok &= __popc((uint32_t)(__ballot(on) >> (lane & 48)) & 0xffffu) == a.kept * LG;
+    // a group with nothing to select is not kept
+    bool on = x != 0 && before < a.kept * LG;
+    const int many = __popc((uint32_t)(__ballot(on) >> (lane & 48)) & 0xffffu);
     const float in = row_min(on ? score : INFINITY), out = row_max(on ? -INFINITY : score);
     const float all = row_max(size);
-    // each score has the errors of two values; their sum's rounding is within the 0x1.1
-    ok &= wide((in - out) * 0.5f, all, biased ? top : all);
+    // Each score has the errors of two values (their sum's rounding is within the 0x1.1).
+    // More lanes than those of the groups to keep: equal scores at the border.
+    const bool sure = many <= a.kept * LG && (out == -INFINITY || wide((in - out) * 0.5f, all, all));
+    if (__any(live && !sure)) {
+      // the scores in 64 bits, of a lane's two largest c's: they are among its three
+      // largest keys where the fourth is certainly below the second
+      if (biased || SOFT) sum_scores();
+      const double ninf = -INFINITY;
+      double p = ninf, q = ninf;
+#pragma unroll
+      for (int v = 0; v < (V < 3 ? V : 3); ++v) {
+        const double c = key[v] ? exact(expert_of(key[v])) : ninf;
+        q = fmax(q, fmin(p, c));
+        p = fmax(p, c);
+      }
+      if (V > 3) {
+        const float second = key_value(key[1 % V]), fourth = key_value(key[3 % V]);
+        const bool clear = key[3 % V] == 0 || wide(second - fourth, second, fourth);
+        const bool clears = row_max(clear ? 0.0f : 1.0f) == 0.0f;
+        ok &= sure || clears;
+      }
+#pragma unroll 1
+      for (int d = 1; d < LG; d <<= 1) {
+        const double op = shfl_xor_f64(p, d), oq = shfl_xor_f64(q, d);
+        q = fmax(fmin(p, op), fmax(q, oq));
+        p = fmax(p, op);
+      }
+      const double mine = q > ninf ? p + q : p;
+      int first = 0;  // lanes of groups that come before this one
+#pragma unroll
+      for (int d = 1; d < 16; ++d) {
+        const double other = shfl_xor_f64(mine, d);
+        first += other > mine || (other == mine && (l ^ d) / LG < l / LG);
+      }
+      if (!sure) on = x != 0 && first < a.kept * LG;
+    }
     if (!on) {
 #pragma unroll
       for (int v = 0; v < V; ++v) key[v] = 0;
     }
   }
-  int id = -1;
-  float last = 0.0f;
+  int id = -1, id2 = -1;  // candidates l and 16 + l
+  float last = 0.0f, kth = 0.0f;
+  bool near = false;  // a gap between candidates is not wide
 #pragma unroll 1
-  for (int j = 0; j <= a.k; ++j) {
-    uint32_t mine = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) mine = max(mine, key[v]);
-    const uint32_t best = row_reduce(mine, [](uint32_t p, uint32_t q) { return max(p, q); });
+  for (int j = 0;; ++j) {
+    const uint32_t best = row_reduce(key[0], [](uint32_t p, uint32_t q) { return max(p, q); });
     const float value = key_value(best);
-    if (best == 0) {
-      ok &= j == a.k;  // a slot without an expert
+    if (best == 0 || (j >= a.k && wide(kth - value, kth, value))) break;
+    if (j == 32) {
+      ok = false;
       break;
     }
-    if (j > 0) ok &= wide(last - value, last, value);
+    near |= j > 0 && !wide(last - value, last, value);
     last = value;
-    if (j == a.k) break;
-    const uint32_t holders = (uint32_t)(__ballot(mine == best) >> (lane & 48)) & 0xffffu;
-    ok &= (holders & (holders - 1)) == 0;  // equal keys of several lanes leave together
-    const int at = (__ffs(holders) - 1) * V + 15 - (int)(best & 15u);
-    if (l == j) id = at;
+    if (j == a.k - 1) kth = value;
+    // of equal keys of several lanes, the lowest lane's
+    const int holder = __ffs((uint32_t)(__ballot(key[0] == best) >> (lane & 48)) & 0xffffu) - 1;
+    const int e = holder * V + 15 - (int)(best & 15u);
+    if (l == j) id = e;
+    if (l + 16 == j) id2 = e;
+    if (l == holder) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
+      for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+      key[V - 1] = 0;
+    }
   }
+  if (__any(live && near && ok)) {
+    if (biased) sum_scores();
+    const double c = id >= 0 ? exact(id) : -INFINITY;
+    if (!__any(id2 >= 0)) {
+      int rank = 0;
+      auto see = [&](auto step) {
+        constexpr int C = 0x121 + decltype(step)::value;  // row_ror by 1 to 15
+        const uint64_t u = (uint64_t)__double_as_longlong(c);
+        const uint64_t o = (uint64_t)dpp_u32<C>((uint32_t)u) | ((uint64_t)dpp_u32<C>((uint32_t)(u >> 32)) << 32);
+        const double oc = __longlong_as_double((long long)o);
+        const int oid = (int)dpp_u32<C>((uint32_t)id);
+        rank += oc > c || (oc == c && oid < id);
+      };
+      for_each_int(see, std::make_integer_sequence<int, 15>{});
+      if (id < 0) rank = l;  // lanes without a candidate stay behind the others
+      id = __builtin_amdgcn_ds_permute(((lane & 48) + rank) * 4, id);
+    } else {
+      const double c2 = id2 >= 0 ? exact(id2) : -INFINITY;
+      int rank = 0, rank2 = 0;
+#pragma unroll 1
+      for (int q = 0; q < 16; ++q) {
+        const double oc = shfl_xor_f64(c, q), oc2 = shfl_xor_f64(c2, q);
+        const int oid = __shfl_xor(id, q, kWave), oid2 = __shfl_xor(id2, q, kWave);
+        rank += (oc > c || (oc == c && oid < id)) + (oc2 > c || (oc2 == c && oid2 < id));
+        rank2 += (oc > c2 || (oc == c2 && oid < id2)) + (oc2 > c2 || (oc2 == c2 && oid2 < id2));
+      }
+      int put = -1;  // the lane of a place looks for its candidate
+#pragma unroll 1
+      for (int q = 0; q < 16; ++q) {
+        const int orank = __shfl_xor(rank, q, kWave), orank2 = __shfl_xor(rank2, q, kWave);
+        const int oid = __shfl_xor(id, q, kWave), oid2 = __shfl_xor(id2, q, kWave);
+        if (oid >= 0 && orank == l) put = oid;
+        if (oid2 >= 0 && orank2 == l) put = oid2;
+      }
+      id = put;
+    }
+  }
+  if (l >= a.k) id = -1;
   float zs = id >= 0 ? row[id] : -INFINITY;
   bool bad = false;
   if (__any(live && !ok)) {
@@ -495,92 +638,128 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Gradient to the logits. A wave a token: lane j < k holds slot j, lane l the
-// columns l + 64 v. With d_j the gradient of slot j's weight and r_j = s_j / sum of the
-// selected scores:
+// Gradient to the logits. Sixteen lanes a token: lane j < k holds slot j, lane l the
+// columns 64 q + 4 l .. + 3. With d_j the gradient of slot j's weight and r_j = s_j / sum of
+// the selected scores:
 //   sigmoid:           dz_e = sum over slots of e of  scale d_j s_j (1 - s_j)
 //   sigmoid, normed:   ... scale r_j (d_j - sum_i r_i d_i) (1 - s_j)
 //   softmax, normed:   ... scale r_j (d_j - sum_i r_i d_i)   (the softmax's own sum cancels)
 //   softmax:           dz_e = s_e (scale sum over slots of e of d_j - scale sum_i s_i d_i)
-// Only the last reads logits that were not selected.
+// Only the last reads logits that were not selected. The slots' values reach their columns
+// through a row of zeros in LDS (slots of the same expert are added up first, in their
+// order), which leaves as whole lines. The row of zeros is what it costs: 16384 x 256, 17
+// MB, a wave a token with a comparison of every slot with every column 9.8 us.
 // ---------------------------------------------------------------------------
-template <int V, bool SOFT, bool NORM>
-__global__ __launch_bounds__(kTokens* kWave) void route_backward_kernel(const float* __restrict__ z,
-                                                                        const int32_t* __restrict__ ids,
-                                                                        const float* __restrict__ dw, int T, int E,
-                                                                        int k, float scale, int accumulate,
-                                                                        float* __restrict__ dz) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long t = (long long)blockIdx.x * kTokens + wave;
-  if (t >= T) return;
-  const size_t row = (size_t)t;
-  auto sum_slots = [&](float x) {
+template <int Q, bool SOFT, bool NORM>
+__global__ __launch_bounds__(256) void route_backward_kernel(const float* __restrict__ z,
+                                                             const int32_t* __restrict__ ids,
+                                                             const float* __restrict__ dw, int T, int E, int k,
+                                                             float scale, int accumulate, float* __restrict__ dz) {
+  __shared__ __align__(16) float rows[16][64 * Q];
+  const int l = threadIdx.x & 15, tok = threadIdx.x >> 4;
+  const long long t = (long long)blockIdx.x * 16 + tok;
+  const bool in = t < T;
+  const size_t row = (size_t)(in ? t : T - 1);  // lanes past the last token repeat it and store nothing
+  const bool vec = E % 4 == 0;
+  float4* mine = reinterpret_cast<float4*>(rows[tok]);
 #pragma unroll
-    for (int m = 1; m < kMaxTopk; m <<= 1) x += __shfl_xor(x, m, kWave);
-    return __shfl(x, 0, kWave);
-  };
-  int id = lane < k ? ids[row * k + lane] : -1;
-  const float d = lane < k ? dw[row * k + lane] : 0.0f;
+  for (int q = 0; q < Q; ++q) mine[16 * q + l] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  int id = l < k ? ids[row * k + l] : -1;
+  const float d = l < k ? dw[row * k + l] : 0.0f;
   const bool slot = id >= 0 && id < E;
   if (!slot) id = -1;
   const float zs = slot ? z[row * E + id] : -INFINITY;
-  float p[V] = {};
-  float val;  // what slot j adds to its expert's column
-  float common = 0.0f;
+  float p[Q][4] = {};
+  float val, common = 0.0f;  // what slot l adds to its expert's column
   if (SOFT && !NORM) {
     float m = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int e = lane + 64 * v;
-      p[v] = e < E ? z[row * E + e] : -INFINITY;
-      m = fmaxf(m, p[v]);
+    for (int q = 0; q < Q; ++q) {
+      const int e = 64 * q + 4 * l;
+      float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      const float* pz = z + row * E + e;
+      if (vec) {
+        if (e < E) v = *reinterpret_cast<const float4*>(pz);
+      } else {
+        if (e < E) v.x = pz[0];
+        if (e + 1 < E) v.y = pz[1];
+        if (e + 2 < E) v.z = pz[2];
+        if (e + 3 < E) v.w = pz[3];
+      }
+      p[q][0] = v.x, p[q][1] = v.y, p[q][2] = v.z, p[q][3] = v.w;
+      m = fmaxf(m, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
     }
+    m = row_max(m);
 #pragma unroll
-    for (int q = 1; q < kWave; q <<= 1) m = fmaxf(m, __shfl_xor(m, q, kWave));
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      p[v] = m > -INFINITY ? expf(p[v] - m) : 0.0f;
-      sum += p[v];
-    }
-#pragma unroll
-    for (int q = 1; q < kWave; q <<= 1) sum += __shfl_xor(sum, q, kWave);
+      for (int c = 0; c < 4; ++c) {
+        p[q][c] = m > -INFINITY ? expf(p[q][c] - m) : 0.0f;
+        sum += p[q][c];
+      }
+    sum = row_sum(sum);
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] *= inv;
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) p[q][c] *= inv;
     const float ps = slot && m > -INFINITY ? expf(zs - m) * inv : 0.0f;
     val = slot ? scale * d : 0.0f;
-    common = sum_slots(slot ? val * ps : 0.0f);
+    common = row_sum(slot ? val * ps : 0.0f);
   } else {
     float r, x = slot ? d : 0.0f;
     if (NORM) {
-      float m = zs;
-#pragma unroll
-      for (int q = 1; q < kMaxTopk; q <<= 1) m = fmaxf(m, __shfl_xor(m, q, kWave));
+      const float m = row_max(zs);
       r = slot && m > -INFINITY ? relative_score<SOFT, float>(zs, m) : 0.0f;
-      const float sum = sum_slots(r);
+      const float sum = row_sum(r);
       r = sum != 0.0f ? r / sum : 0.0f;  // no slot has an expert, or they are -inf
-      x -= sum_slots(slot ? r * x : 0.0f);
+      x -= row_sum(slot ? r * x : 0.0f);
     } else {
       r = slot ? relative_score<false, float>(zs, 0.0f) : 0.0f;
     }
     const float rest = SOFT ? 1.0f : 1.0f / (1.0f + expf(zs));
     val = slot ? scale * r * x * rest : 0.0f;
   }
-  float out[V] = {};
-  for (int j = 0; j < k; ++j) {
-    const int e = __shfl(id, j, kWave);
-    const float a = __shfl(val, j, kWave);
+  // slots of one expert: the first of them has their sum, in their order
+  float total = 0.0f;
+  bool first = slot;
+  for_each_int(
+      [&](auto j) {
+        constexpr int J = decltype(j)::value;
+        const int oid = (int)dpp_u32<0x150 + J>((uint32_t)id);  // row_newbcast
+        const float ov = dpp_f<0x150 + J>(val);
+        if (oid == id) {
+          total += ov;
+          first &= J >= l;
+        }
+      },
+      std::make_integer_sequence<int, kMaxTopk>{});
+  if (first) rows[tok][id] = total;
+  // a wave reads what it has written; LDS serves a wave in order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (!in) return;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (lane + 64 * v == e) out[v] += a;
-  }
+  for (int q = 0; q < Q; ++q) {
+    const int e = 64 * q + 4 * l;
+    const float4 f = mine[16 * q + l];
+    float v[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int e = lane + 64 * v;
-    if (e < E) {
-      float x = SOFT && !NORM ? p[v] * (out[v] - common) : out[v];
-      if (accumulate) x += dz[row * E + e];
-      dz[row * E + e] = x;
+    for (int c = 0; c < 4; ++c)
+      if (SOFT && !NORM) v[c] = p[q][c] * (v[c] - common);
+    float* out = dz + row * E + e;
+    if (vec) {
+      if (e < E) {
+        if (accumulate) {
+          const float4 o = *reinterpret_cast<const float4*>(out);
+          v[0] += o.x, v[1] += o.y, v[2] += o.z, v[3] += o.w;
+        }
+        *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (e + c < E) out[c] = accumulate ? out[c] + v[c] : v[c];
     }
   }
 }
@@ -651,9 +830,9 @@ hipError_t launch_route_backward(const float* z, const int32_t* ids, const float
                                  bool softmax, bool norm, float scale, bool accumulate, float* dz, hipStream_t s) {
   for (int t0 = 0; t0 < T;) {
     const int n = std::min(T - t0, kLaunchTokens);
-    const dim3 grid((unsigned)((n - 1) / kTokens + 1)), block(kTokens * kWave);
+    const unsigned blocks = (unsigned)((n - 1) / 16 + 1);
     auto go = [&](auto kernel) {
-      kernel<<<grid, block, 0, s>>>(z + (size_t)t0 * E, ids + (size_t)t0 * k, dw + (size_t)t0 * k, n, E, k, scale,
+      kernel<<<blocks, 256, 0, s>>>(z + (size_t)t0 * E, ids + (size_t)t0 * k, dw + (size_t)t0 * k, n, E, k, scale,
                                     accumulate ? 1 : 0, dz + (size_t)t0 * E);
     };
     auto kind = [&](auto vv) {
