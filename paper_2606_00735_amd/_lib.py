@@ -716,19 +716,21 @@ def _size_ref(n):
 
 
 def _weight(w, name, dtype, dev):
-    """(pointer, row stride) of a weight matrix [N, K] whose rows may be padded."""
+    """(pointer, rows, columns, row stride) of a weight matrix [N, K] whose rows may be padded."""
     if not isinstance(w, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if w.get_device() != dev:
         raise ValueError(f"{name} must be on the current GPU, cuda:{dev} (libmoe has no CPU path)")
-    if w.dtype != dtype or w.dim() != 2:
+    shape = w.shape
+    if w.dtype is not dtype or len(shape) != 2:
         raise ValueError(f"{name} must be [N, K] of {dtype}")
+    N, K = shape
     sr, sk = w.stride()
-    if w.shape[0] == 1:
-        sr = w.shape[1]
-    if sk != 1 or sr < w.shape[1]:
-        raise ValueError(f"{name} must have unit element stride and rows at least {w.shape[1]} apart")
-    return w.data_ptr(), sr
+    if N == 1:
+        sr = K
+    if sk != 1 or sr < K:
+        raise ValueError(f"{name} must have unit element stride and rows at least {K} apart")
+    return w.data_ptr(), N, K, sr
 
 
 def _matrix(t, name):
@@ -813,15 +815,15 @@ def moe_linear(x, w, bias=None, act="none", mul=None, residual=None, z=None, out
     bias, which moe_linear_backward needs of a layer with an activation. out may be mul or
     residual. ws: linear_ws_bytes bytes, allocated if missing."""
     L = load_library()
-    M, K = _matrix(x, "x")
-    N = _matrix(w, "w")[0]
+    shape = _matrix(x, "x")
+    M, K = shape
     dt, dtype = _dtype_code(x), x.dtype
     dev = torch.cuda.current_device()
     code = _code(ACTS, act, "act")
-    if w.shape[1] != K:
+    xp = _on(x, "x", dtype, dev, shape)
+    wp, N, wk, ldw = _weight(w, "w", dtype, dev)
+    if wk != K:
         raise ValueError(f"w must be [N, {K}], got {list(w.shape)}")
-    xp = _on(x, "x", dtype, dev, (M, K))
-    wp, ldw = _weight(w, "w", dtype, dev)
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=x.device)
     ws, wsp, wsn = _workspace(ws, linear_ws_bytes(M, N, K, dtype) if ws is None else 0, dev, x.device)
@@ -848,10 +850,10 @@ def moe_linear_backward(dy, x, w, z=None, act="none", mul=None, need_dx=True, ne
     code = _code(ACTS, act, "act")
     if dw_dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("dw_dtype must be torch.float32 or torch.bfloat16")
-    if _matrix(w, "w") != (N, K):
-        raise ValueError(f"w must be {[N, K]}, got {list(w.shape)}")
     dyp, xp = _on(dy, "dy", dtype, dev, (M, N)), _on(x, "x", dtype, dev, (M, K))
-    wp, ldw = _weight(w, "w", dtype, dev)
+    wp, wn, wk, ldw = _weight(w, "w", dtype, dev)
+    if wn != N or wk != K:
+        raise ValueError(f"w must be {[N, K]}, got {list(w.shape)}")
 
     def out(t, shape, kind, name):
         t = torch.empty(shape, dtype=kind, device=dy.device) if t is None else t
