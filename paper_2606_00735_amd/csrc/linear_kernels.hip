@@ -198,16 +198,18 @@ struct Panel {
     dma16a(uniform_ptr(base + (live ? (size_t)kc * step : 0)), off[t] & msk, lds + (uint32_t)((t * W + wave) * 1024));
   }
   // the last, partial chunk (n of 64): through registers, zeros past the end
-  __device__ __forceinline__ void load_tail(int kc, int n, char* lds, int wave, int lane) const {
+  __device__ __forceinline__ void load_tail(int kc, int n, u32x4_t (&v)[LOADS], int wave, int lane) const {
     const char* p = base + (size_t)kc * step;
 #pragma unroll
     for (int t = 0; t < LOADS; ++t) {
       const int r = (t * W + wave) * RPI + lane / PP;
       const bool in = TR ? r < n : swz_chunk<kChunk>(r, lane % PP) * 8 < n;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (in) v = *reinterpret_cast<const uint4*>(p + off[t]);
-      *reinterpret_cast<uint4*>(lds + (t * W + wave) * 1024 + lane * 16) = v;
+      v[t] = in ? *reinterpret_cast<const u32x4_t*>(p + off[t]) : u32x4_t{};
     }
+  }
+  __device__ __forceinline__ void store_tail(const u32x4_t (&v)[LOADS], char* lds, int wave, int lane) const {
+#pragma unroll
+    for (int t = 0; t < LOADS; ++t) *reinterpret_cast<u32x4_t*>(lds + (t * W + wave) * 1024 + lane * 16) = v[t];
   }
   // fragment of k-step s for rows [r0, r0 + 32): lane (r = lane % 32, h = lane / 32)
   // holds k = 16 s + 8 h + (0..7) of row r0 + r
@@ -318,21 +320,28 @@ __device__ __forceinline__ TileAt tile_at(unsigned b, unsigned total, int mts, i
 }
 
 // ---------------------------------------------------------------------------
-// BM x BN tile, WM_ x WN_ waves, NS chunks in LDS by direct loads (pipeline_xk).
+// BM x BN tile, WR x WC waves, NS chunks in LDS by direct loads (pipeline_xk).
 // ---------------------------------------------------------------------------
+template <int BM, int BN, int WR, int WC, int NS>
+struct TileShape {
+  static constexpr int W = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+  static constexpr int STAGE = (BM + BN) * kChunk * 2;
+  static constexpr int OUT = (MI > 1 ? 2 : 1) * 32 * WN * 4;  // of a wave (finish_stripes)
+  static constexpr int LDS = STAGE * NS > W * OUT ? STAGE * NS : W * OUT;
+};
+
 template <int BM, int BN, int WR, int WC, int NS, bool TA, bool TB, int ACT>
-__global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
-  constexpr int W = WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+__device__ __forceinline__ void linear_tile(const LinArgs& a, unsigned block, unsigned blocks, bf16_t* smem) {
+  using Sh = TileShape<BM, BN, WR, WC, NS>;
+  constexpr int W = Sh::W, WM = Sh::WM, WN = Sh::WN, MI = Sh::MI, NI = Sh::NI;
   using PA = Panel<BM, TA, W>;
   using PB = Panel<BN, TB, W>;
-  constexpr int STAGE = PA::BYTES + PB::BYTES;
-  constexpr int OUT = (MI > 1 ? 2 : 1) * 32 * WN * 4;  // of a wave (finish_stripes)
-  constexpr int LDS = STAGE * NS > W * OUT ? STAGE * NS : W * OUT;
-  __shared__ __align__(16) bf16_t smem[LDS / 2];
+  constexpr int STAGE = Sh::STAGE, OUT = Sh::OUT;
+  static_assert(STAGE == PA::BYTES + PB::BYTES, "stage");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WC, wn = wave % WC;
   const int mts = (a.rows - 1) / BM + 1, nts = (a.cols - 1) / BN + 1;
-  const TileAt at = tile_at(blockIdx.x, gridDim.x, mts, nts);
+  const TileAt at = tile_at(block, blocks, mts, nts);
   const int row0 = uniform_int(at.mt * BM), col0 = uniform_int(at.nt * BN);
   const int chunks = a.red / kChunk;
   const int k0 = uniform_int((int)((long long)at.split * chunks / a.S));
@@ -341,6 +350,13 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
   PB pb;
   pa.init(a.A, a.lda, row0, a.rows - row0, wave, lane);
   pb.init(a.B, a.ldb, col0, a.cols - col0, wave, lane);
+  // the partial chunk's loads leave first and wait in registers
+  const int n = at.split == a.S - 1 ? a.red - chunks * kChunk : 0;
+  u32x4_t ta[PA::LOADS] = {}, tb[PB::LOADS] = {};
+  if (n > 0) {
+    pa.load_tail(chunks, n, ta, wave, lane);
+    pb.load_tail(chunks, n, tb, wave, lane);
+  }
   f32x16_t acc[MI][NI];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
@@ -373,12 +389,12 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
       for (int i = 0; i < MI; ++i)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[buf][j], fa[buf][i], acc[i][j], 0, 0, 0);
   };
-  pipeline_xk<NS, LOADS, KS>(k1 - k0, smem, STAGE / 2, issue, read, mma, [] {});
-  const int n = a.red - chunks * kChunk;
-  if (n > 0 && at.split == a.S - 1) {
+  // (the tail's loads are older than the pipeline's, whose waits therefore hold)
+  pipeline_xk<NS, LOADS, KS, false, false>(k1 - k0, smem, STAGE / 2, issue, read, mma, [] {});
+  if (n > 0) {
     char* p = reinterpret_cast<char*>(smem);
-    pa.load_tail(chunks, n, p, wave, lane);
-    pb.load_tail(chunks, n, p + PA::BYTES, wave, lane);
+    pa.store_tail(ta, p, wave, lane);
+    pb.store_tail(tb, p + PA::BYTES, wave, lane);
     __syncthreads();
     for (int s = 0; s * 16 < n; ++s) {
       read(smem, s, 0);
@@ -396,8 +412,24 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
             put(lane & 31, j * 8 + 2 * g + (lane >> 5),
                 f32x4_t{acc[n][j][4 * g], acc[n][j][4 * g + 1], acc[n][j][4 * g + 2], acc[n][j][4 * g + 3]});
       },
-      [&](int n) { return row0 + wm * WM + n * 32; },
-      [&](int) { return col0 + wn * WN; });
+      [&](int n) { return row0 + wm * WM + n * 32; }, [&](int) { return col0 + wn * WN; });
+}
+
+template <int BM, int BN, int WR, int WC, int NS, bool TA, bool TB, int ACT>
+__global__ __launch_bounds__(WR* WC* kWave) void linear_tile_kernel(LinArgs a) {
+  __shared__ __align__(16) bf16_t smem[TileShape<BM, BN, WR, WC, NS>::LDS / 2];
+  linear_tile<BM, BN, WR, WC, NS, TA, TB, ACT>(a, blockIdx.x, gridDim.x, smem);
+}
+
+// Both products of a gradient in one launch, where neither fills the chip: dx's tiles, then
+// dw's.
+template <int BM, int BN, int WR, int WC, int NS>
+__global__ __launch_bounds__(WR* WC* kWave) void linear_pair_kernel(LinArgs dx, LinArgs dw, unsigned first) {
+  __shared__ __align__(16) bf16_t smem[TileShape<BM, BN, WR, WC, NS>::LDS / 2];
+  if (blockIdx.x < first)
+    linear_tile<BM, BN, WR, WC, NS, false, true, kActNone>(dx, blockIdx.x, first, smem);
+  else
+    linear_tile<BM, BN, WR, WC, NS, true, true, kActNone>(dw, blockIdx.x - first, gridDim.x - first, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -827,8 +859,8 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
 
 // ---------------------------------------------------------------------------
 // dz = dy * mul * act'(z), dmul = dy * act(z), and partial sums of dz's columns (of the
-// fp32 values, before dz is rounded). A block: 256 columns of a range of rows, 8 columns
-// a lane, 8 rows at a time.
+// fp32 values, before dz is rounded). A block: 64 columns (a line in bf16) of a range of
+// rows, 8 columns a lane, 32 rows at a time.
 // ---------------------------------------------------------------------------
 struct ActBackwardArgs {
   const void *dy, *z, *mul;
@@ -839,10 +871,10 @@ struct ActBackwardArgs {
 
 template <bool BF16, int ACT>
 __global__ __launch_bounds__(256) void act_backward_kernel(ActBackwardArgs a) {
-  __shared__ float sums[8][256];
-  const int tid = threadIdx.x, c8 = tid % 32, ry = tid / 32;
+  __shared__ float sums[32][64];
+  const int tid = threadIdx.x, c8 = tid % 8, ry = tid / 8;
   const int cb = (int)(blockIdx.x / (unsigned)a.P), p = (int)(blockIdx.x % (unsigned)a.P);
-  const int col = cb * 256 + c8 * 8;
+  const int col = cb * 64 + c8 * 8;
   const int r0 = (int)((long long)p * a.rows / a.P), r1 = (int)((long long)(p + 1) * a.rows / a.P);
   float db[8] = {};
   auto load = [&](const void* q, size_t at, float (&f)[8]) {
@@ -862,46 +894,65 @@ __global__ __launch_bounds__(256) void act_backward_kernel(ActBackwardArgs a) {
       *reinterpret_cast<float4*>(static_cast<float*>(q) + at + 4) = make_float4(f[4], f[5], f[6], f[7]);
     }
   };
+  // G rows of a lane at a time, their loads in flight together
+  constexpr int G = 4;
   if (col < a.cols) {
-    for (int r = r0 + ry; r < r1; r += 8) {
-      const size_t at = (size_t)r * a.cols + col;
-      float d[8], z[8], m[8];
-      load(a.dy, at, d);
-      if (a.z != nullptr) load(a.z, at, z);
-      if (a.mul != nullptr) load(a.mul, at, m);
-      if (a.dmul != nullptr) {
-        float g[8];
+    for (int r = r0 + ry; r < r1; r += 32 * G) {
+      float d[G][8] = {}, z[G][8] = {}, m[G][8] = {};
 #pragma unroll
-        for (int q = 0; q < 8; ++q) g[q] = d[q] * act_value<ACT>(z[q]);
-        store(a.dmul, at, g);
+      for (int g = 0; g < G; ++g) {
+        const size_t at = (size_t)(r + 32 * g) * (size_t)a.cols + (size_t)col;
+        if (r + 32 * g < r1) {
+          load(a.dy, at, d[g]);
+          if (a.z != nullptr) load(a.z, at, z[g]);
+          if (a.mul != nullptr) load(a.mul, at, m[g]);
+        }
       }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        if (a.mul != nullptr) d[q] *= m[q];
-        if (ACT != kActNone) d[q] *= act_slope<ACT>(z[q]);
-        db[q] += d[q];
+      for (int g = 0; g < G; ++g) {
+        if (r + 32 * g >= r1) break;
+        const size_t at = (size_t)(r + 32 * g) * (size_t)a.cols + (size_t)col;
+        if (a.dmul != nullptr) {
+          float f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] = d[g][q] * act_value<ACT>(z[g][q]);
+          store(a.dmul, at, f);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          if (a.mul != nullptr) d[g][q] *= m[g][q];
+          if (ACT != kActNone) d[g][q] *= act_slope<ACT>(z[g][q]);
+          db[q] += d[g][q];
+        }
+        if (a.dz != nullptr) store(a.dz, at, d[g]);
       }
-      if (a.dz != nullptr) store(a.dz, at, d);
     }
   }
   if (a.db == nullptr) return;
 #pragma unroll
   for (int q = 0; q < 8; ++q) sums[ry][c8 * 8 + q] = db[q];
   __syncthreads();
-  if (cb * 256 + tid < a.cols) {
+  if (tid < 64 && cb * 64 + tid < a.cols) {
     float s = 0.0f;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s += sums[q][tid];
-    a.db[(size_t)p * a.cols + cb * 256 + tid] = s;
+    for (int q = 0; q < 32; ++q) s += sums[q][tid];
+    a.db[(size_t)p * (size_t)a.cols + cb * 64 + tid] = s;
   }
 }
 
-__global__ __launch_bounds__(256) void bias_join_kernel(const float* __restrict__ part, int cols, int P,
-                                                        float* __restrict__ db) {
-  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+// Joins the sums of P ranges, in their order.
+__global__ __launch_bounds__(64) void bias_join_kernel(const float* __restrict__ part, int cols, int P,
+                                                       float* __restrict__ db) {
+  const int c = (int)(blockIdx.x * 64 + threadIdx.x);
   if (c >= cols) return;
   float s = 0.0f;
-  for (int p = 0; p < P; ++p) s += part[(size_t)p * cols + c];
+  for (int p = 0; p < P; p += 8) {  // eight loads in flight
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = p + q < P ? part[(size_t)(p + q) * (size_t)cols + c] : 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += v[q];
+  }
   db[c] = s;
 }
 
@@ -920,20 +971,30 @@ constexpr int kFewRows = 32;
 
 constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 
-// few: the kernel of few rows can run (no operand is transposed)
+// few: the kernel of few rows can run (no operand is transposed).
+// Few rows: its reads of x grow with the rows, the tiles' do not (us, few rows / 64 x 64 tiles:
+// 16 rows of 7168 x 2048 9.6 / 11.9, 16 of 2048 x 7168 14.9 / 15.4, 8 of 14336 x 4096 25.9 /
+// 23.4, 1 21.3 / 23.4, 32 of 768 x 2048 7.5 / 9.0).
+// Tiles: the largest that fill the chip (256 x 256 where three quarters of it: a tile of 128
+// does 0.6 of its rate). 64 x 64 and 128 x 128 tiles of fewer blocks than CUs may cut the
+// reduction in S ranges, by what a chunk of a tile and the join measured: 0.27 and 0.5 us a
+// chunk, 1 us around a tile, 3.5 us a join and its bytes at 3 TB/s.
 LinPlan linear_plan(int rows, int cols, int red, bool few) {
-  if (few && rows <= kFewRows) return {0, 1};
+  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1};
   const long long cus = device_cu_count();
   auto tiles = [&](int t) { return ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1); };
   LinPlan p{tiles(256) >= cus * 3 / 4 ? 256 : tiles(128) >= cus ? 128 : 64, 1};
-  if (p.tile == 256) return p;
   const long long n = tiles(p.tile);
-  const int chunks = red / kChunk;
-  if (n < cus && chunks >= 8) {
-    long long S = std::min({(2 * cus) / n, (long long)chunks / 4, 16LL});
-    const size_t plane = (size_t)rows * (size_t)cols * 4;
-    S = std::min(S, (long long)(kLinPartBytes / plane));
-    p.S = (int)std::max(1LL, S);
+  if (p.tile == 256 || n >= cus) return p;
+  const long long chunks = red / kChunk, plane = (long long)rows * cols * 4;
+  const long long chunk_ns = p.tile == 64 ? 270 : 500;
+  long long best = LLONG_MAX;
+  for (int S = 1; S <= 16; ++S) {
+    if (S > 1 && (chunks / S < 4 || n * S > 2 * cus || plane * S > (long long)kLinPartBytes)) break;
+    // two blocks of a CU take 1.4 times one's time
+    long long ns = ((chunks + S - 1) / S * chunk_ns + 1000) * (n * S <= cus ? 10 : 14) / 10;
+    if (S > 1) ns += 3500 + 2 * S * plane / 3000;
+    if (ns < best) best = ns, p.S = S;
   }
   return p;
 }
@@ -967,8 +1028,15 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
   if (p.tile == 256)
     linear_big_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
-  else if (p.tile == 128)
+  // more blocks than CUs: two to a CU, fewer chunks ahead each (128 x 128, 336 blocks of 64
+  // chunks: 70 -> 53 us; 256 blocks, one to a CU in any case, 78 us so, 68 us with four chunks
+  // and eight waves)
+  else if (p.tile == 128 && tiles <= device_cu_count())
     linear_tile_kernel<128, 128, 2, 4, 4, TA, TB, ACT><<<(unsigned)tiles, 512, 0, s>>>(a);
+  else if (p.tile == 128)
+    linear_tile_kernel<128, 128, 2, 2, 2, TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
+  else if (tiles <= device_cu_count())
+    linear_tile_kernel<64, 64, 2, 2, 8, TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
   else
     linear_tile_kernel<64, 64, 2, 2, 4, TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
@@ -978,10 +1046,11 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Row ranges of the bias' sums: enough blocks for the chip, at least 32 rows each.
+// Row ranges of the bias' sums: enough blocks for the chip, at least 512 rows each (a join
+// is a launch).
 int bias_ranges(int rows, int cols) {
-  const int cb = (cols - 1) / 256 + 1;
-  return std::max(1, std::min((4 * device_cu_count() + cb - 1) / cb, (rows + 31) / 32));
+  const int cb = (cols - 1) / 64 + 1;
+  return std::max(1, std::min((4 * device_cu_count() + cb - 1) / cb, rows / 512));
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -1029,7 +1098,7 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     b.dz = own ? c.dz : nullptr;
     b.rows = c.M, b.cols = c.N, b.P = P;
     b.db = c.dbias == nullptr ? nullptr : P > 1 ? static_cast<float*>(ws) : c.dbias;
-    const unsigned grid = (unsigned)(((c.N - 1) / 256 + 1) * P);
+    const unsigned grid = (unsigned)((c.N - 1) / 64 + 1) * (unsigned)P;
     e = with_act(c.act, [&](auto act) {
       if (c.bf16)
         act_backward_kernel<true, decltype(act)::value><<<grid, 256, 0, s>>>(b);
@@ -1039,28 +1108,34 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     });
     if (e != hipSuccess) return e;
     if (c.dbias != nullptr && P > 1) {
-      bias_join_kernel<<<(unsigned)((c.N + 255) / 256), 256, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
+      bias_join_kernel<<<(unsigned)((c.N + 63) / 64), 64, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
   const void* dz = own ? c.dz : c.dy;
   void* part = static_cast<char*>(ws) + align256((size_t)P * (size_t)c.N * 4);
-  if (c.dx != nullptr) {
-    LinArgs a{};
-    a.A = dz, a.B = c.w, a.lda = c.N, a.ldb = c.ldw;
-    a.rows = c.M, a.cols = c.K, a.red = c.N, a.out = c.dx;
-    if ((e = launch_product<false, true, kActNone>(a, c.bf16, part, s)) != hipSuccess) return e;
+  LinArgs x{}, w{};
+  x.A = dz, x.B = c.w, x.lda = c.N, x.ldb = c.ldw;
+  x.rows = c.M, x.cols = c.K, x.red = c.N, x.out = c.dx;
+  w.A = dz, w.B = c.x, w.lda = c.N, w.ldb = c.K;
+  w.rows = c.N, w.cols = c.K, w.red = c.M;
+  if (c.dw_bf16)
+    w.out = c.dw;
+  else
+    w.out32 = static_cast<float*>(c.dw);
+  if (c.dx != nullptr && c.dw != nullptr && c.bf16) {
+    const LinPlan px = linear_plan(x.rows, x.cols, x.red, false), pw = linear_plan(w.rows, w.cols, w.red, false);
+    if (px.tile == 64 && px.S == 1 && pw.tile == 64 && pw.S == 1) {
+      auto tiles = [](const LinArgs& a) { return (unsigned)(((a.rows - 1) / 64 + 1) * ((a.cols - 1) / 64 + 1)); };
+      x.S = w.S = 1;
+      linear_pair_kernel<64, 64, 2, 2, 4><<<tiles(x) + tiles(w), 256, 0, s>>>(x, w, tiles(x));
+      return hipGetLastError();
+    }
   }
-  if (c.dw != nullptr) {
-    LinArgs a{};
-    a.A = dz, a.B = c.x, a.lda = c.N, a.ldb = c.K;
-    a.rows = c.N, a.cols = c.K, a.red = c.M;
-    if (c.dw_bf16)
-      a.out = c.dw;
-    else
-      a.out32 = static_cast<float*>(c.dw);
-    if ((e = launch_product<true, true, kActNone>(a, c.bf16, part, s)) != hipSuccess) return e;
-  }
+  if (c.dx != nullptr)
+    if ((e = launch_product<false, true, kActNone>(x, c.bf16, part, s)) != hipSuccess) return e;
+  if (c.dw != nullptr)
+    if ((e = launch_product<true, true, kActNone>(w, c.bf16, part, s)) != hipSuccess) return e;
   return e;
 }
 
