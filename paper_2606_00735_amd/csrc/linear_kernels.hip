@@ -93,6 +93,7 @@ struct LinArgs {
   void* z;               // [rows, cols]: the sum with the bias, or null
   void* out;             // of the operands' type, or
   float* out32;          // fp32: the plain sum
+  float* row_sums;       // [2 column tiles][rows]: parts of the sums of A's rows (linear_big_kernel)
 };
 
 __device__ __forceinline__ void unpack8(uint4 v, float (&f)[8]) {
@@ -445,6 +446,11 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_pair_kernel(LinArgs dx, 
 //
 // Either operand may be transposed; its slot is then 64 rows of the reduction by 128 rows
 // of C, its fragments two transposing reads each.
+//
+// SUMS: also the sums of A's rows over the reduction (the bias' gradient, where A is dz),
+// from the fragments. Column tile j of J takes the chunks j, j + J, ..., a wave one of their
+// two k-steps, so a row's sum comes in 2 J parts. A pass over dz for them costs 25 us
+// (8192 x 7168).
 // ---------------------------------------------------------------------------
 constexpr int kSlotBytes = 128 * kChunk * 2;
 
@@ -556,7 +562,7 @@ struct BigOperand {
   }
 };
 
-template <bool TA, bool TB, int ACT>
+template <bool TA, bool TB, int ACT, bool SUMS>
 __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
   __shared__ __align__(16) bf16_t smem[8 * kSlotBytes / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -631,6 +637,34 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
     __builtin_amdgcn_sched_barrier(0);
   };
   auto keep = [] {};
+  float sum[2][4] = {};  // [A half][row block]: of this lane's row, its part of the reduction
+  int sum_at = at.nt;  // the next chunk whose rows this block sums
+  auto add_rows = [&](int h, int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // said differently for either k-step: merged into one piece of code, the choice
+      // would index the fragments, which then were in memory
+      u32x4_t q = __builtin_bit_cast(u32x4_t, fr[h][i][s]);
+      if (s == 0)
+        asm volatile("; k-step 0" : "+v"(q));
+      else
+        asm volatile("; k-step 1" : "+v"(q));
+      float f[8];
+      unpack8(__builtin_bit_cast(uint4, q), f);
+      sum[h][i] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+    }
+  };
+  auto sums_of = [&]([[maybe_unused]] int h, [[maybe_unused]] int c) __attribute__((always_inline)) {
+    if constexpr (SUMS) {
+      if (c == sum_at) {
+        if (wn == 0)
+          add_rows(h, 0);
+        else
+          add_rows(h, 1);
+        if (h == 1) sum_at += nts;
+      }
+    }
+  };
   // -1 if there is a chunk c, else 0: in scalar registers, where a comparison would be
   // widened in vector registers
   auto live = [&](int c) __attribute__((always_inline)) {
@@ -672,16 +706,20 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
     auto even = [&](int c) __attribute__((always_inline)) {
       phase(0, 0, 3, 0, 2, 0, [&]() __attribute__((always_inline)) { B.advance(live(c + 2)); });
       phase(0, 1, 1, 0, 3, 0, keep);
+      sums_of(0, c);
       phase(1, 1, 0, 1, 1, 0, keep);
       phase(1, 0, 3, 1, 0, 1, [&]() __attribute__((always_inline)) { A.advance(live(c + 3)); });
+      sums_of(1, c);
     };
     int c = 0;
     for (; c + 1 < nK; c += 2) {
       even(c);
       phase(0, 1, 2, 1, 3, 1, [&]() __attribute__((always_inline)) { B.advance(live(c + 3)); });
       phase(0, 0, 1, 1, 2, 1, keep);
+      sums_of(0, c + 1);
       phase(1, 0, 0, 0, 1, 1, keep);
       phase(1, 1, 2, 0, 0, 0, [&]() __attribute__((always_inline)) { A.advance(live(c + 4)); });
+      sums_of(1, c + 1);
     }
     if (c < nK) even(c);
     wait_lgkmcnt0();
@@ -712,11 +750,31 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int j = 0; j < 4; ++j) mma(h, b, i, j, q);
+        if (SUMS && at.nt == 0 && wn == q) {
+          if (q == 0)
+            add_rows(0, 0), add_rows(1, 0);
+          else
+            add_rows(0, 1), add_rows(1, 1);
+        }
       }
     }
     __syncthreads();
   }
   settle();
+  if (SUMS) {
+    // the four lanes of a row hold parts of it
+    float* p = a.row_sums + (size_t)(2 * at.nt + wn) * (size_t)a.rows;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = row0 + wm * 128 + h * 64 + i * 16 + (lane & 15);
+        float v = sum[h][i];
+        v += __shfl_xor(v, 16, kWave);
+        v += __shfl_xor(v, 32, kWave);
+        if (lane < 16 && row < a.rows) p[row] = v;
+      }
+  }
   // stripe n: B half n / 4, A half n / 2 % 2, row blocks 2 (n % 2) and the next
   finish_stripes<ACT, 8, 2>(
       a, reinterpret_cast<char*>(smem) + wave * 16384, at.split, lane,
@@ -1028,8 +1086,16 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
     }
   }
   const long long tiles = ((a.rows - 1LL) / p.tile + 1) * ((a.cols - 1LL) / p.tile + 1) * p.S;
-  if (p.tile == 256)
-    linear_big_kernel<TA, TB, ACT><<<(unsigned)tiles, 256, 0, s>>>(a);
+  if (p.tile == 256) {
+    if constexpr (TA && TB) {
+      if (a.row_sums != nullptr)
+        linear_big_kernel<TA, TB, ACT, true><<<(unsigned)tiles, 256, 0, s>>>(a);
+      else
+        linear_big_kernel<TA, TB, ACT, false><<<(unsigned)tiles, 256, 0, s>>>(a);
+    } else {
+      linear_big_kernel<TA, TB, ACT, false><<<(unsigned)tiles, 256, 0, s>>>(a);
+    }
+  }
   // more blocks than CUs: two to a CU, fewer chunks ahead each (128 x 128, 336 blocks of 64
   // chunks: 70 -> 53 us; 256 blocks, one to a CU in any case, 78 us so, 68 us with four chunks
   // and eight waves)
@@ -1056,6 +1122,12 @@ int bias_ranges(int rows, int cols) {
   return std::max(2, std::min((4 * device_cu_count() + cb - 1) / cb, rows / 128));
 }
 
+// Parts of the bias' sums where dw's large tiles make them (0: they do not): dz is dy, and
+// the tiles read all of it.
+int bias_parts_of_dw(int M, int N, int K, bool bf16) {
+  return bf16 && M > 0 && linear_plan(N, K, M, false).tile == 256 ? 2 * ((K - 1) / 256 + 1) : 0;
+}
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace
@@ -1075,7 +1147,7 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
 
 size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16) {
   if (M == 0) return kLinearWsLeast;
-  return align256((size_t)bias_ranges(M, N) * (size_t)N * 4) +
+  return align256((size_t)std::max(bias_ranges(M, N), bias_parts_of_dw(M, N, K, bf16)) * (size_t)N * 4) +
          std::max(product_ws(M, K, N, false, bf16), product_ws(N, K, M, false, bf16));
 }
 
@@ -1093,8 +1165,14 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     return e;
   }
   const bool own = c.act != kActNone || c.mul != nullptr;  // dz is not dy
-  const int P = bias_ranges(c.M, c.N);
-  if (own || c.dbias != nullptr) {
+  const int parts = bias_parts_of_dw(c.M, c.N, c.K, c.bf16);
+  const bool by_dw = parts > 0 && !own && c.dw != nullptr && c.dbias != nullptr;
+  const int P = by_dw ? parts : bias_ranges(c.M, c.N);
+  auto join_bias = [&] {
+    bias_join_kernel<<<(unsigned)((c.N + 63) / 64), 64, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
+    return hipGetLastError();
+  };
+  if (own || (c.dbias != nullptr && !by_dw)) {
     ActBackwardArgs b{};
     b.dy = c.dy, b.mul = c.mul, b.dmul = c.dmul;
     b.z = c.act != kActNone || c.dmul != nullptr ? c.z : nullptr;
@@ -1114,13 +1192,11 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    if (c.dbias != nullptr && P > 1) {
-      bias_join_kernel<<<(unsigned)((c.N + 63) / 64), 64, 0, s>>>(static_cast<const float*>(ws), c.N, P, c.dbias);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    if (c.dbias != nullptr && P > 1)
+      if ((e = join_bias()) != hipSuccess) return e;
   }
   const void* dz = own ? c.dz : c.dy;
-  void* part = static_cast<char*>(ws) + align256((size_t)P * (size_t)c.N * 4);
+  void* part = static_cast<char*>(ws) + align256((size_t)std::max(P, parts) * (size_t)c.N * 4);
   LinArgs x{}, w{};
   x.A = dz, x.B = c.w, x.lda = c.N, x.ldb = c.ldw;
   x.rows = c.M, x.cols = c.K, x.red = c.N, x.out = c.dx;
@@ -1130,6 +1206,7 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     w.out = c.dw;
   else
     w.out32 = static_cast<float*>(c.dw);
+  if (by_dw) w.row_sums = static_cast<float*>(ws);
   if (c.dx != nullptr && c.dw != nullptr && c.bf16) {
     const LinPlan px = linear_plan(x.rows, x.cols, x.red, false), pw = linear_plan(w.rows, w.cols, w.red, false);
     if (px.tile == 64 && px.S == 1 && pw.tile == 64 && pw.S == 1) {
@@ -1143,6 +1220,7 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     if ((e = launch_product<false, true, kActNone>(x, c.bf16, part, s)) != hipSuccess) return e;
   if (c.dw != nullptr)
     if ((e = launch_product<true, true, kActNone>(w, c.bf16, part, s)) != hipSuccess) return e;
+  if (by_dw) e = join_bias();
   return e;
 }
 
