@@ -1026,6 +1026,7 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t* p, size_t n) {
 struct LinPlan {
   int tile;  // rows and columns of a tile; 0: few rows
   int S;
+  long long ns;  // expected
 };
 constexpr int kFewRows = 32;
 
@@ -1035,28 +1036,49 @@ constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 // Few rows: its reads of x grow with the rows, the tiles' do not (us, few rows / 64 x 64 tiles:
 // 16 rows of 7168 x 2048 9.6 / 11.9, 16 of 2048 x 7168 14.9 / 15.4, 8 of 14336 x 4096 25.9 /
 // 23.4, 1 21.3 / 23.4, 32 of 768 x 2048 7.5 / 9.0).
-// Tiles: the largest that fill the chip (256 x 256 where three quarters of it: a tile of 128
-// does 0.6 of its rate). 64 x 64 and 128 x 128 tiles of fewer blocks than CUs may cut the
-// reduction in S ranges, by what a chunk of a tile and the join measured: 0.27 and 0.5 us a
-// chunk, 1 us around a tile, 3.5 us a join and its bytes at 3 TB/s.
-LinPlan linear_plan(int rows, int cols, int red, bool few) {
-  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1};
-  const long long cus = device_cu_count();
-  auto tiles = [&](int t) { return ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1); };
-  LinPlan p{tiles(256) >= cus * 3 / 4 ? 256 : tiles(128) >= cus ? 128 : 64, 1};
-  const long long n = tiles(p.tile);
-  if (p.tile == 256 || n >= cus) return p;
+// Tiles: the least time by what a 64-wide chunk of a tile and the rest of the tile took where
+// blocks filled the CUs (us; two blocks of a CU together): 256 x 256 1.45 and 9, 128 x 128 0.59
+// and 3, two 1.0 and 4.5, 64 x 64 0.30 and 2.5, two 0.41 and 3.5. The reduction may be cut in S
+// ranges: a join takes 3.5 us and the partial sums' bytes, written and read, at 4 TB/s.
+// (768 x 2048 out of 12265 rows: 64 x 64 tiles uncut 110 us, by this rule 43.)
+LinPlan make_plan(int rows, int cols, int red, bool few, long long cus) {
+  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1, 0};
   const long long chunks = red / kChunk, plane = (long long)rows * cols * 4;
-  const long long chunk_ns = p.tile == 64 ? 270 : 500;
-  long long best = LLONG_MAX;
-  for (int S = 1; S <= 16; ++S) {
-    if (S > 1 && (chunks / S < 4 || n * S > 2 * cus || plane * S > (long long)kLinPartBytes)) break;
-    // two blocks of a CU take 1.4 times one's time
-    long long ns = ((chunks + S - 1) / S * chunk_ns + 1000) * (n * S <= cus ? 10 : 14) / 10;
-    if (S > 1) ns += 3500 + 2 * S * plane / 3000;
-    if (ns < best) best = ns, p.S = S;
+  LinPlan best{64, 1, LLONG_MAX};
+  for (int t : {256, 128, 64}) {
+    const long long n = ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1);
+    for (int S = 1; S <= 16; ++S) {
+      if (S > 1 && (chunks / S < 4 || plane * S > (long long)kLinPartBytes)) break;
+      const long long blocks = n * S, c = (chunks + S - 1) / S;
+      long long ns;
+      if (t == 256)
+        ns = ((blocks - 1) / cus + 1) * (c * 1450 + 9000);
+      else if (blocks <= cus)
+        ns = t == 128 ? c * 590 + 3000 : c * 300 + 2500;
+      else
+        ns = ((blocks - 1) / (2 * cus) + 1) * (t == 128 ? c * 1000 + 4500 : c * 410 + 3500);
+      if (S > 1) ns += 3500 + 2 * S * plane / 4000;
+      if (ns < best.ns) best = {t, S, ns};
+    }
   }
-  return p;
+  return best;
+}
+
+// A plan depends on sizes alone; a few are kept, since a call asks for several and making
+// one takes a microsecond.
+LinPlan linear_plan(int rows, int cols, int red, bool few) {
+  struct Kept {
+    int rows, cols, red, few;
+    long long cus;
+    LinPlan plan;
+  };
+  thread_local Kept kept[64] = {};
+  const long long cus = device_cu_count();
+  const uint32_t h = ((uint32_t)rows * 2654435761u ^ (uint32_t)cols * 2246822519u ^ (uint32_t)red * 3266489917u ^ (few ? 1u : 0u));
+  Kept& k = kept[(h >> 16 ^ h) % 64];
+  if (k.rows != rows || k.cols != cols || k.red != red || k.few != (few ? 1 : 0) || k.cus != cus)
+    k = {rows, cols, red, few ? 1 : 0, cus, make_plan(rows, cols, red, few, cus)};
+  return k.plan;
 }
 
 size_t product_ws(int rows, int cols, int red, bool few, bool bf16) {
@@ -1208,11 +1230,17 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     w.out32 = static_cast<float*>(c.dw);
   if (by_dw) w.row_sums = static_cast<float*>(ws);
   if (c.dx != nullptr && c.dw != nullptr && c.bf16) {
+    // In one launch where that is expected to take less than one after the other: all blocks
+    // at once, or those past two a CU after the shorter ones (768 x 2048 out of 333 rows
+    // 15.0 -> 10.8 us; 1336 x 1000 out of 1000 would be 24.1, and is 21.3).
     const LinPlan px = linear_plan(x.rows, x.cols, x.red, false), pw = linear_plan(w.rows, w.cols, w.red, false);
-    if (px.tile == 64 && px.S == 1 && pw.tile == 64 && pw.S == 1) {
-      auto tiles = [](const LinArgs& a) { return (unsigned)(((a.rows - 1) / 64 + 1) * ((a.cols - 1) / 64 + 1)); };
+    auto tiles = [](const LinArgs& a) { return ((a.rows - 1LL) / 64 + 1) * ((a.cols - 1LL) / 64 + 1); };
+    const long long n = tiles(x) + tiles(w), slots = 2 * device_cu_count();
+    const long long tx = x.red / kChunk * 410LL + 3500, tw = w.red / kChunk * 410LL + 3500;
+    const long long together = n <= slots ? std::max(tx, tw) : std::max(std::max(tx, tw), std::min(tx, tw) + tw);
+    if (!by_dw && n <= 2 * slots && together < px.ns + pw.ns + 1000) {
       x.S = w.S = 1;
-      linear_pair_kernel<64, 64, 2, 2, 4><<<tiles(x) + tiles(w), 256, 0, s>>>(x, w, tiles(x));
+      linear_pair_kernel<64, 64, 2, 2, 4><<<(unsigned)n, 256, 0, s>>>(x, w, (unsigned)tiles(x));
       return hipGetLastError();
     }
   }
