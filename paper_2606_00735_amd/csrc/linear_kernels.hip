@@ -1026,6 +1026,7 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t* p, size_t n) {
 struct LinPlan {
   int tile;  // rows and columns of a tile; 0: few rows
   int S;
+  int cut;       // the first rows, in whole rounds of large tiles; 0: all rows are alike
   long long ns;  // expected
 };
 constexpr int kFewRows = 32;
@@ -1042,9 +1043,9 @@ constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 // ranges: a join takes 3.5 us and the partial sums' bytes, written and read, at 4 TB/s.
 // (768 x 2048 out of 12265 rows: 64 x 64 tiles uncut 110 us, by this rule 43.)
 LinPlan make_plan(int rows, int cols, int red, bool few, long long cus) {
-  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1, 0};
+  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1, 0, 0};
   const long long chunks = red / kChunk, plane = (long long)rows * cols * 4;
-  LinPlan best{64, 1, LLONG_MAX};
+  LinPlan best{64, 1, 0, LLONG_MAX};
   for (int t : {256, 128, 64}) {
     const long long n = ((rows - 1LL) / t + 1) * ((cols - 1LL) / t + 1);
     for (int S = 1; S <= 16; ++S) {
@@ -1058,8 +1059,19 @@ LinPlan make_plan(int rows, int cols, int red, bool few, long long cus) {
       else
         ns = ((blocks - 1) / (2 * cus) + 1) * (t == 128 ? c * 1000 + 4500 : c * 410 + 3500);
       if (S > 1) ns += 3500 + 2 * S * plane / 4000;
-      if (ns < best.ns) best = {t, S, ns};
+      if (ns < best.ns) best = {t, S, 0, ns};
     }
+  }
+  // Whole rounds of large tiles and the rest of the rows by a plan of its own, where a last
+  // round would leave much of the chip idle (2422 x 14336 x 4096, 560 tiles: 300 -> 262 us). A
+  // round that is partly idle runs at a higher clock, so little gains are none (5120 x 8192
+  // out of 9000 rows, expected 636 -> 570 us, took 594 -> 621), nor are short reductions.
+  const long long nts = (cols - 1LL) / 256 + 1, rounds = (((rows - 1LL) / 256 + 1) * nts) / cus;
+  const long long cut = rounds * cus / nts * 256;
+  if (cut > 0 && cut < rows && chunks >= 16) {
+    const LinPlan rest = make_plan(rows - (int)cut, cols, red, few, cus);
+    const long long ns = rounds * (chunks * 1450 + 9000) + rest.ns + 2000;
+    if (ns < best.ns * 85 / 100) best = {256, 1, (int)cut, ns};
   }
   return best;
 }
@@ -1084,6 +1096,7 @@ LinPlan linear_plan(int rows, int cols, int red, bool few) {
 size_t product_ws(int rows, int cols, int red, bool few, bool bf16) {
   if (!bf16 || rows == 0) return 0;
   const LinPlan p = linear_plan(rows, cols, red, few);
+  if (p.cut > 0) return product_ws(rows - p.cut, cols, red, few, bf16);
   return p.S > 1 ? (size_t)p.S * (size_t)rows * (size_t)cols * 4 : 0;
 }
 
@@ -1095,6 +1108,23 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
     return hipGetLastError();
   }
   const LinPlan p = linear_plan(a.rows, a.cols, a.red, !TA && !TB);
+  if (p.cut > 0) {
+    LinArgs top = a;
+    top.rows = p.cut, top.S = 1;
+    linear_big_kernel<TA, TB, ACT, false><<<(unsigned)(p.cut / 256 * ((a.cols - 1) / 256 + 1)), 256, 0, s>>>(top);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const size_t rows = (size_t)p.cut, out = rows * (size_t)a.cols;
+    auto past = [](auto*& q, size_t n) {
+      using Q = std::remove_reference_t<decltype(q)>;
+      if (q != nullptr) q = (Q)((uintptr_t)q + 2 * n);
+    };
+    past(a.A, TA ? rows : rows * (size_t)a.lda);
+    past(a.mul, out), past(a.res, out), past(a.z, out), past(a.out, out);
+    if (a.out32 != nullptr) a.out32 += out;
+    a.rows -= p.cut;
+    return launch_product<TA, TB, ACT>(a, bf16, ws, s);
+  }
   a.S = p.S;
   a.part = static_cast<float*>(ws);
   if constexpr (!TA && !TB) {
@@ -1147,7 +1177,9 @@ int bias_ranges(int rows, int cols) {
 // Parts of the bias' sums where dw's large tiles make them (0: they do not): dz is dy, and
 // the tiles read all of it.
 int bias_parts_of_dw(int M, int N, int K, bool bf16) {
-  return bf16 && M > 0 && linear_plan(N, K, M, false).tile == 256 ? 2 * ((K - 1) / 256 + 1) : 0;
+  if (!bf16 || M == 0) return 0;
+  const LinPlan p = linear_plan(N, K, M, false);
+  return p.tile == 256 && p.S == 1 && p.cut == 0 ? 2 * ((K - 1) / 256 + 1) : 0;
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
