@@ -236,10 +236,11 @@ struct Panel {
 // N stripes of a wave's sums, 32 rows x 32 NI columns each, whose lanes hold groups of 4
 // consecutive columns of a row, through the wave's own piece of LDS to whole rows of 8
 // columns a lane. sums(n, put) puts stripe n's groups: put(row, group of columns, values);
-// the stripe's first row and column are r0(n) and c0(n). mul and res are loaded four stripes ahead (one ahead, their latencies
-// took 20 us a 256 x 256 tile); each element is read by the lane that writes it, so out may
-// be one of them. Rows and columns past C's are not
-// stored.
+// the stripe's first row and column are r0(n) and c0(n). mul and res are loaded four stripes
+// ahead (one ahead, their latencies took 20 us a 256 x 256 tile; the first four before the
+// reduction gain nothing on large tiles, 1 % on small ones, and lose 3 % where blocks share a
+// CU). Each element is read by the lane that writes it, so out may be one of them. Rows and
+// columns past C's are not stored.
 template <int ACT, int N, int NI, class Sums, class Row, class Col>
 __device__ __forceinline__ void finish_stripes(const LinArgs& a, char* lds, int split, int lane, Sums&& sums, Row&& r0,
                                                Col&& c0) {
@@ -454,6 +455,15 @@ __global__ __launch_bounds__(WR* WC* kWave) void linear_pair_kernel(LinArgs dx, 
 // ---------------------------------------------------------------------------
 constexpr int kSlotBytes = 128 * kChunk * 2;
 
+// Position of a 16-byte piece in a transposed slot's row of 256 bytes. A transposing read has
+// its first 32 lanes at rows 0-3 and 8-11 of 32 bytes each: rows r and r + 1 lie 64 bytes
+// apart, rows r and r + 8 32, so no two lanes meet in a bank. (Without the latter the LDS
+// spent 29 000 of a CU's 312 000 cycles of a dx of 8192 x 7168 x 2048 on conflicts, which its
+// MFMAs hid: the time is the same within 0.5 %.)
+__device__ __forceinline__ int big_piece(int row, int piece) {
+  return piece ^ ((row & 3) << 2) ^ (((row >> 3) & 1) << 1);
+}
+
 template <bool TR>
 struct BigOperand {
   static constexpr int RB = TR ? 256 : 128, PP = RB / 16, RPI = 1024 / RB;
@@ -475,7 +485,7 @@ struct BigOperand {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (TR) {
-          const int piece = tr_piece<128>(r, lane % PP);
+          const int piece = big_piece(r, lane % PP);
           off[h][t] = (uint32_t)r * (uint32_t)(ld * 2) +
                       (uint32_t)(min((piece >> 3) * 128 + h * 64 + (piece & 7) * 8, left - 8) * 2);
         } else {
@@ -491,7 +501,7 @@ struct BigOperand {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int colb = (wsel * 64 + i * 16) * 2 + 8 * (lane & 3);
-        fof[0][i] = lds + (uint32_t)(row * RB + tr_piece<128>(row, colb >> 4) * 16 + (colb & 15));
+        fof[0][i] = lds + (uint32_t)(row * RB + big_piece(row, colb >> 4) * 16 + (colb & 15));
         fof[1][i] = fof[0][i] + 4 * kSlotBytes;
         asm("" : "+v"(fof[1][i]));  // a register of its own, not an addition at each read
       }
