@@ -682,7 +682,7 @@ moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_ro
  * logits [T, E] fp32; bias [E] fp32 or NULL; mask [T] uint8 or NULL (all live)
  * ids [T, k] int32, w [T, k] fp32: written completely
  * Limits: 1 <= E <= 256, n_group divides E, 1 <= topk_group <= n_group,
- * 1 <= k <= min(topk_group * E / n_group, 16), scale finite, T * E <= 2^40.
+ * 1 <= k <= min(topk_group * E / n_group, 16), scale finite in fp32, T * E <= 2^40.
  */
 moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask, int T, int E, int k,
                      moe_score score, int n_group, int topk_group, int norm, double scale, int32_t* ids,
@@ -701,8 +701,8 @@ moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask
  * dlogits holds (moe_gate_backward's gradient of the losses, say).
  *
  * logits [T, E], dw [T, k] fp32; ids [T, k] int32; dlogits [T, E] fp32, written completely;
- * it must not overlap logits. Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), scale finite,
- * T * E <= 2^40.
+ * it must not overlap logits or dw. Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), scale
+ * finite in fp32, T * E <= 2^40.
  */
 moe_status moe_route_backward(const float* logits, const int32_t* ids, const float* dw, int T, int E, int k,
                               moe_score score, int norm, double scale, int accumulate, float* dlogits,
@@ -746,7 +746,7 @@ moe_status moe_linear(const void* x, const void* w, const float* bias, const voi
  * dz [M, N] dt: required with an activation or mul (it may be dy itself), not written
  *   without; dmul [M, N] dt or NULL (NULL without mul; not dz, dy or mul)
  * dx [M, K] dt or NULL; dw [N, K] of dw_dt or NULL (fp32 data: fp32; bf16 data: either);
- * dbias [N] fp32 or NULL
+ * dbias [N] fp32 or NULL; no output overlaps another, but dz may be dy
  * ws and limits as moe_linear. M == 0 writes zeros to dw and dbias.
  */
 moe_status moe_linear_backward(const void* dy, const void* x, const void* w, const void* z, const void* mul,

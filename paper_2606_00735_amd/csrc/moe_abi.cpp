@@ -708,7 +708,7 @@ moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask
   if (st != MOE_OK) return st;
   if (score != MOE_SIGMOID && score != MOE_SOFTMAX) return MOE_ERR_INVALID_ARG;
   if (n_group < 1 || n_group > E || E % n_group != 0 || topk_group < 1 || topk_group > n_group ||
-      k > topk_group * (E / n_group) || !std::isfinite(scale))
+      k > topk_group * (E / n_group) || !std::isfinite((float)scale))
     return MOE_ERR_INVALID_ARG;
   if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
@@ -723,11 +723,11 @@ moe_status moe_route_backward(const float* logits, const int32_t* ids, const flo
                               hipStream_t stream) {
   const moe_status st = check_tk(T, k, E);
   if (st != MOE_OK) return st;
-  if ((score != MOE_SIGMOID && score != MOE_SOFTMAX) || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
+  if ((score != MOE_SIGMOID && score != MOE_SOFTMAX) || !std::isfinite((float)scale)) return MOE_ERR_INVALID_ARG;
   if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!logits || !ids || !dw || !dlogits || !aligned16(logits) || !aligned16(dlogits) || !aligned4(ids) ||
-      !aligned4(dw) || dlogits == logits)
+      !aligned4(dw) || dlogits == logits || dlogits == dw)
     return MOE_ERR_INVALID_ARG;
   return hip_status(moe::launch_route_backward(logits, ids, dw, T, E, k, score == MOE_SOFTMAX, norm != 0, (float)scale,
                                                accumulate != 0, dlogits, stream));
@@ -796,6 +796,7 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
     for (const void* in : {dy, x, w, (const void*)(own ? dz : nullptr)})
       if (in && (dx == in || dw == in)) return MOE_ERR_INVALID_ARG;
   }
+  if ((dx && (dx == dw || dx == dmul || dx == dbias)) || (dw && (dw == dmul || dw == dbias))) return MOE_ERR_INVALID_ARG;
   moe::LinearBackwardCall c{dy, x, w, z, mul, M, N, K, ld, (int)act, dt == MOE_BF16, dw_dt == MOE_BF16, dz, dmul, dx,
                             dw, dbias};
   return hip_status(moe::launch_linear_backward(c, ws, stream));

@@ -32,6 +32,7 @@ def route(L, z=FAKE, bias=None, mask=None, T=4, E=16, k=2, score=0, G=4, g=2, no
     (dict(z=NULL), INVALID), (dict(ids=NULL), INVALID), (dict(w=NULL), INVALID), (dict(z=ODD), INVALID),
     (dict(ids=ODD4), INVALID), (dict(w=ODD4), INVALID), (dict(bias=ODD4), INVALID),
     (dict(T=0, z=NULL, ids=NULL, w=NULL), 0),
+    (dict(scale=1e39), INVALID), (dict(scale=-1e39), INVALID),  # not finite in fp32
 ])
 def test_route_checks(L, args, want):
     assert route(L, **args) == want
@@ -46,6 +47,7 @@ def route_backward(L, z=FAKE, ids=FAKE, dw=FAKE, T=4, E=16, k=2, score=0, norm=1
     (dict(scale=math.inf), INVALID), (dict(z=NULL), INVALID), (dict(ids=NULL), INVALID), (dict(dw=NULL), INVALID),
     (dict(dz=NULL), INVALID), (dict(dz=FAKE), INVALID), (dict(z=ODD), INVALID), (dict(dz=ODD), INVALID),
     (dict(dw=ODD4), INVALID), (dict(T=0, z=NULL, ids=NULL, dw=NULL, dz=NULL), 0),
+    (dict(scale=1e39), INVALID), (dict(dw=FAKE2, E=2), INVALID),
 ])
 def test_route_backward_checks(L, args, want):
     assert route_backward(L, **args) == want
@@ -96,6 +98,8 @@ A, B, C, D = (ctypes.c_void_p(0x60000 + 0x10000 * i) for i in range(4))
     (dict(mul=A, dz=B, dmul=FAKE, z=D), INVALID), (dict(act=2, z=A, dz=A), INVALID), (dict(mul=A, dz=A), INVALID),
     (dict(dx=FAKE), INVALID), (dict(dx=FAKE3), INVALID), (dict(dw=FAKE2), INVALID), (dict(act=2, z=A, dz=B, dx=B), INVALID),
     (dict(dy=ODD), INVALID), (dict(x=ODD), INVALID), (dict(w=ODD), INVALID), (dict(dx=ODD), INVALID), (dict(dw=ODD), INVALID),
+    (dict(dw=ctypes.c_void_p(0x40000)), INVALID), (dict(db=ctypes.c_void_p(0x50000)), INVALID),  # one output twice
+    (dict(mul=A, dz=B, dmul=ctypes.c_void_p(0x40000), z=D), INVALID),
     (dict(db=ODD), INVALID), (dict(ws=ODD), INVALID), (dict(act=2, z=ODD, dz=B), INVALID), (dict(act=2, z=A, dz=ODD), INVALID),
 ])
 def test_linear_backward_checks(L, args, want):
