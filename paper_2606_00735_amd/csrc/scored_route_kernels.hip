@@ -8,7 +8,7 @@
 //
 // Which of two scores is larger decides whole numbers, so s and c that decide are held in
 // 64 bits: c's of different experts come as near as fp32 rounds them a few times in a
-// batch of 16384 tokens. The weights are rounded to fp32 once.
+// batch of 16384 tokens. The weights are fp32 (a few roundings each).
 #include <math.h>
 
 #include <algorithm>
@@ -191,7 +191,8 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 // The selection runs on 32-bit keys: c in fp32 (an exponential and a reciprocal of 1 ulp),
 // mapped to integers in the same order, the lowest 4 bits replaced by the position in the
 // lane. A lane sorts its keys once; a round is then a maximum of the lanes' first ones (four
-// DPP steps), and the lane that had it moves its keys up.
+// DPP steps), and the lane that had it takes its next one. k rounds run without a look at
+// their gaps, which the lanes see to afterwards, a candidate each.
 //
 // What fp32 cannot decide is seen from the gaps (`wide`: more than twice what a key can be
 // off). Rounds go on until the next key is certainly below the k-th best, so that the k
@@ -201,7 +202,9 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 // c's of a lane alike at that border, a NaN or an infinite score selects again from all its
 // experts in 64 bits.
 // 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64 bits, a wave each;
-// 37 us without the sort and with all uncertain rows done again.
+// 37 us without the sort and with all uncertain rows done again; 13.6 us with the gaps in the
+// rounds and the keys moved through registers; 10.3-11.3 us so (one token 4.6 us), 1.7 TB/s: a
+// wave of four tokens has some thousand instructions, and all waves run at once.
 // ---------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
@@ -387,7 +390,7 @@ __device__ __forceinline__ void select64(const RouteArgs& a, const float* row, i
 
 template <int V, bool SOFT>
 __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
-  __shared__ double keys64[V * 256];  // of select64
+  __shared__ double keys64[V * 256];  // of select64, and sorted 32-bit keys
   const int lane = threadIdx.x & 63, l = lane & 15;
   const long long t = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const size_t r = (size_t)(t < a.T ? t : a.T - 1);  // lanes past the last token repeat it and store nothing
@@ -544,30 +547,63 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
       for (int v = 0; v < V; ++v) key[v] = 0;
     }
   }
-  int id = -1, id2 = -1;  // candidates l and 16 + l
-  float last = 0.0f, kth = 0.0f;
-  bool near = false;  // a gap between candidates is not wide
-#pragma unroll 1
-  for (int j = 0;; ++j) {
-    const uint32_t best = row_reduce(key[0], [](uint32_t p, uint32_t q) { return max(p, q); });
-    const float value = key_value(best);
-    if (best == 0 || (j >= a.k && wide(kth - value, kth, value))) break;
-    if (j == 32) {
-      ok = false;
-      break;
-    }
-    near |= j > 0 && !wide(last - value, last, value);
-    last = value;
-    if (j == a.k - 1) kth = value;
-    // of equal keys of several lanes, the lowest lane's
-    const int holder = __ffs((uint32_t)(__ballot(key[0] == best) >> (lane & 48)) & 0xffffu) - 1;
-    const int e = holder * V + 15 - (int)(best & 15u);
-    if (l == j) id = e;
-    if (l + 16 == j) id2 = e;
-    if (l == holder) {
+  // The largest key of the row, k times and then as long as one may belong before the k-th.
+  // A lane's two largest left are in registers, the others in LDS (sixteen registers moved up
+  // were a third of a round).
+  constexpr bool kInLds = V > 4;
+  uint32_t k0 = key[0], k1 = V > 1 ? key[1 % V] : 0u;
+  // in the thread's own doubles: another wave may be in select64
+  typedef uint32_t __attribute__((may_alias)) word;
+  word* rest = reinterpret_cast<word*>(keys64 + threadIdx.x);
+  if (kInLds) {
 #pragma unroll
-      for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
-      key[V - 1] = 0;
+    for (int v = 0; v < V; ++v) rest[512 * v] = v + 2 < V ? key[(v + 2) % V] : 0u;
+  }
+  // takes the largest, which is not 0: its expert; of equal keys of several lanes, the
+  // lowest lane's
+  auto take = [&](uint32_t best) __attribute__((always_inline)) {
+    const int holder = __ffs((uint32_t)(__ballot(k0 == best) >> (lane & 48)) & 0xffffu) - 1;
+    if (l == holder && best != 0) {
+      k0 = k1;
+      if (kInLds) {
+        k1 = *rest;
+        rest += 512;
+      } else {
+#pragma unroll
+        for (int v = 1; v + 1 < V; ++v) key[v] = key[v + 1];
+        key[V - 1] = 0;
+        k1 = V > 1 ? key[1 % V] : 0u;
+      }
+    }
+    return holder * V + 15 - (int)(best & 15u);
+  };
+  auto largest = [&] { return row_reduce(k0, [](uint32_t p, uint32_t q) { return max(p, q); }); };
+  int id = -1, id2 = -1;  // candidates l and 16 + l
+  uint32_t mine = 0, best = 0;  // candidate l's key, the last one's
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {
+    best = largest();
+    const int e = take(best);
+    if (l == j && best != 0) id = e, mine = best;
+  }
+  // near: a gap between candidates is not wide
+  const float value = key_value(mine), prev = key_value(dpp_u32<0x111>(mine));  // row_shr by 1
+  bool near = l > 0 && mine != 0 && !wide(prev - value, prev, value);
+  if (best != 0) {
+    const float kth = key_value(best);
+#pragma unroll 1
+    for (int j = a.k;; ++j) {
+      best = largest();
+      const float v = key_value(best);
+      if (best == 0 || wide(kth - v, kth, v)) break;
+      if (j == 32) {
+        ok = false;
+        break;
+      }
+      near = true;
+      const int e = take(best);
+      if (l == j) id = e;
+      if (l + 16 == j) id2 = e;
     }
   }
   if (__any(live && near && ok)) {
