@@ -930,7 +930,8 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
 // fp32 values, before dz is rounded). A block: L lanes of 8 columns by R rows at a time, of
 // a range of rows. Whole rows of 512 bytes where there are rows for many ranges (8192 x 7168
 // for the bias alone: 19.8 us, 5.9 TB/s; 64 columns by 32 rows 30 us); 64 columns by 128 rows
-// and one range, without a join, for few.
+// and one range, without a join, for few; 32 columns by 256 rows where the matrix is small
+// (act_narrow): few blocks, so what counts is how many rows are in flight together.
 // ---------------------------------------------------------------------------
 struct ActBackwardArgs {
   const void *dy, *z, *mul;
@@ -939,9 +940,17 @@ struct ActBackwardArgs {
   int rows, cols, P;
 };
 
+// v plus the value of the lane N places on in the 16-lane row
+template <int N>
+__device__ __forceinline__ float plus_ror(float v) {
+  const int i = __builtin_bit_cast(int, v);
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x120 | N, 0xf, 0xf, false));
+}
+
 template <bool BF16, int ACT, int L, int R>
 __global__ __launch_bounds__(L* R) void act_backward_kernel(ActBackwardArgs a) {
-  __shared__ float sums[R][8 * L];
+  constexpr int PARTS = L < 16 ? L * R / kWave : R;
+  __shared__ float sums[PARTS][8 * L];
   const int tid = threadIdx.x, c8 = tid % L, ry = tid / L;
   const int cb = (int)(blockIdx.x / (unsigned)a.P), p = (int)(blockIdx.x % (unsigned)a.P);
   const int col = cb * 8 * L + c8 * 8;
@@ -999,13 +1008,24 @@ __global__ __launch_bounds__(L* R) void act_backward_kernel(ActBackwardArgs a) {
     }
   }
   if (a.db == nullptr) return;
+  if (L < 16) {  // a wave's rows first
 #pragma unroll
-  for (int q = 0; q < 8; ++q) sums[ry][c8 * 8 + q] = db[q];
+    for (int q = 0; q < 8; ++q) {
+      if (L == 4) db[q] = plus_ror<4>(db[q]);
+      db[q] = plus_ror<8>(db[q]);
+      db[q] += __shfl_xor(db[q], 16, kWave);
+      db[q] += __shfl_xor(db[q], 32, kWave);
+    }
+  }
+  if (L >= 16 || (tid & 63) < L) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sums[L < 16 ? tid >> 6 : ry][c8 * 8 + q] = db[q];
+  }
   __syncthreads();
   if (tid < 8 * L && cb * 8 * L + tid < a.cols) {
     float s = 0.0f;
-#pragma unroll 8
-    for (int q = 0; q < R; ++q) s += sums[q][tid];
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) s += sums[q][tid];
     a.db[(size_t)p * (size_t)a.cols + cb * 8 * L + tid] = s;
   }
 }
@@ -1176,9 +1196,20 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Row ranges of the bias' sums: one up to 1024 rows (no join), then enough blocks of 256
-// columns for the chip, at least 128 rows each.
+// The activation's gradient by blocks of 32 columns x 256 rows: where they are for half the
+// CUs at most and the data are few (us, silu and gate and bias, otherwise / so: 333 x 1336 6.5 /
+// 5.0, 1024 x 2048 13.6 / 9.7, 1500 x 4096 24.0 / 19.5, 16384 x 8 32.8 / 7.6; 2048 x 4096 22.9 /
+// 24.8, 16384 x 2048 76 / 106: its rows of 64 bytes reach two thirds of the bandwidth).
+bool act_narrow(int rows, int cols) {
+  return 2 * ((cols - 1) / 32 + 1) <= device_cu_count() && (long long)rows * cols <= (6 << 20);
+}
+
+// Row ranges of the bias' sums: one up to 768 or 1024 rows (a join takes 2 us), then 512 rows
+// each while blocks of 32 columns fill the chip, or enough blocks of 256 columns for it, at
+// least 128 rows each.
 int bias_ranges(int rows, int cols) {
+  if (act_narrow(rows, cols))
+    return rows <= 768 ? 1 : std::min((rows - 1) / 512 + 1, device_cu_count() / ((cols - 1) / 32 + 1));
   if (rows <= 1024) return 1;
   const int cb = (cols - 1) / 256 + 1;
   return std::max(2, std::min((4 * device_cu_count() + cb - 1) / cb, rows / 128));
@@ -1247,7 +1278,9 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
       constexpr int A = decltype(act)::value;
       auto go = [&](auto bf16) {
         constexpr bool BF = decltype(bf16)::value;
-        if (P == 1)
+        if (act_narrow(c.M, c.N))
+          act_backward_kernel<BF, A, 4, 256><<<(unsigned)((c.N - 1) / 32 + 1) * (unsigned)P, 1024, 0, s>>>(b);
+        else if (P == 1)
           act_backward_kernel<BF, A, 8, 128><<<(unsigned)((c.N - 1) / 64 + 1), 1024, 0, s>>>(b);
         else
           act_backward_kernel<BF, A, 32, 8><<<(unsigned)((c.N - 1) / 256 + 1) * (unsigned)P, 256, 0, s>>>(b);

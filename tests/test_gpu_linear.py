@@ -151,7 +151,8 @@ def test_epilogues(M, N, K, act, dtype):
 
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu", "none"])
 @pytest.mark.parametrize("dtype", [BF, torch.float32])
-@pytest.mark.parametrize("M,N,K", [(1, 256, 64), (65, 264, 1000), (900, 136, 72), (1500, 264, 64)])
+@pytest.mark.parametrize("M,N,K", [(1, 256, 64), (65, 264, 1000), (900, 136, 72), (1500, 264, 64),
+                                   (300, 4232, 64), (1100, 6000, 64)])  # wider than blocks of 32 columns are for
 def test_gradients(M, N, K, act, dtype):
     banner("linear backward", M, N, K, act, dtype)
     g = gen(K + 1)
