@@ -799,21 +799,29 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows (of x): 16 MB of them by 16 columns a block. The weights are read once, from
+// Few rows (of x): 16 MB of them by C columns a block. The weights are read once, from
 // memory to the 16 x 16 x 32 MFMA's registers, the reduction dealt to the W waves k-step
-// by k-step, so that together they read whole lines; their sums are joined in LDS. With
-// one row it is a chain of three latencies (operands, join, stores) around the weights'
-// bytes. All loads of G k-steps are in flight together.
+// by k-step; their sums are joined in LDS. With one row it is a chain of three latencies
+// (operands, join, stores) around the weights' bytes. All loads of G k-steps are in flight
+// together; a second set of registers, so that they never run dry, gained nothing.
+//
+// C = 8, for at most 8 rows: the MFMA's 16 columns are those 8 over two halves of a k-step of
+// 64, its 16 rows the 8 over the same halves; the two of the four products whose halves agree
+// are added. A load then takes whole lines, and there are twice the blocks: one row of 5120 x
+// 8192 25.8 -> 18.1 us (4.6 TB/s), of 2048 x 7168 11.9 -> 7.9, but of 7168 x 2048, whose 448
+// blocks of 16 columns run at once and whose 896 do not, 8.2 -> 9.1.
 // ---------------------------------------------------------------------------
-template <int MB, int W, int G, int ACT>
+template <int MB, int C, int W, int G, int ACT>
 __global__ __launch_bounds__(W* kWave) void linear_few_kernel(LinArgs a) {
+  static_assert(C == 16 || (C == 8 && MB == 1), "columns of a block");
+  constexpr int KW = C == 16 ? 32 : 64, PER = C == 16 ? 2 : 1;  // k of a step; lanes of a row of the epilogue
   __shared__ __align__(16) float part[W][MB][16][16];  // [wave][..][row][column]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = lane & 15, g = lane >> 4;
-  const int col0 = (int)blockIdx.x * 16;
+  const int r = lane & (C - 1), rr = lane & 15, g = lane >> 4;
+  const int col0 = (int)blockIdx.x * C;
   // what the epilogue needs, by the lanes that run it
-  const int er = tid >> 1, ec = col0 + (tid & 1) * 8;
-  const bool mine = tid < MB * 32 && er < a.rows && ec < a.cols;
+  const int er = tid / PER, ec = col0 + tid % PER * 8;
+  const bool mine = tid < MB * C * PER && er < a.rows && ec < a.cols;
   const size_t at = (size_t)er * (size_t)a.cols + (size_t)ec;
   Beside o{};
   Bias8 b{};
@@ -828,13 +836,13 @@ __global__ __launch_bounds__(W* kWave) void linear_few_kernel(LinArgs a) {
   f32x4_t acc[MB];
 #pragma unroll
   for (int m = 0; m < MB; ++m) acc[m] = f32x4_t{};
-  // k-steps of 32; the lane's 8 elements of one are there or not (K % 8 == 0)
-  const int steps = (a.red + 31) / 32;
+  // the lane's 8 elements of a k-step are there or not (K % 8 == 0)
+  const int steps = (a.red + KW - 1) / KW;
   for (int s0 = wave; s0 < steps; s0 += W * G) {
     uint4 fw[G], fx[G][MB];
 #pragma unroll
     for (int q = 0; q < G; ++q) {
-      const int k = (s0 + q * W) * 32 + 8 * g;
+      const int k = (s0 + q * W) * KW + 8 * g + (C == 8 ? 32 * (rr >> 3) : 0);
       const bool in = k < a.red;
       fw[q] = in ? *reinterpret_cast<const uint4*>(w + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -846,17 +854,20 @@ __global__ __launch_bounds__(W* kWave) void linear_few_kernel(LinArgs a) {
       for (int m = 0; m < MB; ++m)
         acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(fw[q]), as_bf16x8(fx[q][m]), acc[m], 0, 0, 0);
   }
-  // the lane holds columns 4 g .. 4 g + 3 of row r
+  // the lane holds columns 4 g .. 4 g + 3 of row rr
 #pragma unroll
-  for (int m = 0; m < MB; ++m) *reinterpret_cast<f32x4_t*>(&part[wave][m][r][4 * g]) = acc[m];
+  for (int m = 0; m < MB; ++m) *reinterpret_cast<f32x4_t*>(&part[wave][m][rr][4 * g]) = acc[m];
   __syncthreads();
   if (!mine) return;
   float v[8] = {};
-#pragma unroll
-  for (int q = 0; q < W; ++q) {
-    const float* p = &part[q][0][er][(tid & 1) * 8];
+  auto add = [&](const float* p) {
     const float4 u = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
     v[0] += u.x, v[1] += u.y, v[2] += u.z, v[3] += u.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+  };
+#pragma unroll
+  for (int q = 0; q < W; ++q) {
+    add(&part[q][0][er][tid % PER * 8]);
+    if (C == 8) add(&part[q][0][8 + er][8]);
   }
   finish8<ACT>(a, at, v, o, b);
 }
@@ -1064,16 +1075,18 @@ constexpr int kFewRows = 32;
 constexpr size_t kLinPartBytes = (size_t)64 << 20;  // partial sums, at most
 
 // few: the kernel of few rows can run (no operand is transposed).
-// Few rows: its reads of x grow with the rows, the tiles' do not (us, few rows / 64 x 64 tiles:
-// 16 rows of 7168 x 2048 9.6 / 11.9, 16 of 2048 x 7168 14.9 / 15.4, 8 of 14336 x 4096 25.9 /
-// 23.4, 1 21.3 / 23.4, 32 of 768 x 2048 7.5 / 9.0).
+// Few rows: its reads of x grow with the rows, more than 8 of them read the weights in half
+// lines, and its blocks go through all of the reduction; tiles do not (us, few rows / tiles:
+// 8 rows of 2048 x 7168 10.1 / 17.2, 16 17.7 / 14.8; 16 of 7168 x 2048 11.0 / 13.1; 32 of
+// 1024 x 4096 13.3 / 14.1; 12 of 64 x 8192 15.0 / 12.6; 8 of 14336 x 4096 29.8 / 29.0, 1 24.3 /
+// 30.6; 32 of 768 x 2048 7.8 / 10.2).
 // Tiles: the least time by what a 64-wide chunk of a tile and the rest of the tile took where
 // blocks filled the CUs (us; two blocks of a CU together): 256 x 256 1.45 and 9, 128 x 128 0.59
 // and 3, two 1.0 and 4.5, 64 x 64 0.30 and 2.5, two 0.41 and 3.5. The reduction may be cut in S
 // ranges: a join takes 3.5 us and the partial sums' bytes, written and read, at 4 TB/s.
 // (768 x 2048 out of 12265 rows: 64 x 64 tiles uncut 110 us, by this rule 43.)
 LinPlan make_plan(int rows, int cols, int red, bool few, long long cus) {
-  if (few && rows <= kFewRows && (long long)rows * cols * red <= 240000000LL) return {0, 1, 0, 0};
+  if (few && rows <= kFewRows && (rows <= 8 || red <= 4096) && (long long)rows * cols * red <= 240000000LL) return {0, 1, 0, 0};
   const long long chunks = red / kChunk, plane = (long long)rows * cols * 4;
   LinPlan best{64, 1, 0, LLONG_MAX};
   for (int t : {256, 128, 64}) {
@@ -1160,10 +1173,12 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   if constexpr (!TA && !TB) {
     if (p.tile == 0) {
       const unsigned blocks = (unsigned)((a.cols + 15) / 16);
-      if (a.rows <= 16)
-        linear_few_kernel<1, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
+      if (a.rows <= 8 && blocks * 4LL <= device_cu_count() * 5LL)
+        linear_few_kernel<1, 8, 8, 8, ACT><<<(unsigned)(a.cols / 8), 512, 0, s>>>(a);
+      else if (a.rows <= 16)
+        linear_few_kernel<1, 16, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
       else
-        linear_few_kernel<2, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
+        linear_few_kernel<2, 16, 8, 8, ACT><<<blocks, 512, 0, s>>>(a);
       return hipGetLastError();
     }
   }
