@@ -1047,12 +1047,12 @@ __global__ __launch_bounds__(64) void bias_join_kernel(const float* __restrict__
   const int c = (int)(blockIdx.x * 64 + threadIdx.x);
   if (c >= cols) return;
   float s = 0.0f;
-  for (int p = 0; p < P; p += 8) {  // eight loads in flight
-    float v[8];
+  for (int p = 0; p < P; p += 16) {  // sixteen loads in flight
+    float v[16];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = p + q < P ? part[(size_t)(p + q) * (size_t)cols + c] : 0.0f;
+    for (int q = 0; q < 16; ++q) v[q] = p + q < P ? part[(size_t)(p + q) * (size_t)cols + c] : 0.0f;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s += v[q];
+    for (int q = 0; q < 16; ++q) s += v[q];
   }
   db[c] = s;
 }
