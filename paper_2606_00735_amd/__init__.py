@@ -9,7 +9,9 @@ incremental swap solver), and an MXFP8 (FP8 E4M3 with E8M0 block
 scales) variant of the expert FFN. For training a router over frozen 4-bit
 experts there are an MXFP4 (E2M1) expert FFN, the balance and z losses with
 per-expert counts, and the gradients of the gate, the combine and the router's
-product. Every step runs in the
+product. Around the routed experts: routing by scores, groups and a balance bias,
+dense products with an epilogue (shared experts), dropout with a residual, and
+their gradients. Every step runs in the
 HIP kernels of ``libmoe.so`` (C ABI in ``include/moe.h``); this package only
 marshals torch tensors into those calls.
 """

@@ -203,8 +203,9 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 // experts in 64 bits.
 // 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64 bits, a wave each;
 // 37 us without the sort and with all uncertain rows done again; 13.6 us with the gaps in the
-// rounds and the keys moved through registers; 10.3-11.3 us so (one token 4.6 us), 1.7 TB/s: a
-// wave of four tokens has some thousand instructions, and all waves run at once.
+// rounds and the keys moved through registers; 10.3 us so, the logits in the last-level cache
+// (from memory 12.5; one token 4.5): a wave of four tokens has some thousand instructions, and
+// all waves run at once.
 // ---------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
