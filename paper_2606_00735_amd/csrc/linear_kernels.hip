@@ -1221,9 +1221,10 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
 // The activation's gradient by blocks of 32 columns x 256 rows: where they are for half the
 // CUs at most and the data are few (us, silu and gate and bias, otherwise / so: 333 x 1336 6.5 /
 // 5.0, 1024 x 2048 13.6 / 9.7, 1500 x 4096 24.0 / 19.5, 16384 x 8 32.8 / 7.6; 2048 x 4096 22.9 /
-// 24.8, 16384 x 2048 76 / 106: its rows of 64 bytes reach two thirds of the bandwidth).
+// 24.8, 16384 x 2048 76 / 106: its rows of 64 bytes reach two thirds of the bandwidth), and for
+// up to 128 columns, of which the other has lanes to spare (2^20 x 8 236 / 35, x 128 404 / 359).
 bool act_narrow(int rows, int cols) {
-  return 2 * ((cols - 1) / 32 + 1) <= device_cu_count() && (long long)rows * cols <= (6 << 20);
+  return 2 * ((cols - 1) / 32 + 1) <= device_cu_count() && (cols <= 128 || (long long)rows * cols <= (6 << 20));
 }
 
 // Row ranges of the bias' sums: one up to 768 or 1024 rows (a join takes 2 us), then 512 rows
@@ -1327,17 +1328,25 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     w.out32 = static_cast<float*>(c.dw);
   if (by_dw) w.row_sums = static_cast<float*>(ws);
   if (c.dx != nullptr && c.dw != nullptr && c.bf16) {
-    // In one launch where that is expected to take less than one after the other: all blocks
-    // at once, or those past two a CU after the shorter ones (768 x 2048 out of 333 rows
-    // 15.0 -> 10.8 us; 1336 x 1000 out of 1000 would be 24.1, and is 21.3).
+    // In one launch where that is expected to take less than one after the other. 64 x 64 tiles:
+    // all blocks at once, or those past two a CU after the shorter ones (768 x 2048 out of 333
+    // rows 15.0 -> 10.8 us). 128 x 128 tiles: a CU for each (1336 x 1000 out of 1000 rows 24.0 ->
+    // 15.9 us, 2048 x 768 out of 1500 25.7 -> 19.8, but out of 700 14.8 -> 19.2; two to a CU took
+    // 0.94 to 1.15 of what is done otherwise).
     const LinPlan px = linear_plan(x.rows, x.cols, x.red, false), pw = linear_plan(w.rows, w.cols, w.red, false);
-    auto tiles = [](const LinArgs& a) { return ((a.rows - 1LL) / 64 + 1) * ((a.cols - 1LL) / 64 + 1); };
-    const long long n = tiles(x) + tiles(w), slots = 2 * device_cu_count();
+    auto tiles = [](const LinArgs& a, int t) { return ((a.rows - 1LL) / t + 1) * ((a.cols - 1LL) / t + 1); };
+    const long long n = tiles(x, 64) + tiles(w, 64), n128 = tiles(x, 128) + tiles(w, 128), slots = 2 * device_cu_count();
     const long long tx = x.red / kChunk * 410LL + 3500, tw = w.red / kChunk * 410LL + 3500;
-    const long long together = n <= slots ? std::max(tx, tw) : std::max(std::max(tx, tw), std::min(tx, tw) + tw);
-    if (!by_dw && n <= 2 * slots && together < px.ns + pw.ns + 1000) {
+    const long long t64 = n <= slots       ? std::max(tx, tw)
+                          : n <= 2 * slots ? std::max(std::max(tx, tw), std::min(tx, tw) + tw)
+                                           : LLONG_MAX;
+    const long long t128 = 2 * n128 <= slots ? std::max(x.red, w.red) / kChunk * 590LL + 3000 : LLONG_MAX;
+    if (!by_dw && std::min(t64, t128) < px.ns + pw.ns + 1000) {
       x.S = w.S = 1;
-      linear_pair_kernel<64, 64, 2, 2, 4><<<(unsigned)n, 256, 0, s>>>(x, w, (unsigned)tiles(x));
+      if (t128 < t64)
+        linear_pair_kernel<128, 128, 2, 4, 4><<<(unsigned)n128, 512, 0, s>>>(x, w, (unsigned)tiles(x, 128));
+      else
+        linear_pair_kernel<64, 64, 2, 2, 4><<<(unsigned)n, 256, 0, s>>>(x, w, (unsigned)tiles(x, 64));
       return hipGetLastError();
     }
   }

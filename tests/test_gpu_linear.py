@@ -62,7 +62,9 @@ SIZES = [(1, 8, 8), (1, 72, 56), (2, 136, 1000), (17, 128, 64), (63, 264, 72), (
          (129, 1336, 1000), (300, 256, 4096), (16, 1024, 2048), (33, 520, 24), (257, 264, 192), (1000, 768, 256), (5, 2048, 8),
          (777, 1288, 520),
          # few rows: a partial k-step of 64 in either half, more columns than blocks of 8 are for, long reductions
-         (8, 72, 24), (7, 64, 104), (9, 64, 104), (3, 5128, 136), (8, 8, 8192), (12, 64, 4104), (4, 5136, 1032)]
+         (8, 72, 24), (7, 64, 104), (9, 64, 104), (3, 5128, 136), (8, 8, 8192), (12, 64, 4104), (4, 5136, 1032),
+         # gradients in one launch of large tiles, ragged in all dimensions
+         (1001, 1336, 1000), (700, 520, 2056)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
