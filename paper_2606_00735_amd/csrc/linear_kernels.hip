@@ -1328,20 +1328,23 @@ hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStre
     w.out32 = static_cast<float*>(c.dw);
   if (by_dw) w.row_sums = static_cast<float*>(ws);
   if (c.dx != nullptr && c.dw != nullptr && c.bf16) {
-    // In one launch where that is expected to take less than one after the other. 64 x 64 tiles:
-    // all blocks at once, or those past two a CU after the shorter ones (768 x 2048 out of 333
-    // rows 15.0 -> 10.8 us). 128 x 128 tiles: a CU for each (1336 x 1000 out of 1000 rows 24.0 ->
-    // 15.9 us, 2048 x 768 out of 1500 25.7 -> 19.8, but out of 700 14.8 -> 19.2; two to a CU took
-    // 0.94 to 1.15 of what is done otherwise).
+    // In one launch where that is expected to take less than one after the other, with their
+    // joins up to four launches, 5 us more than their own times. 64 x 64 tiles: all blocks at once (a
+    // chunk takes longer while both reductions run), or those past two a CU after the shorter ones
+    // (768 x 2048 out of 333 rows 15.0 -> 10.8 us, 2048 x 768 out of 100 17.1 -> 13.7). 128 x 128
+    // tiles: a CU for each (1336 x 1000 out of 1000 rows 24.0 -> 15.9 us, 2048 x 768 out of 1500
+    // 25.7 -> 19.8, but out of 700 14.8 -> 19.2; two to a CU took 0.94 to 1.15 of what is done
+    // otherwise).
     const LinPlan px = linear_plan(x.rows, x.cols, x.red, false), pw = linear_plan(w.rows, w.cols, w.red, false);
     auto tiles = [](const LinArgs& a, int t) { return ((a.rows - 1LL) / t + 1) * ((a.cols - 1LL) / t + 1); };
     const long long n = tiles(x, 64) + tiles(w, 64), n128 = tiles(x, 128) + tiles(w, 128), slots = 2 * device_cu_count();
     const long long tx = x.red / kChunk * 410LL + 3500, tw = w.red / kChunk * 410LL + 3500;
-    const long long t64 = n <= slots       ? std::max(tx, tw)
+    const long long cl = std::max(x.red, w.red) / kChunk, cs = std::min(x.red, w.red) / kChunk;
+    const long long t64 = n <= slots       ? cl * 300 + cs * 110 + 3500
                           : n <= 2 * slots ? std::max(std::max(tx, tw), std::min(tx, tw) + tw)
                                            : LLONG_MAX;
     const long long t128 = 2 * n128 <= slots ? std::max(x.red, w.red) / kChunk * 590LL + 3000 : LLONG_MAX;
-    if (!by_dw && std::min(t64, t128) < px.ns + pw.ns + 1000) {
+    if (!by_dw && std::min(t64, t128) < px.ns + pw.ns + 5000) {
       x.S = w.S = 1;
       if (t128 < t64)
         linear_pair_kernel<128, 128, 2, 4, 4><<<(unsigned)n128, 512, 0, s>>>(x, w, (unsigned)tiles(x, 128));
