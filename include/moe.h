@@ -697,7 +697,8 @@ moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask
  *   sigmoid, norm:   ... of scale r_j (dw_j - sum_i r_i dw_i) (1 - s_j)
  *   softmax:         s_e scale (sum over slots of e of dw_j - sum_i s_i dw_i)
  *   softmax, norm:   sum over slots of e of scale r_j (dw_j - sum_i r_i dw_i)
- * in fp32. Slots whose id is outside [0, E) add nothing. accumulate != 0 adds to what
+ * in fp32. Slots whose id is outside [0, E) add nothing; a token of such slots alone has the
+ * gradient 0, whatever its logits and dw hold. accumulate != 0 adds to what
  * dlogits holds (moe_gate_backward's gradient of the losses, say).
  *
  * logits [T, E], dw [T, k] fp32; ids [T, k] int32; dlogits [T, E] fp32, written completely;

@@ -73,6 +73,8 @@ def route_backward(logits, ids, dw, score="sigmoid", norm=True, scale=1.0):
         z = np.asarray(logits[t], np.float64)
         s = scores(z, score)
         slots = [(j, int(e)) for j, e in enumerate(ids[t]) if 0 <= e < E]
+        if not slots:  # no weight depends on these logits, whatever they hold
+            continue
         d = scale * np.array([float(dw[t, j]) for j, _ in slots])
         if norm:
             r = ratios([z[e] for _, e in slots], score)

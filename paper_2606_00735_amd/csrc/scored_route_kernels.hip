@@ -708,6 +708,9 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const float* __rest
   const float zs = slot ? z[row * E + id] : -INFINITY;
   float p[Q][4] = {};
   float val, common = 0.0f;  // what slot l adds to its expert's column
+  // A token without any expert has no gradient, whatever its logits hold (a softmax's NaN
+  // would pass through a product with 0).
+  const bool none = SOFT && !NORM && row_max(slot ? 1.0f : 0.0f) == 0.0f;
   if (SOFT && !NORM) {
     float m = -INFINITY, sum = 0.0f;
 #pragma unroll
@@ -783,7 +786,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const float* __rest
     float v[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      if (SOFT && !NORM) v[c] = p[q][c] * (v[c] - common);
+      if (SOFT && !NORM) v[c] = none ? 0.0f : p[q][c] * (v[c] - common);
     float* out = dz + row * E + e;
     if (vec) {
       if (e < E) {
