@@ -721,7 +721,8 @@ moe_status moe_route_backward(const float* logits, const int32_t* ids, const flo
  * x [M, K] dt; w [N, K] dt, rows ldw elements apart (0: K; otherwise as the expert
  * weights' strides); bias [N] fp32, mul and residual [M, N] dt: each may be NULL
  * y [M, N] dt; it may be mul or residual itself. z [M, N] dt or NULL: round_dt(z), what
- *   moe_linear_backward needs of a layer with an activation; not y
+ *   moe_linear_backward needs of a layer with an activation. Otherwise neither may share
+ *   memory with an input or with the other
  * ws: partial sums of products of few tiles, split along K and joined in a fixed order
  *   (results do not depend on timing). Its size depends on the device's compute units;
  *   it need not hold anything; calls that share one must not overlap.
@@ -747,7 +748,10 @@ moe_status moe_linear(const void* x, const void* w, const float* bias, const voi
  * dz [M, N] dt: required with an activation or mul (it may be dy itself), not written
  *   without; dmul [M, N] dt or NULL (NULL without mul; not dz, dy or mul)
  * dx [M, K] dt or NULL; dw [N, K] of dw_dt or NULL (fp32 data: fp32; bf16 data: either);
- * dbias [N] fp32 or NULL; no output overlaps another, but dz may be dy
+ * dbias [N] fp32 or NULL
+ * No output may share memory with another, nor with an input; but dz may be dy itself, and dz
+ * and dmul are written before the products, so that they may lie over x without dw and over
+ * w without dx, and dx and dw over z or mul.
  * ws and limits as moe_linear. M == 0 writes zeros to dw and dbias.
  */
 moe_status moe_linear_backward(const void* dy, const void* x, const void* w, const void* z, const void* mul,

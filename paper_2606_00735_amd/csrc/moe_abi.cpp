@@ -7,6 +7,7 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <numeric>
 #include <vector>
 
@@ -21,6 +22,24 @@ using moe::SlotMap;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Whether two operands share memory; an operand that is not there shares none.
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+bool shares(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x != 0 && y != 0 && a.bytes != 0 && b.bytes != 0 && x < y + b.bytes && y < x + a.bytes;
+}
+bool shares_any(const Span& a, std::initializer_list<Span> others) {
+  for (const Span& b : others)
+    if (shares(a, b)) return true;
+  return false;
+}
+// The same, but an operand may be the other one itself (read and written element by element).
+bool shares_part(const Span& a, const Span& b) { return a.p != b.p && shares(a, b); }
+
 bool valid_dtype(moe_dtype dt) { return dt == MOE_F32 || dt == MOE_BF16; }
 
 moe_status hip_status(hipError_t e) { return e == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
@@ -760,7 +779,12 @@ moe_status moe_linear(const void* x, const void* w, const float* bias, const voi
   }
   if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
   if (M == 0) return MOE_OK;
-  if (!x || !w || !y || y == x || y == w || (z && (z == y || z == x || z == w || z == mul || z == residual)))
+  if (!x || !w || !y) return MOE_ERR_INVALID_ARG;
+  const size_t es = dt == MOE_BF16 ? 2 : 4, mn = (size_t)M * N * es;
+  const Span sx{x, (size_t)M * K * es}, sw{w, ((size_t)(N - 1) * ld + K) * es}, sb{bias, (size_t)N * 4}, sm{mul, mn},
+      sr{residual, mn}, sy{y, mn}, sz{z, mn};
+  if (shares_any(sy, {sx, sw, sb, sz}) || shares_part(sy, sm) || shares_part(sy, sr) ||
+      shares_any(sz, {sx, sw, sb, sm, sr}))
     return MOE_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(mul) || !aligned16(residual) || !aligned16(y) ||
       !aligned16(z) || !aligned16(ws))
@@ -786,17 +810,23 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
   if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(z) || !aligned16(mul) || !aligned16(dz) ||
       !aligned16(dmul) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias) || !aligned16(ws))
     return MOE_ERR_INVALID_ARG;
+  const bool own = act != MOE_ACT_NONE || mul != nullptr;
   if (M > 0) {
-    const bool own = act != MOE_ACT_NONE || mul != nullptr;
     if (!dy || (dx && !w) || (dw && !x) || (own && !dz) || (dmul && !mul) ||
         ((act != MOE_ACT_NONE || dmul) && !z))
       return MOE_ERR_INVALID_ARG;
-    if ((dmul && (dmul == dz || dmul == dy || dmul == mul || dmul == z)) || (own && (dz == z || dz == mul)))
-      return MOE_ERR_INVALID_ARG;
-    for (const void* in : {dy, x, w, (const void*)(own ? dz : nullptr)})
-      if (in && (dx == in || dw == in)) return MOE_ERR_INVALID_ARG;
   }
-  if ((dx && (dx == dw || dx == dmul || dx == dbias)) || (dw && (dw == dmul || dw == dbias))) return MOE_ERR_INVALID_ARG;
+  const size_t es = dt == MOE_BF16 ? 2 : 4, mn = (size_t)M * N * es, mk = (size_t)M * K * es, nk = (size_t)N * K;
+  const Span sdy{dy, mn}, sx{x, mk}, sw{w, ((size_t)(N - 1) * ld + K) * es}, sz{z, mn}, sm{mul, mn},
+      sdz{own ? dz : nullptr, mn}, sdm{dmul, mn}, sdx{dx, mk}, sdw{dw, nk * (dw_dt == MOE_BF16 ? 2 : 4)},
+      sdb{dbias, (size_t)N * 4}, none{nullptr, 0};
+  // The pass that writes dz, dmul and the bias' sums comes first and reads dy, z and mul, each
+  // element before it is written; the products then read x and w.
+  if (shares_any(sdb, {sdy, sx, sw, sz, sm, sdz, sdm, sdx, sdw}) || shares_part(sdz, sdy) ||
+      shares_any(sdz, {sz, sm, sdm, dw ? sx : none, dx ? sw : none}) ||
+      shares_any(sdm, {sdy, sz, sm, dw ? sx : none, dx ? sw : none}) ||
+      shares_any(sdx, {sdy, sx, sw, sdz, sdm, sdw}) || shares_any(sdw, {sdy, sx, M > 0 ? sw : none, sdz, sdm}))
+    return MOE_ERR_INVALID_ARG;
   moe::LinearBackwardCall c{dy, x, w, z, mul, M, N, K, ld, (int)act, dt == MOE_BF16, dw_dt == MOE_BF16, dz, dmul, dx,
                             dw, dbias};
   return hip_status(moe::launch_linear_backward(c, ws, stream));
