@@ -680,7 +680,8 @@ moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_ro
  * NaN weights; its ids are of its other experts.
  *
  * logits [T, E] fp32; bias [E] fp32 or NULL; mask [T] uint8 or NULL (all live)
- * ids [T, k] int32, w [T, k] fp32: written completely
+ * ids [T, k] int32, w [T, k] fp32: written completely; they may share memory neither with
+ *   an input nor with each other
  * Limits: 1 <= E <= 256, n_group divides E, 1 <= topk_group <= n_group,
  * 1 <= k <= min(topk_group * E / n_group, 16), scale finite in fp32, T * E <= 2^40.
  */
@@ -702,7 +703,7 @@ moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask
  * dlogits holds (moe_gate_backward's gradient of the losses, say).
  *
  * logits [T, E], dw [T, k] fp32; ids [T, k] int32; dlogits [T, E] fp32, written completely;
- * it must not overlap logits or dw. Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), scale
+ * it must not overlap logits, ids or dw. Limits: 1 <= E <= 256, 1 <= k <= min(E, 16), scale
  * finite in fp32, T * E <= 2^40.
  */
 moe_status moe_route_backward(const float* logits, const int32_t* ids, const float* dw, int T, int E, int k,
@@ -769,7 +770,8 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
  * elements uses ceil(n / 4) counters: the caller moves offset on between calls that are to
  * differ.
  *
- * x, residual (or NULL), out [n] dt; out may be x or residual itself
+ * x, residual (or NULL), out [n] dt; out may be x or residual itself, but not a part of
+ *   either, nor of rng
  * rng [2] uint64 (DEVICE): seed, offset; read when the call runs, so a captured call takes
  *   what a replay finds there
  * Limits: 0 <= p < 1, n <= 2^40. n == 0 is a no-op.

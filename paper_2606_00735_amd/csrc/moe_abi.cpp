@@ -733,6 +733,9 @@ moe_status moe_route(const float* logits, const float* bias, const uint8_t* mask
   if (T == 0) return MOE_OK;
   if (!logits || !ids || !w || !aligned16(logits) || !aligned4(bias) || !aligned4(ids) || !aligned4(w))
     return MOE_ERR_INVALID_ARG;
+  const Span sz{logits, (size_t)T * E * 4}, sb{bias, (size_t)E * 4}, sm{mask, (size_t)T}, si{ids, (size_t)T * k * 4},
+      sw{w, (size_t)T * k * 4};
+  if (shares_any(si, {sz, sb, sm, sw}) || shares_any(sw, {sz, sb, sm})) return MOE_ERR_INVALID_ARG;
   return hip_status(moe::launch_route(logits, bias, mask, T, E, k, score == MOE_SOFTMAX, n_group, topk_group, norm != 0,
                                       scale, ids, w, stream));
 }
@@ -746,8 +749,10 @@ moe_status moe_route_backward(const float* logits, const int32_t* ids, const flo
   if ((long long)T * E > (1LL << 40)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!logits || !ids || !dw || !dlogits || !aligned16(logits) || !aligned16(dlogits) || !aligned4(ids) ||
-      !aligned4(dw) || dlogits == logits || dlogits == dw)
+      !aligned4(dw))
     return MOE_ERR_INVALID_ARG;
+  const size_t te = (size_t)T * E * 4, tk = (size_t)T * k * 4;
+  if (shares_any({dlogits, te}, {{logits, te}, {ids, tk}, {dw, tk}})) return MOE_ERR_INVALID_ARG;
   return hip_status(moe::launch_route_backward(logits, ids, dw, T, E, k, score == MOE_SOFTMAX, norm != 0, (float)scale,
                                                accumulate != 0, dlogits, stream));
 }
@@ -839,6 +844,10 @@ moe_status moe_dropout_add(const void* x, const void* residual, long long n, dou
   if (n == 0) return MOE_OK;
   if (!x || !rng || !out || !aligned16(x) || !aligned16(residual) || !aligned16(out) ||
       (reinterpret_cast<uintptr_t>(rng) & 7u) != 0)
+    return MOE_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)n * (dt == MOE_BF16 ? 2 : 4);
+  const Span so{out, bytes};
+  if (shares_part(so, {x, bytes}) || shares_part(so, {residual, bytes}) || shares(so, {rng, 2 * sizeof(uint64_t)}))
     return MOE_ERR_INVALID_ARG;
   // p < 1, so the threshold is below 2^32
   return hip_status(moe::launch_dropout(x, residual, rng, n, (uint32_t)std::floor(p * 4294967296.0),
