@@ -671,7 +671,8 @@ moe_status moe_router_grad(const float* dlogits, const void* x, const void* w_ro
  *              values go to the lower group and the lower expert id
  *   w[t,j]   = scale * s_j, or with norm scale * s_j / sum of the selected s (a ratio
  *              that selected scores have where they underflow, too)
- * Experts are selected as by s and c in 64 bits; w is fp32, off by a few roundings.
+ * Experts are selected as by s and c in 64 bits; w is computed in 64 bits and rounded to fp32
+ * once.
  *
  * An expert whose logit is -inf, or whose c is -inf or NaN, is not selected (a -inf
  * takes part in a softmax with 0). A slot for which no expert is left, and every slot of a

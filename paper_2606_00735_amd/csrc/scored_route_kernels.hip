@@ -8,7 +8,8 @@
 //
 // Which of two scores is larger decides whole numbers, so s and c that decide are held in
 // 64 bits: c's of different experts come as near as fp32 rounds them a few times in a
-// batch of 16384 tokens. The weights are fp32 (a few roundings each).
+// batch of 16384 tokens. The weights of what is selected are computed in 64 bits as well and
+// rounded to fp32 once.
 #include <math.h>
 
 #include <algorithm>
@@ -241,8 +242,16 @@ __device__ __forceinline__ float row_sum(float x) {
   return row_reduce(x, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ double row_sum64(double x) {
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1) x += shfl_xor_f64(x, m);
+  auto plus = [&](auto step) {
+    constexpr int C = decltype(step)::value;
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    const uint64_t o = (uint64_t)dpp_u32<C>((uint32_t)u) | ((uint64_t)dpp_u32<C>((uint32_t)(u >> 32)) << 32);
+    x += __longlong_as_double((long long)o);
+  };
+  plus(std::integral_constant<int, 0xB1>{});   // as row_reduce
+  plus(std::integral_constant<int, 0x4E>{});
+  plus(std::integral_constant<int, 0x141>{});
+  plus(std::integral_constant<int, 0x140>{});
   return x;
 }
 
@@ -451,6 +460,17 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     inv = __builtin_amdgcn_rcpf(sum);
     top = inv;
   }
+  // The softmax's sum in 64 bits (over e^hi): weights that are not normed need it, c's beside a
+  // bias where they decide.
+  double total = 1.0;
+  bool have_total = false;
+  if (SOFT && !a.norm) {
+    have_total = true;
+    total = 0.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) total += z[v] > -INFINITY ? exp((double)z[v] - (double)hi) : 0.0;
+    total = row_sum64(total);
+  }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float c = SOFT ? exp_fast(z[v] - hi) * inv : __builtin_amdgcn_rcpf(1.0f + exp_fast(-z[v]));
@@ -465,8 +485,6 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
   };
   sort_keys<V>(key);
   // c of an expert in 64 bits. A softmax's sum counts beside a bias only.
-  double total = 1.0;
-  bool have_total = false;
   auto exact = [&](int e) {
     const double zd = (double)row[e];
     const double sc = SOFT ? exp(zd - (double)hi) / total : 1.0 / (1.0 + exp(-zd));
@@ -654,23 +672,26 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     if (!ok) id = id64, zs = zs64;
   }
   if (!live) id = -1;
-  // Weights in fp32, by one formula whatever path has selected: a few roundings each (36
-  // at most, and those of arguments).
+  // Weights in 64 bits, by one formula whatever path has selected, rounded once (in fp32 they
+  // were off by one or two roundings more; it costs 0.3 us of 16384 x 256, and 4.8 where the softmax's
+  // sum has to be in 64 bits, too: 8.1 -> 12.9 without groups, as many exponentials as scores).
   const bool slot = l < a.k && id >= 0;
-  float x;
+  double x, sum = 1.0;
   if (a.norm) {
     const float m = row_max(slot ? zs : -INFINITY);
-    x = slot ? relative_score<SOFT, float>(zs, m) : 0.0f;
-    const float sum = row_sum(x);
-    x = slot ? x / sum * (float)a.scale : 0.0f;
+    x = slot ? relative_score<SOFT, double>(zs, m) : 0.0;
+    sum = row_sum64(x);
+  } else if (SOFT) {
+    x = exp((double)zs - (double)hi);
+    sum = total;
   } else {
-    x = SOFT ? expf(zs - hi) * inv : relative_score<false, float>(zs, 0.0f);
-    x = slot ? x * (float)a.scale : 0.0f;
+    x = 1.0 / (1.0 + exp(-(double)zs));
   }
+  x = slot ? x / sum * a.scale : 0.0;
   if (bad && live) x = NAN;
   if (l < a.k && t < a.T) {
     a.ids[r * a.k + l] = id;
-    a.w[r * a.k + l] = x;
+    a.w[r * a.k + l] = (float)x;
   }
 }
 
