@@ -783,7 +783,7 @@ def moe_route_backward(logits, ids, dweights, score="sigmoid", norm=True, scale=
 
 
 def linear_ws_bytes(M, N, K, dtype):
-    """Bytes of moe_linear's workspace."""
+    """Bytes of a workspace for moe_linear with at most M rows."""
     n = ctypes.c_size_t(0)
     dt = MOE_BF16 if dtype == torch.bfloat16 else MOE_F32
     _check("moe_linear", load_library().moe_linear(None, None, None, None, None, M, N, K, 0, 0, dt, None, None, None,
@@ -792,7 +792,7 @@ def linear_ws_bytes(M, N, K, dtype):
 
 
 def linear_backward_ws_bytes(M, N, K, dtype):
-    """Bytes of moe_linear_backward's workspace."""
+    """Bytes of a workspace for moe_linear_backward with at most M rows."""
     n = ctypes.c_size_t(0)
     dt = MOE_BF16 if dtype == torch.bfloat16 else MOE_F32
     _check("moe_linear_backward", load_library().moe_linear_backward(

@@ -120,7 +120,9 @@ struct LinearCall {
   bool bf16;
   void *y, *z;
 };
+// Workspaces: enough for every call of at most M rows, and what a call of M rows needs.
 size_t linear_ws_bytes(int M, int N, int K, bool bf16);
+size_t linear_ws_needed(int M, int N, int K, bool bf16);
 hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s);
 struct LinearBackwardCall {
   const void *dy, *x, *w, *z, *mul;
@@ -130,6 +132,7 @@ struct LinearBackwardCall {
   float* dbias;
 };
 size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16);
+size_t linear_backward_ws_needed(int M, int N, int K, bool bf16);
 hipError_t launch_linear_backward(const LinearBackwardCall& c, void* ws, hipStream_t s);
 
 // Dropout with a residual (dropout_kernels.hip): rng holds the seed and the first

@@ -1150,6 +1150,14 @@ size_t product_ws(int rows, int cols, int red, bool few, bool bf16) {
   return p.S > 1 ? (size_t)p.S * (size_t)rows * (size_t)cols * 4 : 0;
 }
 
+// The most that product_ws asks for up to these rows, cols and red: of fewer rows a product may be
+// cut in more ranges (4096 out of 14336: none for 16384 rows, 64 MB for 1024).
+size_t product_ws_up_to(int rows, int cols, int red, bool bf16) {
+  const long long ranges = std::min(16, red / kChunk / 4);
+  if (!bf16 || ranges < 2) return 0;
+  return (size_t)std::min((long long)kLinPartBytes, ranges * rows * cols * 4);
+}
+
 template <bool TA, bool TB, int ACT>
 hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
   if (!bf16) {
@@ -1238,6 +1246,14 @@ int bias_ranges(int rows, int cols) {
   return std::max(2, std::min((4 * device_cu_count() + cb - 1) / cb, rows / 128));
 }
 
+// The most ranges for up to these rows.
+int bias_ranges_up_to(int rows, int cols) {
+  const int few = (cols - 1) / 32 + 1, cb = (cols - 1) / 256 + 1, cus = device_cu_count();
+  int most = rows > 1024 ? std::max(2, std::min((4 * cus + cb - 1) / cb, rows / 128)) : 1;
+  if (2 * few <= cus && rows > 768) most = std::max(most, std::min((rows - 1) / 512 + 1, cus / few));
+  return most;
+}
+
 // Parts of the bias' sums where dw's large tiles make them (0: they do not): dz is dy, and
 // the tiles read all of it.
 int bias_parts_of_dw(int M, int N, int K, bool bf16) {
@@ -1253,7 +1269,12 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // Never 0: a call without a workspace asks for its size.
 constexpr size_t kLinearWsLeast = 256;
 
-size_t linear_ws_bytes(int M, int N, int K, bool bf16) { return std::max(kLinearWsLeast, product_ws(M, N, K, true, bf16)); }
+size_t linear_ws_bytes(int M, int N, int K, bool bf16) {
+  return std::max(kLinearWsLeast, product_ws_up_to(M, N, K, bf16));
+}
+size_t linear_ws_needed(int M, int N, int K, bool bf16) {
+  return std::max(kLinearWsLeast, product_ws(M, N, K, true, bf16));
+}
 
 hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
   LinArgs a{};
@@ -1264,6 +1285,15 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t s) {
 }
 
 size_t linear_backward_ws_bytes(int M, int N, int K, bool bf16) {
+  if (M == 0) return kLinearWsLeast;
+  // dw's sums have the same size whatever the rows: as many ranges as that allows
+  const size_t plane = (size_t)N * (size_t)K * 4;
+  const size_t dw = std::min(product_ws_up_to(N, K, M, bf16), kLinPartBytes / plane * plane);
+  const int parts = bf16 ? 2 * ((K - 1) / 256 + 1) : 0;
+  return align256((size_t)std::max(bias_ranges_up_to(M, N), parts) * (size_t)N * 4) +
+         std::max(product_ws_up_to(M, K, N, bf16), dw);
+}
+size_t linear_backward_ws_needed(int M, int N, int K, bool bf16) {
   if (M == 0) return kLinearWsLeast;
   return align256((size_t)std::max(bias_ranges(M, N), bias_parts_of_dw(M, N, K, bf16)) * (size_t)N * 4) +
          std::max(product_ws(M, K, N, false, bf16), product_ws(N, K, M, false, bf16));

@@ -777,12 +777,11 @@ moe_status moe_linear(const void* x, const void* w, const float* bias, const voi
   const moe_status st = linear_shape_ok(M, N, K, ldw, act, dt, &ld);
   if (st != MOE_OK) return st;
   if (ws_bytes == nullptr) return MOE_ERR_INVALID_ARG;
-  const size_t need = moe::linear_ws_bytes(M, N, K, dt == MOE_BF16);
   if (ws == nullptr) {
-    *ws_bytes = need;
+    *ws_bytes = moe::linear_ws_bytes(M, N, K, dt == MOE_BF16);
     return MOE_OK;
   }
-  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (*ws_bytes < moe::linear_ws_needed(M, N, K, dt == MOE_BF16)) return MOE_ERR_WORKSPACE;
   if (M == 0) return MOE_OK;
   if (!x || !w || !y) return MOE_ERR_INVALID_ARG;
   const size_t es = dt == MOE_BF16 ? 2 : 4, mn = (size_t)M * N * es;
@@ -806,12 +805,11 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
   const moe_status st = linear_shape_ok(M, N, K, ldw, act, dt, &ld);
   if (st != MOE_OK) return st;
   if (ws_bytes == nullptr || !valid_dtype(dw_dt) || (dt == MOE_F32 && dw_dt != MOE_F32)) return MOE_ERR_INVALID_ARG;
-  const size_t need = moe::linear_backward_ws_bytes(M, N, K, dt == MOE_BF16);
   if (ws == nullptr) {
-    *ws_bytes = need;
+    *ws_bytes = moe::linear_backward_ws_bytes(M, N, K, dt == MOE_BF16);
     return MOE_OK;
   }
-  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
+  if (*ws_bytes < moe::linear_backward_ws_needed(M, N, K, dt == MOE_BF16)) return MOE_ERR_WORKSPACE;
   if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(z) || !aligned16(mul) || !aligned16(dz) ||
       !aligned16(dmul) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias) || !aligned16(ws))
     return MOE_ERR_INVALID_ARG;
