@@ -745,12 +745,14 @@ def moe_route(logits, k, score="sigmoid", bias=None, mask=None, n_group=1, topk_
               weights=None):
     """Experts and gate weights from scores of the logits [T, E]: sigmoid or softmax, a bias
     [E] that counts for the selection only, the topk_group best of n_group groups, top-k,
-    weights normalised (norm) and scaled. mask [T] uint8: 0 for tokens that get id -1 and
-    weight 0. Returns (ids [T, k] int32, weights [T, k] fp32)."""
+    weights normalised (norm) and scaled. mask [T] (bool or uint8): 0 for tokens that get id -1
+    and weight 0. Returns (ids [T, k] int32, weights [T, k] fp32)."""
     L = load_library()
     T, E = _matrix(logits, "logits")
     dev = torch.cuda.current_device()
     code = _code(SCORES, score, "score")
+    if isinstance(mask, torch.Tensor) and mask.dtype is torch.bool:
+        mask = mask.view(torch.uint8)
     if ids is None:
         ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
     if weights is None:
