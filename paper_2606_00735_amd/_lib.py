@@ -481,7 +481,8 @@ def moe_layer(x, w_router, bias, k, expert_map, w_gate, w_up, w_down, logits=Fal
     x_perm is not built (None in the result); every other output is the same.
     ``route`` (a dict of moe_route's score, n_group, topk_group, norm, scale and mask)
     selects by moe_route on the router's product; ``bias`` then counts for the selection
-    only.
+    only, and the logits are always part of the result. ``logits``: True for them, or a
+    tensor [T, E] that receives them.
     """
     b = {} if bufs is None else bufs
     T = x.shape[0]
@@ -494,11 +495,17 @@ def moe_layer(x, w_router, bias, k, expert_map, w_gate, w_up, w_down, logits=Fal
         ids, wts, lg = moe_gate_topk(x, w_router, bias, k, logits=logits, ids=b.get("ids"),
                                      weights=b.get("weights"), ws=gws)
     else:
-        top, top_w, lg = moe_gate_topk(x, w_router, None, 1, logits=b.get("logits", True), ids=b.get("top"),
-                                       weights=b.get("top_w"), ws=gws)
+        mine = isinstance(logits, torch.Tensor)
+        lg = logits if mine else b.get("logits", True)
+        for name, t, shape in (("logits", lg, (T, E)), ("top", b.get("top"), (T, 1)), ("top_w", b.get("top_w"), (T, 1))):
+            if isinstance(t, torch.Tensor) and t.shape != shape:
+                raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        top, top_w, lg = moe_gate_topk(x, w_router, None, 1, logits=lg, ids=b.get("top"), weights=b.get("top_w"), ws=gws)
         ids, wts = moe_route(lg, k, bias=bias, ids=b.get("ids"), weights=b.get("weights"), **route)
         if bufs is not None:
-            bufs.update(logits=lg, top=top, top_w=top_w)
+            bufs.update(top=top, top_w=top_w)
+            if not mine:  # a caller's tensor stays with its call
+                bufs["logits"] = lg
     counts, offsets, hws = moe_expert_histogram_scan(ids, E, expert_map, ws=b.get("hist_ws"),
                                                      counts=b.get("counts"), offsets=b.get("offsets"))
     x_perm, perm_src, dest = moe_permute(x, ids, expert_map, hws, x_perm=b.get("x_perm"),

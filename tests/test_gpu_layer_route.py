@@ -1,6 +1,6 @@
 """GPU tests of moe_layer(route=...) as a program calls it: bf16 and fp32, sizes of the
-library's workloads, the fused gather, boolean masks. Its outputs are those of its own steps called one by one, so they
-are compared bit for bit; ids and weights are the oracle's on the logits that it used."""
+library's workloads, the fused gather, boolean masks, a caller's buffer for the logits. Its outputs
+are those of its own steps called one by one, so they are compared bit for bit; ids and weights are the oracle's on the logits that it used."""
 import numpy as np
 import pytest
 import torch
@@ -91,3 +91,34 @@ def test_boolean_masks():
         moe.moe_route(z, 4, mask=mask[:49])
     with pytest.raises(ValueError):
         moe.moe_route(z, 4, mask=mask.int())
+
+
+@pytest.mark.parametrize("bufs", [False, True])
+def test_logits_go_to_the_callers_buffer(bufs):
+    """As without route: logits may be a tensor that receives them."""
+    print("CASE routed layer logits", bufs, flush=True)
+    t = make(40, 128, 256, 16, BF)
+    mine = torch.full((40, 16), 7.0, device=DEV)
+    kept = {} if bufs else None
+    if bufs:
+        layer(t, 4, route=ROUTE, bufs=kept)
+    r = layer(t, 4, route=ROUTE, logits=mine, bufs=kept)
+    want = steps(t, 4, ROUTE)["logits"]
+    assert r["logits"] is mine and torch.equal(mine, want)
+    if bufs:  # and stay the caller's: a later call without it does not write there
+        t["x"].mul_(2.0)
+        after = layer(t, 4, route=ROUTE, bufs=kept)["logits"]
+        assert after is not mine and torch.equal(mine, want) and not torch.equal(after, want)
+
+
+def test_buffers_of_another_batch_are_refused():
+    """Before anything is launched that would write past their ends."""
+    print("CASE routed layer other batch", flush=True)
+    t, kept = make(40, 128, 256, 16, BF), {}
+    layer(t, 4, route=ROUTE, bufs=kept)
+    for T in (39, 41):
+        other = {**t, "x": make(T, 128, 256, 16, BF)["x"]}
+        with pytest.raises(ValueError, match="logits"):
+            layer(other, 4, route=ROUTE, bufs=kept)
+        with pytest.raises(ValueError, match="logits"):
+            layer(other, 4, route=ROUTE, logits=torch.empty((40, 16), device=DEV))
