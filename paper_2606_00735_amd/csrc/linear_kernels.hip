@@ -47,16 +47,28 @@ __device__ __forceinline__ float normal_below(float z) {
   return z >= 0.0f ? 1.0f - q : q;
 }
 
-template <int ACT>
+// F32: the data are fp32, whose silu is to be exact at any size of z (5 u of the value, a step being
+// 2 u): by an exponential of -|z| itself, which neither overflows nor rounds its argument, and true
+// quotients. Of bf16 data a value is rounded by up to 2^-8 of itself; sigmoid32's argument, rounded
+// before the exponential, moves it by |z| 2^-24.
+template <int ACT, bool F32 = false>
 __device__ __forceinline__ float act_value(float z) {
   if (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
+  if (ACT == kActSilu && F32) {
+    const float e = expf(-fabsf(z));
+    return (z < 0.0f ? z * e : z) / (1.0f + e);
+  }
   if (ACT == kActSilu) return z * sigmoid32(z);
   if (ACT == kActGelu) return z * normal_below(z);
   return z;
 }
-template <int ACT>
+template <int ACT, bool F32 = false>
 __device__ __forceinline__ float act_slope(float z) {
   if (ACT == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+  if (ACT == kActSilu && F32) {
+    const float e = expf(-fabsf(z)), large = 1.0f / (1.0f + e), small = e * large;
+    return z < 0.0f ? small * (1.0f + z * large) : large * (1.0f + z * small);
+  }
   if (ACT == kActSilu) {
     const float q = sigmoid32(z);
     return q * (1.0f + z * (1.0f - q));
@@ -936,7 +948,7 @@ __global__ __launch_bounds__(256) void linear_f32_kernel(LinArgs a) {
       float v = acc[i][j];
       if (a.bias != nullptr) v += a.bias[col];
       if (a.z != nullptr) static_cast<float*>(a.z)[at] = v;
-      v = act_value<ACT>(v);
+      v = act_value<ACT, true>(v);
       if (a.mul != nullptr) v *= static_cast<const float*>(a.mul)[at];
       if (a.res != nullptr) v += static_cast<const float*>(a.res)[at];
       (a.out32 != nullptr ? a.out32 : static_cast<float*>(a.out))[at] = v;
@@ -1012,13 +1024,13 @@ __global__ __launch_bounds__(L* R) void act_backward_kernel(ActBackwardArgs a) {
         if (a.dmul != nullptr) {
           float f[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] = d[g][q] * act_value<ACT>(z[g][q]);
+          for (int q = 0; q < 8; ++q) f[q] = d[g][q] * act_value<ACT, !BF16>(z[g][q]);
           store(a.dmul, at, f);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           if (a.mul != nullptr) d[g][q] *= m[g][q];
-          if (ACT != kActNone) d[g][q] *= act_slope<ACT>(z[g][q]);
+          if (ACT != kActNone) d[g][q] *= act_slope<ACT, !BF16>(z[g][q]);
           db[q] += d[g][q];
         }
         if (a.dz != nullptr) store(a.dz, at, d[g]);
