@@ -41,8 +41,8 @@ __device__ __forceinline__ double shfl_f64(double v, int l) {
 template <bool SOFT, class F>
 __device__ __forceinline__ F relative_score(float z, float m) {
   if (SOFT) return exp((F)z - (F)m);
-  if (z > 0.0f) return (F)1 / ((F)1 + exp(-(F)z));
-  return exp((F)z - (F)fminf(m, 0.0f)) / ((F)1 + exp((F)z));
+  const F over = exp((F)z - (F)fminf(m, 0.0f)), e = exp(z > 0.0f ? -(F)z : (F)z);  // without a branch: side by side
+  return (z > 0.0f ? (F)1 : over) / ((F)1 + e);
 }
 
 // The best (value, index) of a wave: the largest value, the lowest index of equal ones.
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
     have_total = true;
     total = 0.0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) total += z[v] > -INFINITY ? exp((double)z[v] - (double)hi) : 0.0;
+    for (int v = 0; v < V; ++v) total += exp(fmax((double)z[v] - (double)hi, -800.0));  // 0 of -inf, without a branch
     total = row_sum64(total);
   }
 #pragma unroll
@@ -673,8 +673,9 @@ __global__ __launch_bounds__(256) void route_rows_kernel(RouteArgs a) {
   }
   if (!live) id = -1;
   // Weights in 64 bits, by one formula whatever path has selected, rounded once (in fp32 they
-  // were off by one or two roundings more; it costs 0.3 us of 16384 x 256, and 4.8 where the softmax's
-  // sum has to be in 64 bits, too: 8.1 -> 12.9 without groups, as many exponentials as scores).
+  // were off by one or two roundings more; it costs 0.2 us of 16384 x 256, and 3.0 where the softmax's
+  // sum has to be in 64 bits, too: 7.9 -> 10.9 without groups, as many exponentials as scores; 12.9
+  // with a branch around each).
   const bool slot = l < a.k && id >= 0;
   double x, sum = 1.0;
   if (a.norm) {
