@@ -31,7 +31,7 @@ __device__ __forceinline__ float sigmoid32(float z) {
 __device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(z * z * -0.7213475204f); }
 // The normal distribution's integral up to z. Its small side is exp(-z^2 / 2) R(|z|), R
 // smooth: a polynomial of degree 8 in t = 1 / (1 + 0.3 |z|), fitted for the least largest
-// relative error over [0, 14], 1.5e-7, 4.8e-7 in fp32 (a call of erfcf cost an epilogue of
+// relative error over [0, 14], 1.7e-7 with its constants in fp32, 4.8e-7 computed in fp32 (a call of erfcf cost an epilogue of
 // 16384 x 2048 values 50 us).
 __device__ __forceinline__ float normal_below(float z) {
   const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(z), 1.0f));
@@ -826,9 +826,12 @@ __global__ __launch_bounds__(256) void linear_big_kernel(LinArgs a) {
 //
 // C = 8, for at most 8 rows: the MFMA's 16 columns are those 8 over two halves of a k-step of
 // 64, its 16 rows the 8 over the same halves; the two of the four products whose halves agree
-// are added. A load then takes whole lines, and there are twice the blocks: one row of 5120 x
-// 8192 25.8 -> 18.1 us (4.6 TB/s), of 2048 x 7168 11.9 -> 7.9, but of 7168 x 2048, whose 448
-// blocks of 16 columns run at once and whose 896 do not, 8.2 -> 9.1.
+// are added. A load then takes whole lines, and there are twice the blocks. Taken up to 5120
+// columns on 256 CUs, whatever the reduction (us, 16 columns / 8; one row: 2048 out of 8192 12.8 /
+// 8.6, 4096 16.7 / 13.9, 5120 25.6 / 18.1, 4.6 TB/s, 2048 out of 2048 4.6 / 4.1; 8 rows: 2048 out of
+// 8192 16.3 / 11.2, 5120 out of 2048 9.0 / 10.0). Beyond, it loses with short reductions (7168 out
+// of 2048 8.0 / 8.8, 14336 13.1 / 15.2) and would win with long ones of one row (7168 out of 8192
+// 27.5 / 23.5, 14336 49.8 / 41.3).
 // ---------------------------------------------------------------------------
 template <int MB, int C, int W, int G, int ACT>
 __global__ __launch_bounds__(W* kWave) void linear_few_kernel(LinArgs a) {
@@ -1239,8 +1242,8 @@ hipError_t launch_product(LinArgs a, bool bf16, void* ws, hipStream_t s) {
 }
 
 // The activation's gradient by blocks of 32 columns x 256 rows: where they are for half the
-// CUs at most and the data are few (us, silu and gate and bias, otherwise / so: 333 x 1336 6.5 /
-// 5.0, 1024 x 2048 13.6 / 9.7, 1500 x 4096 24.0 / 19.5, 16384 x 8 32.8 / 7.6; 2048 x 4096 22.9 /
+// CUs at most and the data are few (us in a captured graph, silu and gate and bias, otherwise /
+// so: 333 x 1336 6.5 / 4.8, 1024 x 2048 13.6 / 9.7, 1500 x 4096 24.0 / 19.5, 16384 x 8 32.8 / 7.6; 2048 x 4096 22.9 /
 // 24.8, 16384 x 2048 76 / 106: its rows of 64 bytes reach two thirds of the bandwidth), and for
 // up to 128 columns, of which the other has lanes to spare (2^20 x 8 236 / 35, x 128 404 / 359).
 bool act_narrow(int rows, int cols) {

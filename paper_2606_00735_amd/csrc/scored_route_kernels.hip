@@ -186,8 +186,9 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 }
 
 // ---------------------------------------------------------------------------
-// Sixteen lanes a token, lane l the experts l V .. l V + V - 1, where groups are whole
-// lanes (1, 2, 4, 8 or 16 of them) or there is one group.
+// Sixteen lanes a token, lane l the experts l V .. l V + V - 1: any number of experts without
+// groups, and groups of one, two, four, eight or sixteen whole lanes of 1, 2, 4, 8, 10, 12 or 16
+// experts (lane_experts).
 //
 // The selection runs on 32-bit keys: c in fp32 (an exponential and a reciprocal of 1 ulp),
 // mapped to integers in the same order, the lowest 4 bits replaced by the position in the
@@ -204,9 +205,9 @@ __global__ __launch_bounds__(kTokens* kWave) void route_kernel(const float* __re
 // experts in 64 bits.
 // 16384 tokens x 256 experts, 4 of 8 groups: 61 us with every row in 64 bits, a wave each;
 // 37 us without the sort and with all uncertain rows done again; 13.6 us with the gaps in the
-// rounds and the keys moved through registers; 10.3 us so, the logits in the last-level cache
-// (from memory 12.5; one token 4.5): a wave of four tokens has some thousand instructions, and
-// all waves run at once.
+// rounds and the keys moved through registers; 11.4-11.8 us so, the logits in the last-level
+// cache (from memory 13.0; one token 4.7). A wave of four tokens has 960 vector instructions, four
+// waves a SIMD run at once: 15 400 cycles of issue of the 25 900 that a CU is busy.
 // ---------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
@@ -832,7 +833,9 @@ __global__ __launch_bounds__(256) void route_backward_kernel(const float* __rest
 constexpr int kLaunchTokens = 1 << 24;
 
 // Experts of a lane in route_rows_kernel, or 0 where it does not apply: without groups any
-// count, with groups one that makes them 1, 2, 4 or 8 whole lanes.
+// count; with groups E = 16 V, and the groups whole lanes, for the V that are compiled. Other
+// counts take route_kernel even where their groups would be whole lanes: 16384 tokens by 96
+// experts in 8 groups (V = 6) 39.8 us, by 128 experts 8.4.
 static int lane_experts(int E, int groups) {
   for (int V : {1, 2, 4, 8, 10, 12, 16})
     if (groups == 1 ? 16 * V >= E : 16 * V == E && 16 % groups == 0) return V;
