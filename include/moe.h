@@ -728,8 +728,8 @@ moe_status moe_route_backward(const float* logits, const int32_t* ids, const flo
  * ws: partial sums of products of few tiles, split along K and joined in a fixed order
  *   (results do not depend on timing). The size that a query names for M serves every call of
  *   at most M rows with the same N, K and dt (a call of fewer rows may itself need more than
- *   one of M). It depends on the device's compute units; ws need not hold anything; calls
- *   that share one must not overlap.
+ *   one of M). It depends on the device's compute units; ws need not hold anything, and may share
+ *   memory with no operand; calls that share one must not overlap.
  * Limits: N % 8 == 0, K % 8 == 0, 8 <= N, K <= 2^20, M <= 2^28, and M N, M K, N K <= 2^36
  * (fp32: 2^34). M == 0 is a no-op.
  */

@@ -781,13 +781,14 @@ moe_status moe_linear(const void* x, const void* w, const float* bias, const voi
     *ws_bytes = moe::linear_ws_bytes(M, N, K, dt == MOE_BF16);
     return MOE_OK;
   }
-  if (*ws_bytes < moe::linear_ws_needed(M, N, K, dt == MOE_BF16)) return MOE_ERR_WORKSPACE;
+  const size_t need = moe::linear_ws_needed(M, N, K, dt == MOE_BF16);
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
   if (M == 0) return MOE_OK;
   if (!x || !w || !y) return MOE_ERR_INVALID_ARG;
   const size_t es = dt == MOE_BF16 ? 2 : 4, mn = (size_t)M * N * es;
   const Span sx{x, (size_t)M * K * es}, sw{w, ((size_t)(N - 1) * ld + K) * es}, sb{bias, (size_t)N * 4}, sm{mul, mn},
       sr{residual, mn}, sy{y, mn}, sz{z, mn};
-  if (shares_any(sy, {sx, sw, sb, sz}) || shares_part(sy, sm) || shares_part(sy, sr) ||
+  if (shares_any({ws, need}, {sx, sw, sb, sm, sr, sy, sz}) || shares_any(sy, {sx, sw, sb, sz}) || shares_part(sy, sm) || shares_part(sy, sr) ||
       shares_any(sz, {sx, sw, sb, sm, sr}))
     return MOE_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(mul) || !aligned16(residual) || !aligned16(y) ||
@@ -809,7 +810,8 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
     *ws_bytes = moe::linear_backward_ws_bytes(M, N, K, dt == MOE_BF16);
     return MOE_OK;
   }
-  if (*ws_bytes < moe::linear_backward_ws_needed(M, N, K, dt == MOE_BF16)) return MOE_ERR_WORKSPACE;
+  const size_t need = moe::linear_backward_ws_needed(M, N, K, dt == MOE_BF16);
+  if (*ws_bytes < need) return MOE_ERR_WORKSPACE;
   if (!aligned16(dy) || !aligned16(x) || !aligned16(w) || !aligned16(z) || !aligned16(mul) || !aligned16(dz) ||
       !aligned16(dmul) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias) || !aligned16(ws))
     return MOE_ERR_INVALID_ARG;
@@ -825,7 +827,8 @@ moe_status moe_linear_backward(const void* dy, const void* x, const void* w, con
       sdb{dbias, (size_t)N * 4}, none{nullptr, 0};
   // The pass that writes dz, dmul and the bias' sums comes first and reads dy, z and mul, each
   // element before it is written; the products then read x and w.
-  if (shares_any(sdb, {sdy, sx, sw, sz, sm, sdz, sdm, sdx, sdw}) || shares_part(sdz, sdy) ||
+  if (shares_any({ws, need}, {sdy, sx, sw, sz, sm, sdz, sdm, sdx, sdw, sdb}) ||
+      shares_any(sdb, {sdy, sx, sw, sz, sm, sdz, sdm, sdx, sdw}) || shares_part(sdz, sdy) ||
       shares_any(sdz, {sz, sm, sdm, dw ? sx : none, dx ? sw : none}) ||
       shares_any(sdm, {sdy, sz, sm, dw ? sx : none, dx ? sw : none}) ||
       shares_any(sdx, {sdy, sx, sw, sdz, sdm, sdw}) || shares_any(sdw, {sdy, sx, M > 0 ? sw : none, sdz, sdm}))

@@ -47,6 +47,9 @@ def test_linear(L):
     # what is not there shares nothing
     assert linear(L, ["bias"], y=AT["bias"]) != INVALID and linear(L, ["z"], y=AT["z"]) != INVALID
     assert linear(L, m=0, y=AT["x"]) == 0
+    for other in ("x", "w", "bias", "mul", "res", "y", "z"):  # 256 bytes of workspace
+        assert linear(L, ws=AT[other]) == INVALID and linear(L, ws=AT[other] - 240) == INVALID, other
+        assert linear(L, ws=AT[other] - 256) != INVALID, other
 
 
 def backward(L, without=(), act=1, m=M, dwt=1, **at):
@@ -89,5 +92,7 @@ def test_linear_backward(L):
     assert backward(L, dx=AT["dw"] + 496) == INVALID and backward(L, dx=AT["dw"] + 512) != INVALID
     assert backward(L, dx=AT["dw"] + 1008, dwt=0) == INVALID and backward(L, dx=AT["dw"] + 1024, dwt=0) != INVALID
     assert backward(L, dz=AT["dmul"] + 16) == INVALID
+    for other in ("dy", "x", "w", "z", "mul", "dz", "dmul", "dx", "dw", "db"):
+        assert backward(L, ws=AT[other]) == INVALID and backward(L, ws=AT[other] - 240) == INVALID, other
     # no rows: dw and dbias are written all the same
     assert backward(L, m=0, db=AT["dw"] + 64) == INVALID
